@@ -15,6 +15,15 @@
  *                   ring of expert slots on a copy stream while the compute
  *                   stream runs the experts whose weights have landed
  *
+ * and the attention half of the same decoder layer:
+ *
+ *   moe_rope, moe_rope_cache   rotary positions; keys and values quantized
+ *                   into a paged e4m3 cache as they are written
+ *   moe_cache_read  cached sequences back as packed bf16
+ *   moe_attn_prefill  attention over packed prompts, grouped heads
+ *   moe_attn_decode  attention of one token per sequence over the cache,
+ *                   a prefix that all sequences share computed once
+ *
  * Conventions (all entry points):
  *   - Every pointer is owned by the caller.  "device" pointers are HIP device
  *     memory of the current device; "pinned host" pointers come from
@@ -56,6 +65,11 @@ typedef enum {
 /* Bits OR-ed into the optional device status word by moe_permute. */
 #define MOE_DEV_BAD_EXPERT_ID 1  /* an id outside [0, n_experts) */
 #define MOE_DEV_DUP_EXPERT_ID 2  /* the same id twice in one token's top-k */
+/* Bits OR-ed in by the rotary, cache and attention calls. */
+#define MOE_DEV_BAD_POSITION 4   /* a position outside the rotary table */
+#define MOE_DEV_BAD_SLOT 8       /* a cache slot beyond the last page */
+#define MOE_DEV_BAD_PAGE 16      /* a page id outside [0, n_pages) */
+#define MOE_DEV_BAD_LENGTH 32    /* lengths or offsets that leave their tensors or page tables */
 
 /* Kernel family used by moe_expert_ffn.  AUTO picks DECODE for
  * tokens <= MOE_DECODE_MAX_TOKENS, else PREFILL; both compute the same
@@ -429,6 +443,179 @@ typedef struct {
 #define MOE_SOP_RECORD_OFF 6
 moe_status_t moe_stream_schedule(moe_dims_t dims, int32_t T, int32_t chunk_tokens, int32_t ring_slots,
                                  uint8_t* off_recorded, moe_stream_op_t* ops, int32_t cap, int32_t* n_ops);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Attention half of the layer.
+ *
+ * q_heads query heads read kv_heads key/value heads: head h reads key/value
+ * head h / (q_heads / kv_heads).  Activations are bf16 rows [tokens, heads,
+ * head_dim]; the heads of a token are contiguous, consecutive tokens lie
+ * *_stride elements apart (a multiple of 8, at least heads * head_dim), so q,
+ * k and v may be views of one packed projection.  Activation pointers are
+ * 16-byte aligned.  Requires head_dim 64 or 128, 1 <= kv_heads <= q_heads <=
+ * 1024, q_heads % kv_heads == 0; else MOE_ERR_UNSUPPORTED_SHAPE.
+ * ---------------------------------------------------------------------------
+ */
+typedef struct {
+  int32_t q_heads;
+  int32_t kv_heads;
+  int32_t head_dim;
+} moe_attn_dims_t;
+
+/*
+ * Paged key/value cache of one layer.  A page holds page_size tokens (a power
+ * of two, 16..1024): per head the e4m3 codes of its tokens' rows, and one fp32
+ * scale per token and head; value = code * scale.  Slot s is token s %
+ * page_size of page s / page_size.  Which pages a sequence owns, in order, is
+ * the caller's page table.  Nothing needs clearing: what lies in slots behind
+ * a sequence's length is never used, whatever its bits.
+ */
+typedef struct {
+  uint8_t* k;       /* device e4m3 [n_pages, kv_heads, page_size, head_dim], 16-byte aligned */
+  uint8_t* v;       /* as k */
+  float* k_scale;   /* device fp32 [n_pages, kv_heads, page_size], 16-byte aligned */
+  float* v_scale;   /* as k_scale */
+  int32_t n_pages;  /* >= 1 */
+  int32_t page_size;
+} moe_kv_cache_t;
+
+/*
+ * Rotary positions.  Pair i (0 <= i < rot_dim / 2) of a head at position p
+ * turns by the angle p * f_i:
+ *   y0 = x0 cos - x1 sin,  y1 = x1 cos + x0 sin
+ * in fp32, every product and sum rounded separately.  The pair is elements
+ * (i, i + rot_dim / 2) in the HALF layout and (2i, 2i + 1) in the INTERLEAVED
+ * one; elements rot_dim .. head_dim - 1 are kept.
+ */
+typedef enum {
+  MOE_ROPE_HALF = 0,
+  MOE_ROPE_INTERLEAVED = 1
+} moe_rope_layout_t;
+
+/* Frequencies f_i from g_i = base^(-2i / rot_dim):
+ *   PLAIN     f_i = g_i
+ *   LINEAR    f_i = g_i / factor (positions interpolated)
+ *   BY_PARTS  f_i = g_i / factor where pair i turns less than slow_turns times
+ *             over the original context of original_len positions, g_i where
+ *             it turns more than fast_turns times, in between mixed linearly in
+ *             the number of turns: with r = original_len g_i / 2 pi and
+ *             w = clamp((r - slow_turns) / (fast_turns - slow_turns), 0, 1),
+ *             f_i = (1 - w) g_i / factor + w g_i. */
+typedef enum {
+  MOE_ROPE_PLAIN = 0,
+  MOE_ROPE_LINEAR = 1,
+  MOE_ROPE_BY_PARTS = 2
+} moe_rope_scaling_t;
+
+typedef struct {
+  int32_t rot_dim;       /* rotated elements per head: a multiple of 16, 16..head_dim */
+  int32_t scaling;       /* moe_rope_scaling_t */
+  double base;           /* > 1 */
+  double factor;         /* LINEAR, BY_PARTS: > 0 */
+  double original_len;   /* BY_PARTS: > 0 */
+  double slow_turns;     /* BY_PARTS: 0 <= slow_turns < fast_turns */
+  double fast_turns;
+  double magnitude;      /* factor on all cosines and sines (1 without attention scaling) */
+} moe_rope_cfg_t;
+
+/*
+ * The table that the calls below read: row p (0 <= p < n_pos) holds the
+ * rot_dim / 2 cosines and then the rot_dim / 2 sines of position p, angles and
+ * functions in 64 bits, rounded once.  table: device fp32 [n_pos, rot_dim],
+ * 16-byte aligned.  Set-up, not part of a layer call.
+ */
+moe_status_t moe_rope_table(moe_rope_cfg_t cfg, int32_t n_pos, float* table, hipStream_t stream);
+
+/*
+ * Rotates queries and keys: q_out, k_out = bf16 of the rotated q, k (contiguous
+ * rows; may be the inputs where these are contiguous).  positions: device
+ * int32 [T]; one outside [0, n_pos) sets MOE_DEV_BAD_POSITION and leaves that
+ * token's outputs unspecified.  Either of q and k may be NULL with its output.
+ */
+moe_status_t moe_rope(moe_attn_dims_t dims, int32_t T, const uint16_t* q, int64_t q_stride, const uint16_t* k,
+                      int64_t k_stride, const int32_t* positions, const float* table, int32_t n_pos, int32_t rot_dim,
+                      moe_rope_layout_t layout, uint16_t* q_out, uint16_t* k_out, int32_t* dev_status,
+                      hipStream_t stream);
+
+/*
+ * moe_rope, and the rotated keys and the values written into the cache, one
+ * launch.  Per token and head: s = max|y| / 448 and code = e4m3(y / s) by the
+ * rule of moe_quant_act over the head's head_dim elements; y is the fp32
+ * rotated key (not rounded to bf16 in between) or the value.
+ * slots: device int32 [T], each token's slot; a negative one leaves the
+ * token unwritten (padding), one past the last page sets MOE_DEV_BAD_SLOT and
+ * leaves it unwritten.  Slots must be distinct.  k_out may be NULL (prompts'
+ * attention wants it, a decode step does not).
+ */
+moe_status_t moe_rope_cache(moe_attn_dims_t dims, int32_t T, const uint16_t* q, int64_t q_stride, const uint16_t* k,
+                            int64_t k_stride, const uint16_t* v, int64_t v_stride, const int32_t* positions,
+                            const float* table, int32_t n_pos, int32_t rot_dim, moe_rope_layout_t layout,
+                            const int32_t* slots, moe_kv_cache_t cache, uint16_t* q_out, uint16_t* k_out,
+                            int32_t* dev_status, hipStream_t stream);
+
+/*
+ * Reads cached sequences back: rows cu[b] .. cu[b+1] - 1 of k_out and v_out =
+ * bf16(code * scale) of the first cu[b+1] - cu[b] tokens that row b of the page
+ * table holds.  page_table: device int32 [B, table_width], rows contiguous.
+ * cu: device int32 [B + 1], not decreasing, 0..T.  k_out, v_out:
+ * device bf16 [T, kv_heads, head_dim], contiguous; rows outside all sequences
+ * are not written.  A page id outside the cache or a sequence longer than its
+ * table row sets MOE_DEV_BAD_PAGE / MOE_DEV_BAD_LENGTH and its rows get zeros.
+ * q_heads is not looked at beyond the check of dims.
+ */
+moe_status_t moe_cache_read(moe_attn_dims_t dims, moe_kv_cache_t cache, const int32_t* page_table, int32_t B,
+                            int32_t table_width, const int32_t* cu, int32_t T, uint16_t* k_out, uint16_t* v_out,
+                            int32_t* dev_status, hipStream_t stream);
+
+/*
+ * Attention over packed prompts:
+ *   out[i] = sum_j softmax_j(scale * q[i] . k[j]) v[j]
+ * over the keys j of i's own sequence; with causal != 0 over those up to i's
+ * place, sequences' ends aligned: query i of lq sees keys 0 .. i + lk - lq (a
+ * chunk of queries behind keys that are cached already).  A query that sees no
+ * key gets zeros.  Scores, the running maximum and sum and the accumulation are
+ * fp32; the softmax's numerators are rounded to bf16 for the product with v.
+ *
+ * Sequence b: queries cu_q[b] .. cu_q[b+1] - 1 of T_q, keys cu_k[b] ..
+ * cu_k[b+1] - 1 of T_k (device int32 [B + 1], not decreasing); offsets that
+ * leave the tensors are cut to them and set MOE_DEV_BAD_LENGTH.  Rows
+ * of out outside all sequences are not written.  max_k: the longest sequence's
+ * number of keys; it decides how the work is split and nothing else.  q:
+ * [T_q, q_heads, head_dim]; k, v: [T_k, kv_heads, head_dim]; out: contiguous
+ * [T_q, q_heads, head_dim], no overlap with the inputs.  scale > 0.
+ * ws: moe_attn_prefill_workspace(dims, B, T_q, max_k) bytes, 256-byte aligned.
+ */
+size_t moe_attn_prefill_workspace(moe_attn_dims_t dims, int32_t B, int32_t T_q, int32_t max_k);
+moe_status_t moe_attn_prefill(moe_attn_dims_t dims, int32_t B, int32_t T_q, int32_t T_k, int32_t max_k,
+                              const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride,
+                              const uint16_t* v, int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k,
+                              float scale, int32_t causal, uint16_t* out, int32_t* dev_status, void* ws,
+                              size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Attention of one token per sequence over the cache: out[b] as above over the
+ * prefix's keys and then the first lens[b] tokens of row b of the page table
+ * (the new token's own among them: moe_rope_cache comes first).
+ *
+ * prefix_pages: device int32, the pages of the first prefix_len tokens that
+ * all sequences share (a prompt's prefix written once); NULL with prefix_len
+ * 0.  The prefix is read once for the whole batch: every sequence's queries are
+ * rows of one product.  page_table: device int32 [B, table_width], entries
+ * behind a sequence's last page are not read.  lens: device int32 [B], 0 for
+ * an idle slot (with no prefix either its output is zeros).  A length below 0
+ * or beyond table_width pages is cut and sets MOE_DEV_BAD_LENGTH; a page id
+ * outside the cache sets MOE_DEV_BAD_PAGE and leaves the outputs that need it
+ * unspecified.  max_len: the longest of lens; it decides how the work is split
+ * and nothing else.  q: [B, q_heads, head_dim]; out contiguous, no overlap.
+ * ws: moe_attn_decode_workspace(dims, B, max_len, prefix_len) bytes, 256-byte
+ * aligned.
+ */
+size_t moe_attn_decode_workspace(moe_attn_dims_t dims, int32_t B, int32_t max_len, int32_t prefix_len);
+moe_status_t moe_attn_decode(moe_attn_dims_t dims, int32_t B, const uint16_t* q, int64_t q_stride, moe_kv_cache_t cache,
+                             const int32_t* page_table, int32_t table_width, const int32_t* lens, int32_t max_len,
+                             const int32_t* prefix_pages, int32_t prefix_len, float scale, uint16_t* out,
+                             int32_t* dev_status, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
  * Diagnostics: per-launch kernel timing.  After moe_profile_begin(n), every

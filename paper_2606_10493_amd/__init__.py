@@ -1,4 +1,4 @@
-"""MI355X (gfx950) routed-expert FP8 MoE FFN.
+"""MI355X (gfx950) routed-expert FP8 MoE FFN, and the attention half of its decoder layer.
 
 Thin Python binding of libmoe.so (the C ABI in include/moe.h).  Functions
 carry the C names and only marshal arguments: every step of the layer runs
@@ -16,7 +16,9 @@ from ._lib import (  # noqa: F401
     MOE_ERR_WORKSPACE, MOE_ERR_HIP, MOE_REGIME_AUTO, MOE_REGIME_DECODE, MOE_REGIME_PREFILL,
     MOE_DEV_BAD_EXPERT_ID, MOE_DEV_DUP_EXPERT_ID, MOE_DECODE_MAX_TOKENS, MOE_NOALLOC_SCRATCH_BYTES, MoeDims,
     MoeRouterCfg, MoeStreamOp, MOE_SOP_WAIT_OFF, MOE_SOP_COPY, MOE_SOP_RECORD_ON, MOE_SOP_WAIT_ON, MOE_SOP_LAUNCH,
-    MOE_SOP_RECORD_OFF,
+    MOE_SOP_RECORD_OFF, MoeAttnDims, MoeKvCache, MoeRopeCfg, MOE_DEV_BAD_POSITION, MOE_DEV_BAD_SLOT,
+    MOE_DEV_BAD_PAGE, MOE_DEV_BAD_LENGTH, MOE_ROPE_HALF, MOE_ROPE_INTERLEAVED, MOE_ROPE_PLAIN, MOE_ROPE_LINEAR,
+    MOE_ROPE_BY_PARTS,
     EXPORTED_SYMBOLS,
 )
 from ._lib import check as _check
@@ -284,4 +286,7 @@ def moe_profile_end():
     return out
 
 
+from .attention import (  # noqa: E402,F401
+    AttentionBuffers, KVCache, moe_attn_decode, moe_attn_decode_workspace, moe_attn_prefill,
+    moe_attn_prefill_workspace, moe_cache_read, moe_rope, moe_rope_cache, moe_rope_table, run_attention)
 from .layer import MoELayerBuffers, run_layer  # noqa: E402,F401

@@ -21,6 +21,17 @@ MOE_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 MOE_DEV_BAD_EXPERT_ID = 1
 MOE_DEV_DUP_EXPERT_ID = 2
+MOE_DEV_BAD_POSITION = 4
+MOE_DEV_BAD_SLOT = 8
+MOE_DEV_BAD_PAGE = 16
+MOE_DEV_BAD_LENGTH = 32
+
+MOE_ROPE_HALF = 0
+MOE_ROPE_INTERLEAVED = 1
+
+MOE_ROPE_PLAIN = 0
+MOE_ROPE_LINEAR = 1
+MOE_ROPE_BY_PARTS = 2
 
 MOE_SOP_WAIT_OFF = 1
 MOE_SOP_COPY = 2
@@ -44,6 +55,21 @@ class MoeStreamOp(ctypes.Structure):
     _fields_ = [("op", ctypes.c_int32), ("a", ctypes.c_int32), ("b", ctypes.c_int32), ("c", ctypes.c_int32)]
 
 
+class MoeAttnDims(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class MoeKvCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class MoeRopeCfg(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original_len", ctypes.c_double), ("slow_turns", ctypes.c_double),
+                ("fast_turns", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
 class MoEError(RuntimeError):
     def __init__(self, status: int, detail: str):
         self.status = status
@@ -64,6 +90,8 @@ lib = ctypes.CDLL(LIB_PATH)
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _S = ctypes.c_size_t
+_L = ctypes.c_int64
+_F = ctypes.c_float
 _ST = ctypes.c_int
 
 _SIGS = {
@@ -94,6 +122,16 @@ _SIGS = {
     "moe_stream_schedule": (_ST, [MoeDims, _I, _I, _I, _P, _P, _I, ctypes.POINTER(ctypes.c_int32)]),
     "moe_ffn_streamed": (_ST, [MoeDims, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _S,
                                 _P, _P]),
+    "moe_rope_table": (_ST, [MoeRopeCfg, _I, _P, _P]),
+    "moe_rope": (_ST, [MoeAttnDims, _I, _P, _L, _P, _L, _P, _P, _I, _I, _ST, _P, _P, _P, _P]),
+    "moe_rope_cache": (_ST, [MoeAttnDims, _I, _P, _L, _P, _L, _P, _L, _P, _P, _I, _I, _ST, _P, MoeKvCache, _P, _P, _P,
+                             _P]),
+    "moe_cache_read": (_ST, [MoeAttnDims, MoeKvCache, _P, _I, _I, _P, _I, _P, _P, _P, _P]),
+    "moe_attn_prefill_workspace": (_S, [MoeAttnDims, _I, _I, _I]),
+    "moe_attn_prefill": (_ST, [MoeAttnDims, _I, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _P, _F, _I, _P, _P, _P, _S,
+                               _P]),
+    "moe_attn_decode_workspace": (_S, [MoeAttnDims, _I, _I, _I]),
+    "moe_attn_decode": (_ST, [MoeAttnDims, _I, _P, _L, MoeKvCache, _P, _I, _P, _I, _P, _I, _F, _P, _P, _P, _S, _P]),
     "moe_profile_begin": (_ST, [_I]),
     "moe_profile_end": (_I, []),
     "moe_profile_get": (_ST, [_I, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_char_p)]),
