@@ -1,16 +1,27 @@
-// Attention of one token per sequence over the paged e4m3 cache.
+// Attention of one token per sequence over the paged e4m3 cache, behind a
+// prefix that all sequences share.
 //
-// The G query heads of a key/value head are the columns of 16x16x32 bf16
-// MFMAs (16 of them, padded), so a key's codes are read and converted once for
-// the group:
-//   S^T = K Q^T   keys' codes go from the pages to registers as the first
-//                 operand (lane: key lane % 16, 16 codes at 16 (lane / 16) of
-//                 each 64), converted to bf16 exactly; a lane ends with the scores
-//                 of query lane % 16 for keys 4 (lane / 16) + i
-//   O^T = V^T P^T values' codes go through LDS and come back transposed
+// The query heads of a key/value head are the columns of 16x16x32 MFMAs, so a
+// key's codes are read and converted once for all of them.  A sequence's own keys
+// have its G query heads as columns, the prefix's keys those of all sequences
+// (B * G columns), so the prefix is read once for the batch.
+//   S^T = K Q^T   (bf16) keys' codes go from the pages to registers as the
+//                 first operand (lane: key lane % 16, 16 codes at 16 (lane / 16)
+//                 of each 64), converted exactly; a lane ends with the scores of
+//                 query lane % 16 for keys 4 (lane / 16) + i
+//   O^T = V^T P^T (f16) values' codes go through LDS and come back transposed
 //                 (ds_read_b64_tr_b8) in the order of keys that the scores have
-// Scales stay fp32: a key's multiplies its score, a value's its softmax numerator,
-// which is rounded to bf16 once.
+// Scales stay fp32: a key's multiplies its score, a value's its numerator.  The
+// numerators are rounded once for the product, to f16: a code is exact in f16 as
+// it is in bf16, and f16 has three bits more.  Its range is kept by dividing the
+// values' scales by their running maximum (`vref`), which rescales the
+// accumulator as the running maximum of the scores does; what underflows is
+// below 2^-25 of the largest term.
+//
+// Bound by memory: head_dim + 4 bytes per key, value and head against 4 * G *
+// head_dim flops.  One long context has few rows, so keys are cut into parts, one
+// workgroup each, whose waves take every fourth step of 32 keys; a second launch
+// joins the parts.
 #include <math.h>
 
 #include <algorithm>
@@ -27,188 +38,425 @@ struct DecodeArgs {
   moe_kv_cache_t cache;
   const int32_t *pages, *lens, *prefix_pages;
   uint16_t* out;
+  float* part_o;   // [B * q_heads][slots][D]: a part's sums, not divided
+  float* part_ml;  // [B * q_heads][slots][2]: its running maximum and sum
   int32_t* status;
   int B, width, prefix_len, kv_heads, group, page_shift;
-  float c;  // scale * log2(e)
+  int part_keys, prefix_parts, own_parts;  // slots: the prefix's parts, then a sequence's own
+  int prefix_blocks, own_blocks;           // column blocks of all sequences' and of one's queries
+  float c;                                 // scale * log2(e)
 };
 
-constexpr int kKeys = 32;   // keys per step of a wave
+constexpr int kKeys = 32;  // keys per step of a wave
 constexpr int kWaves = 4;
-constexpr int kCols = 16;   // queries per product
+constexpr int kStride = kKeys * kWaves;
 
-// One wave's running softmax: lane's query is column lane % 16.
-template <int D>
-struct Running {
-  v4f o[D / 16];  // O^T: rows 16 i + 4 (lane / 16) + 0..3
-  float m, l;     // l: this lane's keys only, summed over the lane groups at the end
-};
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
-__device__ __forceinline__ int page_at(const DecodeArgs& a, const int32_t* pages, int index) {
-  const int p = pages[index];
-  if (p >= 0 && p < a.cache.n_pages) return p;
-  if (a.status && (threadIdx.x & 63) == 0) atomicOr(a.status, MOE_DEV_BAD_PAGE);
-  return 0;  // in bounds; the outputs that need it are unspecified
+__device__ __forceinline__ v8h e4m3x8_to_f16(uint32_t lo, uint32_t hi) {
+  union {
+    v8h v;
+    v2h p[4];
+  } r;
+  r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false);
+  r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+  r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false);
+  r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+  return r.v;
 }
 
-// Keys [t0, t0 + 32) of the `len` that `pages` hold.
+// The running softmax of NC blocks of 16 queries; a lane's query is column
+// lane % 16 of each block.
+template <int D, int NC>
+struct Running {
+  v4f o[NC][D / 16];     // O^T / vref: rows 16 i + 4 (lane / 16) + 0..3
+  float m[NC], l[NC];    // l: this lane's keys only, summed over the lane groups at the end
+  float vref;
+};
+
+// 32 keys and values on their way.
 template <int D>
-__device__ __forceinline__ void step(const DecodeArgs& a, const int32_t* pages, int len, int t0, int kvh,
-                                     const v8bf (&qf)[D / 32], uint8_t* lds_v, Running<D>& run) {
+struct Tile {
+  uint4 k[2][D / 64], v[D / 32];
+  float4 ks[2], vs[2];
+};
+
+// A part of one sequence's (or the prefix's) keys: [begin, end) of the `len`
+// that `pages` hold, key/value head kvh.
+struct Part {
+  const int32_t* pages;
+  int len, begin, end, kvh;
+};
+
+// Keys [t, t + 32) lie in one page or two: each half of 16 in one.
+struct Pages {
+  int id[2];
+};
+__device__ __forceinline__ Pages pages_of(const DecodeArgs& a, const Part& p, int t) {
+  Pages r;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) r.id[u] = p.pages[min(t + 16 * u, p.len - 1) >> a.page_shift];
+  return r;
+}
+
+template <int D>
+__device__ __forceinline__ int value_place(int row, int c) {
+  const int f = D == 128 ? ((row >> 1) & 3) | ((row >> 2) & 4) : ((row >> 2) & 1) | ((row >> 3) & 2);
+  return row * D + ((c ^ f) * 16);
+}
+
+template <int D>
+__device__ __forceinline__ void load_tile(const DecodeArgs& a, const Part& p, int t0, const Pages& pg, bool& bad,
+                                          Tile<D>& x) {
+  constexpr int kChunks = D / 16;
   const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
-  const int mask = a.cache.page_size - 1, last = len - 1;
-  // each half of 16 keys lies in one page; keys behind the end repeat the last
+  const int mask = a.cache.page_size - 1, last = p.len - 1;
   int64_t base[2];
-  int row0[2];
+  int row0[2];  // keys behind the end repeat the last
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    const int t = min(t0 + 16 * u, last) & ~15;
-    base[u] = ((int64_t)page_at(a, pages, t >> a.page_shift) * a.kv_heads + kvh) << a.page_shift;
-    row0[u] = t;
+    const bool wrong = pg.id[u] < 0 || pg.id[u] >= a.cache.n_pages;
+    bad |= wrong;
+    row0[u] = min(t0 + 16 * u, last) & ~15;
+    base[u] = ((int64_t)(wrong ? 0 : pg.id[u]) * a.kv_heads + p.kvh) << a.page_shift;
   }
-  v4f s[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int t = min(row0[u] + c16, last) & mask;
     const uint8_t* krow = a.cache.k + (base[u] + t) * D + 16 * g;
-    s[u] = v4f{};
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      const uint4 x = *reinterpret_cast<const uint4*>(krow + 64 * i);
-      s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e4m3x8_to_bf16(x.x, x.y), qf[2 * i], s[u], 0, 0, 0);
-      s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e4m3x8_to_bf16(x.z, x.w), qf[2 * i + 1], s[u], 0, 0, 0);
-    }
+    for (int i = 0; i < D / 64; ++i) x.k[u][i] = *reinterpret_cast<const uint4*>(krow + 64 * i);
   }
-  // values to LDS: rows of D codes, 16-byte chunks swizzled
-  constexpr int kChunks = D / 16;
-  const auto place = [](int row, int c) {
-    const int f = D == 128 ? ((row >> 1) & 3) | ((row >> 2) & 4) : ((row >> 2) & 1) | ((row >> 3) & 2);
-    return row * D + ((c ^ f) * 16);
-  };
 #pragma unroll
-  for (int i = 0; i < 32 * kChunks / 64; ++i) {
-    const int p = 64 * i + lane, row = p / kChunks, c = p % kChunks, u = row >> 4;
-    const int t = min(row0[u] + (row & 15), last) & mask;
-    *reinterpret_cast<uint4*>(lds_v + place(row, c)) =
-        *reinterpret_cast<const uint4*>(a.cache.v + ((u ? base[1] : base[0]) + t) * D + 16 * c);
+  for (int i = 0; i < D / 32; ++i) {
+    const int at = 64 * i + lane, row = at / kChunks, c = at % kChunks, u = row >> 4;
+    const int t = min((u ? row0[1] : row0[0]) + (row & 15), last) & mask;
+    x.v[i] = *reinterpret_cast<const uint4*>(a.cache.v + ((u ? base[1] : base[0]) + t) * D + 16 * c);
   }
-  float vs[2][4];
-  float top = -INFINITY;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int64_t at = base[u] + (row0[u] & mask) + 4 * g;
-    const float4 ks = *reinterpret_cast<const float4*>(a.cache.k_scale + at);
-    const float4 vv = *reinterpret_cast<const float4*>(a.cache.v_scale + at);
-    const float kk[4] = {ks.x, ks.y, ks.z, ks.w}, vx[4] = {vv.x, vv.y, vv.z, vv.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool there = t0 + 16 * u + 4 * g + i < len;  // a slot behind the end may hold any bits
-      s[u][i] = there ? s[u][i] * (kk[i] * a.c) : -INFINITY;
-      vs[u][i] = there ? vx[i] : 0.0f;
-      top = fmaxf(top, s[u][i]);
-    }
+    x.ks[u] = *reinterpret_cast<const float4*>(a.cache.k_scale + at);
+    x.vs[u] = *reinterpret_cast<const float4*>(a.cache.v_scale + at);
   }
-  top = fmaxf(top, __shfl_xor(top, 16, 64));
-  top = fmaxf(top, __shfl_xor(top, 32, 64));
-  const float m = fmaxf(run.m, top), alpha = __builtin_amdgcn_exp2f(run.m - m);
-  run.m = m;
-  float sum = 0.0f;
-  union {
-    v8bf v;
-    uint32_t x[4];
-  } p;
+}
+
+template <int D, int NC>
+__device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int t0, const Tile<D>& x,
+                                         const v8bf (&qf)[NC][D / 32], uint8_t* lds_v, Running<D, NC>& run) {
+  constexpr int kChunks = D / 16;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    const int at = 64 * i + lane;
+    *reinterpret_cast<uint4*>(lds_v + value_place<D>(at / kChunks, at % kChunks)) = x.v[i];
+  }
+  v4f s[NC][2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    float e[4];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) s[n][u] = v4f{};
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const v8bf lo = e4m3x8_to_bf16(x.k[u][i].x, x.k[u][i].y), hi = e4m3x8_to_bf16(x.k[u][i].z, x.k[u][i].w);
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        s[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, qf[n][2 * i], s[n][u], 0, 0, 0);
+        s[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, qf[n][2 * i + 1], s[n][u], 0, 0, 0);
+      }
+    }
+  }
+  float ks[2][4], vs[2][4];
+  float vtop = run.vref;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const float kk[4] = {x.ks[u].x, x.ks[u].y, x.ks[u].z, x.ks[u].w}, vv[4] = {x.vs[u].x, x.vs[u].y, x.vs[u].z, x.vs[u].w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      e[i] = __builtin_amdgcn_exp2f(s[u][i] - m);
-      sum += e[i];
-      e[i] *= vs[u][i];
+      const bool there = t0 + 16 * u + 4 * g + i < p.len;  // a slot behind the end may hold any bits
+      ks[u][i] = there ? kk[i] * a.c : -1.0f;              // scales are not negative
+      vs[u][i] = there ? vv[i] : 0.0f;
+      vtop = fmaxf(vtop, vs[u][i]);
     }
-    p.x[2 * u] = pack_bf16(e[0], e[1]);
-    p.x[2 * u + 1] = pack_bf16(e[2], e[3]);
   }
-  run.l = run.l * alpha + sum;
+  vtop = fmaxf(vtop, __shfl_xor(vtop, 16, 64));
+  vtop = fmaxf(vtop, __shfl_xor(vtop, 32, 64));
+  const float inv = 1.0f / vtop, faded = run.vref * inv;
+  run.vref = vtop;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vs[u][i] *= inv;
+
+  union {
+    v8h v;
+    v2h x[4];
+  } pf[NC];
+  float fade[NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[n][u][i] = ks[u][i] >= 0.0f ? s[n][u][i] * ks[u][i] : -INFINITY;
+        top = fmaxf(top, s[n][u][i]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float m = fmaxf(run.m[n], top), alpha = __builtin_amdgcn_exp2f(run.m[n] - m);
+    run.m[n] = m;
+    float sum = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float e[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(s[n][u][i] - m);
+        sum += e[i];
+        e[i] *= vs[u][i];
+      }
+      pf[n].x[2 * u] = v2h{(_Float16)e[0], (_Float16)e[1]};
+      pf[n].x[2 * u + 1] = v2h{(_Float16)e[2], (_Float16)e[3]};
+    }
+    run.l[n] = run.l[n] * alpha + sum;
+    fade[n] = alpha * faded;
+  }
   // lane j of a 16-lane group gives the address of row j / 2, half j % 2 of an 8 x 16 block and gets column j:
   // rows 0..3 are keys 4 g + 0..3, rows 4..7 keys 16 + 4 g + 0..3
   const int j = c16 >> 1, row = (j < 4 ? 0 : 12) + 4 * g + j;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
-    const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-        (__attribute__((address_space(3))) v2i*)(lds_v + place(row, i) + 8 * (c16 & 1)));
-    run.o[i] *= alpha;
-    run.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e4m3x8_to_bf16(x[0], x[1]), p.v, run.o[i], 0, 0, 0);
-  }
-}
-
-// One workgroup per (sequence, key/value head, block of 16 of its queries); the
-// waves take every fourth step and are joined through LDS.
-template <int D>
-__global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(DecodeArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds_v[kWaves][kKeys * D];
-  __shared__ float lds_o[kWaves][kCols][D + 4];
-  __shared__ float lds_m[kWaves][kCols], lds_l[kWaves][kCols];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c16 = lane & 15;
-  const int b = blockIdx.x, kvh = blockIdx.y, col0 = blockIdx.z * kCols;
-  const int cols = min(kCols, a.group - col0);
-  const int head0 = kvh * a.group + col0;
-
-  v8bf qf[D / 32];
-  const uint16_t* qrow = a.q + b * a.q_stride + (head0 + min(c16, cols - 1)) * D + 16 * g;
+    const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+        (__attribute__((address_space(3))) v2i*)(lds_v + value_place<D>(row, i) + 8 * (c16 & 1)));
+    const v8h vf = e4m3x8_to_f16(y[0], y[1]);
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    qf[2 * i] = *reinterpret_cast<const v8bf*>(qrow + 64 * i);
-    qf[2 * i + 1] = *reinterpret_cast<const v8bf*>(qrow + 64 * i + 8);
-  }
-  Running<D> run;
-  run.m = kNoScore;
-  run.l = 0.0f;
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) run.o[i] = v4f{};
-
-  int len = a.lens[b];
-  const int64_t most = min((int64_t)a.width << a.page_shift, (int64_t)0x7fffffff);
-  if (len < 0 || len > most) {
-    if (a.status && threadIdx.x == 0) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
-    len = len < 0 ? 0 : (int)most;
-  }
-  for (int t = wave * kKeys; t < a.prefix_len; t += kWaves * kKeys)
-    step<D>(a, a.prefix_pages, a.prefix_len, t, kvh, qf, lds_v[wave], run);
-  for (int t = wave * kKeys; t < len; t += kWaves * kKeys)
-    step<D>(a, a.pages + (int64_t)b * a.width, len, t, kvh, qf, lds_v[wave], run);
-
-  run.l += __shfl_xor(run.l, 16, 64);
-  run.l += __shfl_xor(run.l, 32, 64);
-  if (g == 0) {
-    lds_m[wave][c16] = run.m;
-    lds_l[wave][c16] = run.l;
-  }
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<v4f*>(&lds_o[wave][c16][16 * i + 4 * g]) = run.o[i];
-  __syncthreads();
-  for (int p = threadIdx.x; p < cols * D / 4; p += 64 * kWaves) {
-    const int col = p / (D / 4), d = p % (D / 4) * 4;
-    float m = kNoScore;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, lds_m[w][col]);
-    float l = 0.0f;
-    v4f o = {};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(lds_m[w][col] - m);
-      l += lds_l[w][col] * f;
-      o += *reinterpret_cast<const v4f*>(&lds_o[w][col][d]) * f;
+    for (int n = 0; n < NC; ++n) {
+      run.o[n][i] *= fade[n];
+      run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n].v, run.o[n][i], 0, 0, 0);
     }
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    *reinterpret_cast<uint2*>(a.out + ((int64_t)b * (a.kv_heads * a.group) + head0 + col) * D + d) =
-        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
   }
 }
 
+// Workgroups: the prefix's parts (part, column block, head), then the sequences'
+// own (part, column block, sequence, head); heads fastest, so that workgroups
+// that share keys have numbers equal mod 8 (one XCD's L2) where kv_heads is a
+// multiple of 8.
+template <int D, int NC>
+__global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(DecodeArgs a) {
+  constexpr int kCols = 16 * NC;
+  __shared__ __attribute__((aligned(16))) uint8_t lds_v[kWaves][kKeys * D];
+  __shared__ __attribute__((aligned(16))) float lds_o[kWaves][16][D + 4];
+  __shared__ float lds_m[kWaves][kCols], lds_l[kWaves][kCols];
+  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  int item = blockIdx.x;
+  const int n_prefix = a.prefix_parts * a.prefix_blocks * a.kv_heads;
+  const bool shared = item < n_prefix;
+  if (!shared) item -= n_prefix;
+  Part p;
+  p.kvh = item % a.kv_heads;
+  item /= a.kv_heads;
+  int b = 0, slot;
+  if (!shared) {
+    b = item % a.B;
+    item /= a.B;
+  }
+  const int blocks = shared ? a.prefix_blocks : a.own_blocks;
+  const int col0 = item % blocks * kCols, part = item / blocks;
+  const int cols = min(kCols, (shared ? a.B * a.group : a.group) - col0);
+  bool bad_len = false;
+  if (shared) {
+    p.pages = a.prefix_pages;
+    p.len = a.prefix_len;
+    slot = part;
+  } else {
+    p.pages = a.pages + (int64_t)b * a.width;
+    p.len = a.lens[b];
+    const int64_t most = min((int64_t)a.width << a.page_shift, (int64_t)0x7fffffff);
+    bad_len = p.len < 0 || p.len > most;
+    p.len = p.len < 0 ? 0 : (int)min((int64_t)p.len, most);
+    slot = a.prefix_parts + part;
+  }
+  const int64_t begin = (int64_t)part * a.part_keys;
+  const bool last_part = part == (shared ? a.prefix_parts : a.own_parts) - 1;
+  if (bad_len && a.status && part == 0 && threadIdx.x == 0) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
+  if (begin >= p.len && part > 0) return;  // the join looks at lens, too
+  p.begin = (int)begin;
+  p.end = last_part ? p.len : (int)min((int64_t)p.len, begin + a.part_keys);
+
+  // column n of block col0: query head (col % G) of the group, of sequence col / G in the prefix
+  const auto row_of = [&](int col) {  // row of q and out, counted in heads
+    const int s = shared ? (col0 + col) / a.group : b;
+    return (int64_t)s * (a.kv_heads * a.group) + p.kvh * a.group + (shared ? (col0 + col) % a.group : col0 + col);
+  };
+  Running<D, NC> run;
+  run.vref = 0x1p-126f;  // 1 / vref stays finite
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    run.m[n] = kNoScore;
+    run.l[n] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) run.o[n][i] = v4f{};
+  }
+  int t = p.begin + wave * kKeys;
+  if (t < p.end) {
+    v8bf qf[NC][D / 32];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      const int64_t r = row_of(min(16 * n + c16, cols - 1));
+      const int64_t heads = a.kv_heads * a.group;
+      const uint16_t* qrow = a.q + r / heads * a.q_stride + r % heads * D + 16 * g;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        qf[n][2 * i] = *reinterpret_cast<const v8bf*>(qrow + 64 * i);
+        qf[n][2 * i + 1] = *reinterpret_cast<const v8bf*>(qrow + 64 * i + 8);
+      }
+    }
+    bool bad = false;
+    Tile<D> x, y;
+    load_tile<D>(a, p, t, pages_of(a, p, t), bad, x);
+    Pages ahead = pages_of(a, p, t + kStride);
+    while (true) {
+      const bool more = t + kStride < p.end;
+      if (more) {
+        load_tile<D>(a, p, t + kStride, ahead, bad, y);
+        ahead = pages_of(a, p, t + 2 * kStride);
+      }
+      use_tile<D, NC>(a, p, t, x, qf, lds_v[wave], run);
+      if (!more) break;
+      t += kStride;
+      x = y;
+    }
+    if (bad && a.status && lane == 0) atomicOr(a.status, MOE_DEV_BAD_PAGE);
+  }
+
+  // the waves' sums joined, one block of 16 columns at a time
+  const bool whole = a.prefix_parts + a.own_parts == 1;
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    float l = run.l[n];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (g == 0) {
+      lds_m[wave][16 * n + c16] = run.m[n];
+      lds_l[wave][16 * n + c16] = l;
+    }
+    if (n > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<v4f*>(&lds_o[wave][c16][16 * i + 4 * g]) = run.o[n][i] * run.vref;
+    __syncthreads();
+    const int here = min(16, cols - 16 * n);
+    for (int at = threadIdx.x; at < here * (D / 4); at += 64 * kWaves) {
+      const int col = at / (D / 4), d = at % (D / 4) * 4;
+      float m = kNoScore;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, lds_m[w][16 * n + col]);
+      float sum = 0.0f;
+      v4f o = {};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(lds_m[w][16 * n + col] - m);
+        sum += lds_l[w][16 * n + col] * f;
+        o += *reinterpret_cast<const v4f*>(&lds_o[w][col][d]) * f;
+      }
+      const int64_t r = row_of(16 * n + col);
+      if (whole) {
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        *reinterpret_cast<uint2*>(a.out + r * D + d) =
+            make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+      } else {
+        const int64_t at_part = r * (a.prefix_parts + a.own_parts) + slot;
+        *reinterpret_cast<v4f*>(a.part_o + at_part * D + d) = o;
+        if (d == 0) *reinterpret_cast<float2*>(a.part_ml + at_part * 2) = make_float2(m, sum);
+      }
+    }
+  }
+}
+
+// One workgroup per output row: its parts' sums, weighed by their maxima.  Eight
+// (D = 128) or sixteen parts at a time, 16 bytes a lane.
 template <int D>
-moe_status_t launch_decode(const DecodeArgs& a, hipStream_t stream) {
-  MOE_LAUNCH("attn_decode", attn_decode_kernel<D>, dim3(a.B, a.kv_heads, (a.group + kCols - 1) / kCols),
-             dim3(64 * kWaves), 0, stream, a);
+__global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
+  constexpr int kLanes = D / 4, kAtOnce = 256 / kLanes;
+  __shared__ __attribute__((aligned(16))) float lds_o[kAtOnce][D];
+  __shared__ float lds_l[kAtOnce];
+  const int64_t r = blockIdx.x;
+  const int slots = a.prefix_parts + a.own_parts;
+  const int b = (int)(r / (a.kv_heads * a.group));
+  const int64_t len = min((int64_t)max(a.lens[b], 0), (int64_t)a.width << a.page_shift);
+  // parts that ran: all of the prefix's, and those of the sequence that begin before its end (the first always)
+  const int used = a.prefix_parts +
+                   (int)min((int64_t)a.own_parts, max((int64_t)1, (len + a.part_keys - 1) / a.part_keys));
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + r * slots;
+  float m = kNoScore;
+  for (int s = threadIdx.x & 63; s < used; s += 64) m = fmaxf(m, ml[s].x);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+  const int sub = threadIdx.x % kLanes, first = threadIdx.x / kLanes;
+  v4f o = {};
+  float l = 0.0f;
+#pragma unroll 4
+  for (int s = first; s < used; s += kAtOnce) {
+    const float2 x = ml[s];
+    const float f = __builtin_amdgcn_exp2f(x.x - m);
+    l += x.y * f;
+    o += *reinterpret_cast<const v4f*>(a.part_o + (r * slots + s) * D + 4 * sub) * f;
+  }
+  *reinterpret_cast<v4f*>(&lds_o[first][4 * sub]) = o;
+  if (sub == 0) lds_l[first] = l;
+  __syncthreads();
+  if (first > 0) return;
+#pragma unroll
+  for (int w = 1; w < kAtOnce; ++w) {
+    o += *reinterpret_cast<const v4f*>(&lds_o[w][4 * sub]);
+    l += lds_l[w];
+  }
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  *reinterpret_cast<uint2*>(a.out + r * D + 4 * sub) =
+      make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+}
+
+struct DecodePlan {
+  int part_keys, prefix_parts, own_parts, prefix_blocks, own_blocks, col_blocks;
+  int64_t slots_of_rows;  // B * q_heads * slots where there is more than one slot
+};
+
+DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int32_t prefix_len) {
+  DecodePlan p{};
+  const int group = d.q_heads / d.kv_heads;
+  p.col_blocks = group > 16 || (prefix_len > 0 && (int64_t)B * group > 16) ? 2 : 1;
+  p.own_blocks = (group + 16 * p.col_blocks - 1) / (16 * p.col_blocks);
+  p.prefix_blocks = (int)(((int64_t)B * group + 16 * p.col_blocks - 1) / (16 * p.col_blocks));
+  const int64_t keys = ((int64_t)B * p.own_blocks * max_len + (int64_t)p.prefix_blocks * prefix_len) * d.kv_heads;
+  const int64_t even = (keys + 767) / 768;
+  p.part_keys = (int)std::min<int64_t>(1024, std::max<int64_t>(256, (even + kStride - 1) / kStride * kStride));
+  p.own_parts = std::max(1, (int)(((int64_t)max_len + p.part_keys - 1) / p.part_keys));
+  p.prefix_parts = (int)(((int64_t)prefix_len + p.part_keys - 1) / p.part_keys);
+  const int slots = p.own_parts + p.prefix_parts;
+  p.slots_of_rows = slots > 1 ? (int64_t)B * d.q_heads * slots : 0;
+  return p;
+}
+
+size_t part_bytes(const DecodePlan& p, int width) {
+  return ((size_t)p.slots_of_rows * width * sizeof(float) + 255) & ~(size_t)255;
+}
+
+template <int D>
+moe_status_t launch_decode(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream) {
+  const int64_t items = ((int64_t)p.prefix_parts * p.prefix_blocks + (int64_t)p.own_parts * p.own_blocks * a.B) * a.kv_heads;
+  const int64_t rows = (int64_t)a.B * a.kv_heads * a.group;
+  if (items * 64 * kWaves >= (int64_t)1 << 32 || rows * 256 >= (int64_t)1 << 32)
+    return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_decode: %lld parts", (long long)items);
+  if (p.col_blocks == 1)
+    MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, 1>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
+  else
+    MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, 2>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
+  if (p.slots_of_rows)
+    MOE_LAUNCH("attn_join", attn_join_kernel<D>, dim3((unsigned)rows), dim3(256), 0, stream, a);
   return check_launch("moe_attn_decode");
 }
 
@@ -219,11 +467,10 @@ moe_status_t launch_decode(const DecodeArgs& a, hipStream_t stream) {
 using namespace moe;
 
 extern "C" size_t moe_attn_decode_workspace(moe_attn_dims_t d, int32_t B, int32_t max_len, int32_t prefix_len) {
-  (void)d;
-  (void)B;
-  (void)max_len;
-  (void)prefix_len;
-  return 0;
+  if (check_attn_dims(d, "moe_attn_decode_workspace") != MOE_OK || B < 1 || B > 65535 || max_len < 0 || prefix_len < 0)
+    return 0;
+  const DecodePlan p = plan_decode(d, B, max_len, prefix_len);
+  return part_bytes(p, d.head_dim) + part_bytes(p, 2);
 }
 
 extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint16_t* q, int64_t q_stride,
@@ -246,7 +493,12 @@ extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint
   const size_t need = moe_attn_decode_workspace(d, B, max_len, prefix_len);
   if (need && (!ws || ws_bytes < need || !aligned(ws, 256)))
     return fail(MOE_ERR_WORKSPACE, "moe_attn_decode: workspace %zu bytes, needs %zu, 256-byte aligned", ws_bytes, need);
-  const DecodeArgs a{q, q_stride, cache, page_table, lens, prefix_pages, out, dev_status, B, table_width, prefix_len,
-                     d.kv_heads, d.q_heads / d.kv_heads, __builtin_ctz((unsigned)cache.page_size), scale * kLog2e};
-  return d.head_dim == 64 ? launch_decode<64>(a, stream) : launch_decode<128>(a, stream);
+  const DecodePlan p = plan_decode(d, B, max_len, prefix_len);
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  float* part_o = p.slots_of_rows ? reinterpret_cast<float*>(base) : nullptr;
+  float* part_ml = p.slots_of_rows ? reinterpret_cast<float*>(base + part_bytes(p, d.head_dim)) : nullptr;
+  const DecodeArgs a{q, q_stride, cache, page_table, lens, prefix_pages, out, part_o, part_ml, dev_status, B, table_width,
+                     prefix_len, d.kv_heads, d.q_heads / d.kv_heads, __builtin_ctz((unsigned)cache.page_size),
+                     p.part_keys, p.prefix_parts, p.own_parts, p.prefix_blocks, p.own_blocks, scale * kLog2e};
+  return d.head_dim == 64 ? launch_decode<64>(a, p, stream) : launch_decode<128>(a, p, stream);
 }
