@@ -75,6 +75,15 @@ struct Running {
   float vref;
 };
 
+// The maximum over the four lanes that hold one query (lane, lane ^ 16, ^ 32,
+// ^ 48), by register swaps between rows of 16 and of 32 lanes.
+__device__ __forceinline__ float quad_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // 32 keys and values on their way.
 template <int D>
 struct Tile {
@@ -142,9 +151,11 @@ __device__ __forceinline__ void load_tile(const DecodeArgs& a, const Part& p, in
   }
 }
 
-template <int D, int NC>
+// The step at t0, whose keys and values are in x; once they are taken from there,
+// `next` loads those of the next step.
+template <int D, int NC, typename Next>
 __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int t0, const Tile<D>& x,
-                                         const v8bf (&qf)[NC][D / 32], uint8_t* lds_v, Running<D, NC>& run) {
+                                         const v8bf (&qf)[NC][D / 32], uint8_t* lds_v, Running<D, NC>& run, Next next) {
   constexpr int kChunks = D / 16;
   const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
 #pragma unroll
@@ -180,8 +191,8 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
       vtop = fmaxf(vtop, vs[u][i]);
     }
   }
-  vtop = fmaxf(vtop, __shfl_xor(vtop, 16, 64));
-  vtop = fmaxf(vtop, __shfl_xor(vtop, 32, 64));
+  vtop = quad_max(vtop);
+  next();
   const float inv = 1.0f / vtop, faded = run.vref * inv;
   run.vref = vtop;
 #pragma unroll
@@ -204,9 +215,7 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
         s[n][u][i] = ks[u][i] >= 0.0f ? s[n][u][i] * ks[u][i] : -INFINITY;
         top = fmaxf(top, s[n][u][i]);
       }
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float m = fmaxf(run.m[n], top), alpha = __builtin_amdgcn_exp2f(run.m[n] - m);
+    const float m = fmaxf(run.m[n], quad_max(top)), alpha = __builtin_amdgcn_exp2f(run.m[n] - m);
     run.m[n] = m;
     float sum = 0.0f;
 #pragma unroll
@@ -245,7 +254,7 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
 // that share keys have numbers equal mod 8 (one XCD's L2) where kv_heads is a
 // multiple of 8.
 template <int D, int NC>
-__global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, NC == 1 ? 3 : 2) void attn_decode_kernel(DecodeArgs a) {
   constexpr int kCols = 16 * NC;
   __shared__ __attribute__((aligned(16))) uint8_t lds_v[kWaves][kKeys * D];
   __shared__ __attribute__((aligned(16))) float lds_o[kWaves][16][D + 4];
@@ -289,9 +298,9 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(DecodeArgs a) 
   p.end = last_part ? p.len : (int)min((int64_t)p.len, begin + a.part_keys);
 
   // column n of block col0: query head (col % G) of the group, of sequence col / G in the prefix
-  const auto row_of = [&](int col) {  // row of q and out, counted in heads
-    const int s = shared ? (col0 + col) / a.group : b;
-    return (int64_t)s * (a.kv_heads * a.group) + p.kvh * a.group + (shared ? (col0 + col) % a.group : col0 + col);
+  const auto split = [&](int col, int& seq, int& head) {
+    seq = shared ? (col0 + col) / a.group : b;
+    head = p.kvh * a.group + (shared ? col0 + col - seq * a.group : col0 + col);
   };
   Running<D, NC> run;
   run.vref = 0x1p-126f;  // 1 / vref stays finite
@@ -307,9 +316,9 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(DecodeArgs a) 
     v8bf qf[NC][D / 32];
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-      const int64_t r = row_of(min(16 * n + c16, cols - 1));
-      const int64_t heads = a.kv_heads * a.group;
-      const uint16_t* qrow = a.q + r / heads * a.q_stride + r % heads * D + 16 * g;
+      int seq, head;
+      split(min(16 * n + c16, cols - 1), seq, head);
+      const uint16_t* qrow = a.q + seq * a.q_stride + head * D + 16 * g;
 #pragma unroll
       for (int i = 0; i < D / 64; ++i) {
         qf[n][2 * i] = *reinterpret_cast<const v8bf*>(qrow + 64 * i);
@@ -317,20 +326,15 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(DecodeArgs a) 
       }
     }
     bool bad = false;
-    Tile<D> x, y;
+    Tile<D> x;
     load_tile<D>(a, p, t, pages_of(a, p, t), bad, x);
     Pages ahead = pages_of(a, p, t + kStride);
-    while (true) {
-      const bool more = t + kStride < p.end;
-      if (more) {
-        load_tile<D>(a, p, t + kStride, ahead, bad, y);
+    for (; t < p.end; t += kStride)
+      use_tile<D, NC>(a, p, t, x, qf, lds_v[wave], run, [&] {
+        if (t + kStride >= p.end) return;
+        load_tile<D>(a, p, t + kStride, ahead, bad, x);
         ahead = pages_of(a, p, t + 2 * kStride);
-      }
-      use_tile<D, NC>(a, p, t, x, qf, lds_v[wave], run);
-      if (!more) break;
-      t += kStride;
-      x = y;
-    }
+      });
     if (bad && a.status && lane == 0) atomicOr(a.status, MOE_DEV_BAD_PAGE);
   }
 
@@ -363,7 +367,9 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(DecodeArgs a) 
         sum += lds_l[w][16 * n + col] * f;
         o += *reinterpret_cast<const v4f*>(&lds_o[w][col][d]) * f;
       }
-      const int64_t r = row_of(16 * n + col);
+      int seq, head;
+      split(16 * n + col, seq, head);
+      const int64_t r = (int64_t)seq * (a.kv_heads * a.group) + head;
       if (whole) {
         const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
         *reinterpret_cast<uint2*>(a.out + r * D + d) =
@@ -432,7 +438,7 @@ DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int
   p.own_blocks = (group + 16 * p.col_blocks - 1) / (16 * p.col_blocks);
   p.prefix_blocks = (int)(((int64_t)B * group + 16 * p.col_blocks - 1) / (16 * p.col_blocks));
   const int64_t keys = ((int64_t)B * p.own_blocks * max_len + (int64_t)p.prefix_blocks * prefix_len) * d.kv_heads;
-  const int64_t even = (keys + 767) / 768;
+  const int64_t even = (keys + 511) / 512;
   p.part_keys = (int)std::min<int64_t>(1024, std::max<int64_t>(256, (even + kStride - 1) / kStride * kStride));
   p.own_parts = std::max(1, (int)(((int64_t)max_len + p.part_keys - 1) / p.part_keys));
   p.prefix_parts = (int)(((int64_t)prefix_len + p.part_keys - 1) / p.part_keys);

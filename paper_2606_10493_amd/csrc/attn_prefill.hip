@@ -82,11 +82,35 @@ __device__ __forceinline__ int staged(int row, int c) {
   return row * (D * 2) + ((c ^ f) * 16);
 }
 
+constexpr int kStages = 3;  // tiles of keys and values in LDS
+
+// The maximum over a lane and lane ^ 32, by a register swap between the half-waves.
+__device__ __forceinline__ float pair_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// One wave's part of staging keys or values t0 .. t0 + 63: 1 KB a call, straight
+// into LDS, in the order that `staged` gives (a lane fetches the chunk that
+// belongs at its place).  Rows behind the sequence's end repeat its last:
+// finite, weighed by 0.
 template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void attn_prefill_kernel(PrefillArgs a) {
-  constexpr int kChunks = D / 8;  // 16-byte chunks of a row
-  constexpr int kTileRows = kWaveRows * WAVES;
-  __shared__ __attribute__((aligned(16))) uint8_t lds_k[kKeys * D * 2], lds_v[kKeys * D * 2];
+__device__ __forceinline__ void stage(const uint16_t* base, int64_t stride, int t0, int last, uint32_t lds) {
+  constexpr int kCalls = kKeys * D * 2 / 1024 / WAVES, kRows = 1024 / (D * 2);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < kCalls; ++i) {
+    const int call = wave * kCalls + i;
+    const int row = call * kRows + lane / (D / 8);
+    const int c = (staged<D>(row, lane % (D / 8)) % (D * 2)) / 16;
+    async_load_1k(base + (int64_t)min(t0 + row, last) * stride + 8 * c, lds + 1024 * call);
+  }
+}
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs a) {
+  constexpr int kTileRows = kWaveRows * WAVES, kTileBytes = kKeys * D * 2;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages][2][kTileBytes];
 
   int b, local, n_tiles;
   if (!find_tile(a, kTileRows, blockIdx.x, b, local, n_tiles)) return;
@@ -106,102 +130,121 @@ __global__ __launch_bounds__(64 * WAVES) void attn_prefill_kernel(PrefillArgs a)
   const bool live = r < n_rows;
   const int64_t rc = live ? r : n_rows - 1;
   const int tok = (int)(rc / a.group), head = kvh * a.group + (int)(rc - (int64_t)tok * a.group);
-  // the last key that this row sees, and that the tile's last row sees
-  const int limit = a.causal ? tok + lk - lq : lk - 1;
+  // the last key that this row sees, that the tile's first row sees and that its last row sees
+  const int limit = min(a.causal ? tok + lk - lq : lk - 1, lk - 1);
+  const int first_limit = min(a.causal ? (int)(row0 / a.group) + lk - lq : lk - 1, lk - 1);
   const int tile_last = a.causal ? (int)((min(row0 + kTileRows, n_rows) - 1) / a.group) + lk - lq : lk - 1;
-  const int first_limit = a.causal ? (int)(row0 / a.group) + lk - lq : lk - 1;
   const int n_key_tiles = tile_last < 0 ? 0 : tile_last / kKeys + 1;
-
-  v8bf qf[D / 16];
-  const uint16_t* qrow = a.q + (q0 + (int64_t)tok) * a.q_stride + head * D + 8 * h;
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const v8bf*>(qrow + 16 * i);
 
   v16f o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = v16f{};
   float m = kNoScore, l = 0.0f;
 
-  const uint16_t* kbase = a.k + (int64_t)k0 * a.k_stride + kvh * D;
-  const uint16_t* vbase = a.v + (int64_t)k0 * a.v_stride + kvh * D;
-  for (int kt = 0; kt < n_key_tiles; ++kt) {
-    const int t0 = kt * kKeys;
-    __syncthreads();
-    // rows behind the sequence's end repeat its last: finite, weighed by 0
+  if (n_key_tiles > 0) {
+    v8bf qf[D / 16];
+    const uint16_t* qrow = a.q + (q0 + (int64_t)tok) * a.q_stride + head * D + 8 * h;
 #pragma unroll
-    for (int i = 0; i < kKeys * kChunks / (64 * WAVES); ++i) {
-      const int p = i * 64 * WAVES + (int)threadIdx.x, row = p / kChunks, c = p % kChunks;
-      const int64_t t = min(t0 + row, lk - 1);
-      *reinterpret_cast<uint4*>(lds_k + staged<D>(row, c)) = *reinterpret_cast<const uint4*>(kbase + t * a.k_stride + 8 * c);
-      *reinterpret_cast<uint4*>(lds_v + staged<D>(row, c)) = *reinterpret_cast<const uint4*>(vbase + t * a.v_stride + 8 * c);
-    }
-    __syncthreads();
+    for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const v8bf*>(qrow + 16 * i);
 
-    v16f s[2];
+    const uint16_t* kbase = a.k + (int64_t)k0 * a.k_stride + kvh * D;
+    const uint16_t* vbase = a.v + (int64_t)k0 * a.v_stride + kvh * D;
+    const uint32_t lds0 = lds_address(lds);
+    const auto fetch = [&](int kt, int st) {
+      stage<D, WAVES>(kbase, a.k_stride, kt * kKeys, lk - 1, lds0 + (2 * st) * kTileBytes);
+      stage<D, WAVES>(vbase, a.v_stride, kt * kKeys, lk - 1, lds0 + (2 * st + 1) * kTileBytes);
+    };
+    const auto scores = [&](const uint8_t* lds_k, v16f (&s)[2]) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      s[u] = v16f{};
+      for (int u = 0; u < 2; ++u) {
+        s[u] = v16f{};
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        const v8bf kf = *reinterpret_cast<const v8bf*>(lds_k + staged<D>(32 * u + col, 2 * i + h));
-        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[u], 0, 0, 0);
+        for (int i = 0; i < D / 16; ++i) {
+          const v8bf kf = *reinterpret_cast<const v8bf*>(lds_k + staged<D>(32 * u + col, 2 * i + h));
+          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[u], 0, 0, 0);
+        }
       }
-    }
-    if (t0 + kKeys - 1 > min(first_limit, lk - 1)) {
+    };
+
+    fetch(0, 0);
+    wait_async_and_barrier<0>();
+    if (n_key_tiles > 1) fetch(1, 1);
+    v16f s[2], s_next[2];
+    scores(lds[0][0], s);
+    int st = 0;
+    for (int kt = 0; kt < n_key_tiles; ++kt) {
+      const int st1 = st == kStages - 1 ? 0 : st + 1, st2 = st1 == kStages - 1 ? 0 : st1 + 1;
+      // tile kt + 1 is here, and every wave is done with tile kt - 1, whose place tile kt + 2 takes
+      wait_async_and_barrier<0>();
+      if (kt + 2 < n_key_tiles) fetch(kt + 2, st2);
+      // the next tile's scores: matrix work beside this tile's softmax.  Behind the last tile they are not used.
+      scores(lds[st1][0], s_next);
+
+      const int t0 = kt * kKeys;
+      if (t0 + kKeys - 1 > first_limit) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (t0 + 32 * u + 8 * (i / 4) + 4 * h + (i & 3) > limit) s[u][i] = -INFINITY;
+      }
+      float top = s[0][0];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (t0 + 32 * u + 8 * (i / 4) + 4 * h + (i & 3) > min(limit, lk - 1)) s[u][i] = -INFINITY;
-    }
-    float top = s[0][0];
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+      top = pair_max(top) * a.c;
+      // The accumulator is rescaled only when some row's maximum has grown by more than 2^8: numerators up to 2^8 are
+      // as exact, and most tiles of a long row go without.
+      if (__any(top > m + 8.0f)) {
+        const float m_new = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= alpha;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float m_new = fmaxf(m, top * a.c);
-    const float alpha = __builtin_amdgcn_exp2f(m - m_new);
-    m = m_new;
-    float sum = 0.0f;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.c, -m));
-        sum += s[u][i];
+        for (int i = 0; i < D / 32; ++i) o[i] *= alpha;
       }
-    l = l * alpha + sum;
+      float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] *= alpha;
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.c, -m));
+          sum += s[u][i];
+        }
+      l += sum;
 
+      const uint8_t* lds_v = lds[st][1];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        union {
-          v8bf v;
-          uint32_t x[4];
-        } p;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p.x[i] = pack_bf16(s[u][8 * w + 2 * i], s[u][8 * w + 2 * i + 1]);
-        // lane j of a 16-lane group gives the address of row j / 4, 8-byte piece j % 4 of a 4 x 16 block and
-        // gets column j of it
-        const int row = 32 * u + 16 * w + 4 * h + ((lane & 15) >> 2);
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) {
-          const int c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), piece = 8 * (lane & 1);
+        for (int w = 0; w < 2; ++w) {
           union {
             v8bf v;
-            v4s x[2];
-          } vf;
-          vf.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) v4s*)(lds_v + staged<D>(row, c) + piece));
-          vf.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) v4s*)(lds_v + staged<D>(row + 8, c) + piece));
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, p.v, o[dt], 0, 0, 0);
+            uint32_t x[4];
+          } p;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p.x[i] = pack_bf16(s[u][8 * w + 2 * i], s[u][8 * w + 2 * i + 1]);
+          // lane j of a 16-lane group gives the address of row j / 4, 8-byte piece j % 4 of a 4 x 16 block and
+          // gets column j of it
+          const int row = 32 * u + 16 * w + 4 * h + ((lane & 15) >> 2);
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt) {
+            const int c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), piece = 8 * (lane & 1);
+            union {
+              v8bf v;
+              v4s x[2];
+            } vf;
+            vf.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) v4s*)(lds_v + staged<D>(row, c) + piece));
+            vf.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) v4s*)(lds_v + staged<D>(row + 8, c) + piece));
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, p.v, o[dt], 0, 0, 0);
+          }
         }
-      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) s[u] = s_next[u];
+      st = st1;
+    }
   }
 
   l += __shfl_xor(l, 32, 64);
@@ -219,7 +262,7 @@ __global__ __launch_bounds__(64 * WAVES) void attn_prefill_kernel(PrefillArgs a)
 
 template <int D>
 moe_status_t launch_prefill(const PrefillArgs& a, hipStream_t stream) {
-  constexpr int kWaves = 4;
+  constexpr int kWaves = 8;
   const int64_t tiles = (int64_t)a.T_q * a.group / (kWaves * kWaveRows) + a.B;  // sequences may each add a part of one
   if (tiles * kWaves * 64 >= (int64_t)1 << 32)
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_prefill: %lld row tiles", (long long)tiles);
