@@ -451,8 +451,8 @@ moe_status_t moe_stream_schedule(moe_dims_t dims, int32_t T, int32_t chunk_token
  * q_heads query heads read kv_heads key/value heads: head h reads key/value
  * head h / (q_heads / kv_heads).  Activations are bf16 rows [tokens, heads,
  * head_dim]; the heads of a token are contiguous, consecutive tokens lie
- * *_stride elements apart (a multiple of 8, at least heads * head_dim), so q,
- * k and v may be views of one packed projection.  Activation pointers are
+ * *_stride elements apart (a multiple of 8, at least heads * head_dim, below
+ * 2^23), so q, k and v may be views of one packed projection.  Activation pointers are
  * 16-byte aligned.  Requires head_dim 64 or 128, 1 <= kv_heads <= q_heads <=
  * 1024, q_heads % kv_heads == 0; else MOE_ERR_UNSUPPORTED_SHAPE.
  * ---------------------------------------------------------------------------

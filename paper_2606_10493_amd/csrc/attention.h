@@ -47,12 +47,13 @@ inline moe_status_t check_attn_dims(const moe_attn_dims_t& d, const char* who) {
   return MOE_OK;
 }
 
+constexpr int64_t kMaxStride = (int64_t)1 << 23;
 inline moe_status_t check_rows(const void* p, int64_t stride, int32_t heads, int32_t dim, const char* who,
                                const char* name) {
   if (!p) return fail(MOE_ERR_INVALID_ARG, "%s: %s is NULL", who, name);
   if (!aligned(p, 16)) return fail(MOE_ERR_INVALID_ARG, "%s: %s must be 16-byte aligned", who, name);
-  if (stride < (int64_t)heads * dim || stride % 8 || stride > ((int64_t)1 << 31))
-    return fail(MOE_ERR_INVALID_ARG, "%s: stride %lld of %s must be a multiple of 8, %lld to 2^31", who, (long long)stride,
+  if (stride < (int64_t)heads * dim || stride % 8 || stride >= kMaxStride)
+    return fail(MOE_ERR_INVALID_ARG, "%s: stride %lld of %s must be a multiple of 8, from %lld to below 2^23", who, (long long)stride,
                 name, (long long)heads * dim);
   return MOE_OK;
 }

@@ -16,6 +16,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attention.h"
 
@@ -34,6 +35,7 @@ struct PrefillArgs {
 };
 
 constexpr int kKeys = 64;  // keys per tile
+constexpr int kRing = 4;   // tiles of keys, and of values, in LDS
 constexpr int kWaveRows = 32;
 
 // Sequence b's rows of a packed tensor, cut to the tensor.
@@ -82,7 +84,6 @@ __device__ __forceinline__ int staged(int row, int c) {
   return row * (D * 2) + ((c ^ f) * 16);
 }
 
-constexpr int kStages = 3;  // tiles of keys and values in LDS
 
 // The maximum over a lane and lane ^ 32, by a register swap between the half-waves.
 __device__ __forceinline__ float pair_max(float x) {
@@ -95,35 +96,46 @@ __device__ __forceinline__ float pair_max(float x) {
 // belongs at its place).  Rows behind the sequence's end repeat its last:
 // finite, weighed by 0.
 template <int D, int WAVES>
-__device__ __forceinline__ void stage(const uint16_t* base, int64_t stride, int t0, int last, uint32_t lds) {
+__device__ __forceinline__ void stage(const uint16_t* base, int64_t stride, int t0, int last, int wave, uint32_t lds) {
   constexpr int kCalls = kKeys * D * 2 / 1024 / WAVES, kRows = 1024 / (D * 2);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  t0 = min(t0, last);
+  const uint16_t* tile = base + t0 * stride;
 #pragma unroll
   for (int i = 0; i < kCalls; ++i) {
     const int call = wave * kCalls + i;
     const int row = call * kRows + lane / (D / 8);
     const int c = (staged<D>(row, lane % (D / 8)) % (D * 2)) / 16;
-    async_load_1k(base + (int64_t)min(t0 + row, last) * stride + 8 * c, lds + 1024 * call);
+    // a row's offset in its tile has 30 bits: strides have 24 in bytes
+    async_load_1k_at(tile, __umul24(min(row, last - t0), (uint32_t)(stride * 2)) + 16 * c, lds + 1024 * call);
   }
 }
 
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs a) {
   constexpr int kTileRows = kWaveRows * WAVES, kTileBytes = kKeys * D * 2;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages][2][kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRing][kTileBytes];  // keys, values
 
   int b, local, n_tiles;
-  if (!find_tile(a, kTileRows, blockIdx.x, b, local, n_tiles)) return;
-  local = n_tiles - 1 - local;  // a sequence's longest rows first
+  const int kvh = blockIdx.x % a.kv_heads;
+  if (!find_tile(a, kTileRows, blockIdx.x / a.kv_heads, b, local, n_tiles)) return;
+  // the same for the whole workgroup, and kept in scalar registers
+  b = __builtin_amdgcn_readfirstlane(b);
+  local = __builtin_amdgcn_readfirstlane(n_tiles - 1 - local);  // a sequence's longest rows first
   int q0, lq, k0, lk;
   sequence_rows(a.cu_q, b, a.T_q, q0, lq);
   sequence_rows(a.cu_k, b, a.T_k, k0, lk);
-  if (a.status && blockIdx.y == 0 && threadIdx.x == 0 &&
+  if (a.status && kvh == 0 && threadIdx.x == 0 &&
       (q0 != a.cu_q[b] || q0 + lq != a.cu_q[b + 1] || k0 != a.cu_k[b] || k0 + lk != a.cu_k[b + 1]))
     atomicOr(a.status, MOE_DEV_BAD_LENGTH);
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, h = lane >> 5;
-  const int kvh = blockIdx.y;
+  q0 = __builtin_amdgcn_readfirstlane(q0);
+  lq = __builtin_amdgcn_readfirstlane(lq);
+  k0 = __builtin_amdgcn_readfirstlane(k0);
+  lk = __builtin_amdgcn_readfirstlane(lk);
+
+  const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t n_rows = (int64_t)lq * a.group;
   const int64_t row0 = (int64_t)local * kTileRows;
   const int64_t r = row0 + wave * kWaveRows + col;
@@ -150,43 +162,52 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     const uint16_t* kbase = a.k + (int64_t)k0 * a.k_stride + kvh * D;
     const uint16_t* vbase = a.v + (int64_t)k0 * a.v_stride + kvh * D;
     const uint32_t lds0 = lds_address(lds);
-    const auto fetch = [&](int kt, int st) {
-      stage<D, WAVES>(kbase, a.k_stride, kt * kKeys, lk - 1, lds0 + (2 * st) * kTileBytes);
-      stage<D, WAVES>(vbase, a.v_stride, kt * kKeys, lk - 1, lds0 + (2 * st + 1) * kTileBytes);
+    const auto fetch_k = [&](int kt) __attribute__((always_inline)) {
+      stage<D, WAVES>(kbase, a.k_stride, kt * kKeys, lk - 1, wave, lds0 + kt % kRing * kTileBytes);
     };
-    const auto scores = [&](const uint8_t* lds_k, v16f (&s)[2]) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        s[u] = v16f{};
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const v8bf kf = *reinterpret_cast<const v8bf*>(lds_k + staged<D>(32 * u + col, 2 * i + h));
-          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[u], 0, 0, 0);
-        }
+    const auto fetch_v = [&](int kt) __attribute__((always_inline)) {
+      stage<D, WAVES>(vbase, a.v_stride, kt * kKeys, lk - 1, wave, lds0 + (kRing + kt % kRing) * kTileBytes);
+    };
+    constexpr int kCalls = 2 * (kTileBytes / 1024 / WAVES);  // of a wave for one tile's keys and values
+
+    v16f s[2];  // scores of a tile
+    union {
+      v8bf v[4];
+      uint32_t x[16];
+    } p;  // its numerators
+
+    // Operand f of a step: the next tile's keys (the first D / 8, the two blocks of 32 keys in turn), then this tile's
+    // values.  The swizzle makes an operand's place the first one's with some bits flipped, plus a constant.
+    constexpr int kK = D / 8, kAhead = 6;
+    const int k_place = lds0 + staged<D>(col, h);
+    // lane j of a 16-lane group gives the address of row j / 4, 8-byte piece j % 4 of a 4 x 16 block and gets column j
+    const int v_place = lds0 + kRing * kTileBytes +
+                        staged<D>(4 * h + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+    const auto operand = [&](int kp, int vp, int f) __attribute__((always_inline)) {
+      union {
+        v8bf v;
+        v4s x[2];
+      } r;
+      if (f < kK) {
+        r.v = *(__attribute__((address_space(3))) const v8bf*)(uintptr_t)((kp ^ (32 * (f >> 1))) + (f & 1) * 32 * (D * 2));
+        return r.v;
       }
+      const int w = (f - kK) / (D / 32), dt = (f - kK) % (D / 32);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        r.x[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(
+            (vp ^ (64 * dt + 32 * x)) + (16 * w + 8 * x) * (D * 2)));
+      return r.v;
     };
-
-    fetch(0, 0);
-    wait_async_and_barrier<0>();
-    if (n_key_tiles > 1) fetch(1, 1);
-    v16f s[2], s_next[2];
-    scores(lds[0][0], s);
-    int st = 0;
-    for (int kt = 0; kt < n_key_tiles; ++kt) {
-      const int st1 = st == kStages - 1 ? 0 : st + 1, st2 = st1 == kStages - 1 ? 0 : st1 + 1;
-      // tile kt + 1 is here, and every wave is done with tile kt - 1, whose place tile kt + 2 takes
-      wait_async_and_barrier<0>();
-      if (kt + 2 < n_key_tiles) fetch(kt + 2, st2);
-      // the next tile's scores: matrix work beside this tile's softmax.  Behind the last tile they are not used.
-      scores(lds[st1][0], s_next);
-
-      const int t0 = kt * kKeys;
-      if (t0 + kKeys - 1 > first_limit) {
+    // The vector phase of tile kt: its scores become numerators; maximum, sum and accumulator follow.  A tile behind
+    // the row's last key changes nothing (masked).
+    const auto weigh = [&](auto masked, int kt) __attribute__((always_inline)) {
+      if (decltype(masked)::value) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (t0 + 32 * u + 8 * (i / 4) + 4 * h + (i & 3) > limit) s[u][i] = -INFINITY;
+            if (kt * kKeys + 32 * u + 8 * (i / 4) + 4 * h + (i & 3) > limit) s[u][i] = -INFINITY;
       }
       float top = s[0][0];
 #pragma unroll
@@ -203,48 +224,86 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) o[i] *= alpha;
       }
-      float sum = 0.0f;
+      float sum[2] = {};
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.c, -m));
-          sum += s[u][i];
+        for (int i = 0; i < 16; i += 2) {
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.c, -m));
+          const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i + 1], a.c, -m));
+          sum[0] += x;
+          sum[1] += y;
+          p.x[8 * u + i / 2] = pack_bf16(x, y);
         }
-      l += sum;
+      l += sum[0] + sum[1];
+    };
+    // A step is a vector phase (`weigh`) and a matrix phase: the next tile's scores, then this tile's numerators times
+    // its values, with the operands read from LDS kAhead products early, the first ones before the phase begins.
+    //
+    // The two waves of a SIMD run a phase apart, so that one has matrix work while the other has vector work: the
+    // late half of the waves starts with one barrier more.  In phase 2 t the early half multiplies tile t and the late
+    // half weighs it; in phase 2 t + 1 the early half weighs tile t + 1 and the late half multiplies tile t.
+    //
+    // Ring: keys t and values t - 1 are last read in phase 2 t - 1 (by the late half's matrix phase of tile t - 1).  Keys
+    // t + kRing and values t + kRing - 1 take their places, fetched in phase 2 t by the late half and in phase 2 t + 1 by
+    // the early one, at the start of their vector phases.  They are first read at the end of phase 2 (t + kRing) - 3.
+    // Every vector phase ends by waiting for all fetches but its own, so a fetch has two phases or more to
+    // arrive, and the barrier after that wait comes before the first read.  (Behind the end the last row is fetched;
+    // the scores of the tile behind the last are not used.)
+    const bool late = wave >= WAVES / 2;
+    const auto step = [&](auto masked, int kt) __attribute__((always_inline)) {
+      const int ft = late ? kt : kt - 1;
+      fetch_k(ft + kRing);
+      fetch_v(ft + kRing - 1);
+      weigh(masked, kt);
+      // opaque: the operands' places are computed in every step, which costs less than the registers to keep them
+      int kp = k_place + (kt + 1) % kRing * kTileBytes, vp = v_place + kt % kRing * kTileBytes;
+      asm volatile("" : "+v"(kp), "+v"(vp));
+      v8bf ops[kAhead + 1];
+#pragma unroll
+      for (int f = 0; f < kAhead; ++f) ops[f] = operand(kp, vp, f);
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kCalls) : "memory");
+      __builtin_amdgcn_s_setprio(1);
+      __builtin_amdgcn_sched_barrier(0);
+      s[0] = s[1] = v16f{};
+#pragma unroll
+      for (int f = 0; f < 2 * kK; ++f) {
+        if (f + kAhead < 2 * kK) ops[(f + kAhead) % (kAhead + 1)] = operand(kp, vp, f + kAhead);
+        const v8bf x = ops[f % (kAhead + 1)];
+        const int g = f - kK;
+        if (f < kK)
+          s[f & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[f >> 1], s[f & 1], 0, 0, 0);
+        else
+          o[g % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p.v[g / (D / 32)], o[g % (D / 32)], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_setprio(0);
+      asm volatile("s_barrier" : : : "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
 
-      const uint8_t* lds_v = lds[st][1];
+    fetch_k(0);
+    fetch_k(1);
+    fetch_v(0);
+    fetch_k(2);
+    fetch_v(1);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kCalls) : "memory");
+    s[0] = s[1] = v16f{};
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          union {
-            v8bf v;
-            uint32_t x[4];
-          } p;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p.x[i] = pack_bf16(s[u][8 * w + 2 * i], s[u][8 * w + 2 * i + 1]);
-          // lane j of a 16-lane group gives the address of row j / 4, 8-byte piece j % 4 of a 4 x 16 block and
-          // gets column j of it
-          const int row = 32 * u + 16 * w + 4 * h + ((lane & 15) >> 2);
-#pragma unroll
-          for (int dt = 0; dt < D / 32; ++dt) {
-            const int c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), piece = 8 * (lane & 1);
-            union {
-              v8bf v;
-              v4s x[2];
-            } vf;
-            vf.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) v4s*)(lds_v + staged<D>(row, c) + piece));
-            vf.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) v4s*)(lds_v + staged<D>(row + 8, c) + piece));
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, p.v, o[dt], 0, 0, 0);
-          }
-        }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) s[u] = s_next[u];
-      st = st1;
+    for (int f = 0; f < kK; ++f)
+      s[f & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(k_place, v_place, f), qf[f >> 1], s[f & 1], 0, 0, 0);
+    if (late) {
+      fetch_k(kRing - 1);
+      fetch_v(kRing - 2);
+      asm volatile("s_barrier" : : : "memory");
     }
+    const int n_free = min((first_limit + 1) / kKeys, n_key_tiles);  // tiles without a masked key for any row
+    int kt = 0;
+    for (; kt < n_free; ++kt) step(std::false_type{}, kt);
+    for (; kt < n_key_tiles; ++kt) step(std::true_type{}, kt);
+    if (!late) asm volatile("s_barrier" : : : "memory");
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
   }
 
   l += __shfl_xor(l, 32, 64);
@@ -263,11 +322,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
 template <int D>
 moe_status_t launch_prefill(const PrefillArgs& a, hipStream_t stream) {
   constexpr int kWaves = 8;
-  const int64_t tiles = (int64_t)a.T_q * a.group / (kWaves * kWaveRows) + a.B;  // sequences may each add a part of one
-  if (tiles * kWaves * 64 >= (int64_t)1 << 32)
-    return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_prefill: %lld row tiles", (long long)tiles);
-  MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves>), dim3((unsigned)tiles, a.kv_heads), dim3(64 * kWaves), 0,
-             stream, a);
+  // Row tiles (sequences may each add a part of one), heads fastest: workgroups that share keys have numbers equal
+  // mod 8 (one XCD's L2) where kv_heads is a multiple of 8, and all heads' longest rows come first.
+  const int64_t items = ((int64_t)a.T_q * a.group / (kWaves * kWaveRows) + a.B) * a.kv_heads;
+  if (items * kWaves * 64 >= (int64_t)1 << 32)
+    return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_prefill: %lld row tiles", (long long)items);
+  MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
   return check_launch("moe_attn_prefill");
 }
 
