@@ -11,51 +11,49 @@ from __future__ import annotations
 
 import torch
 
+from . import _dev, _stream  # defined before the package imports this module
 from ._lib import MoeAttnDims, MoeKvCache, MoeRopeCfg, MOE_ROPE_HALF, MOE_ROPE_PLAIN, check as _check, lib
 
 
-def _stream(stream):
-    from . import _stream as current
-    return current(stream)
-
-
-def _dev(t, dtype_bytes, name):
-    from . import _dev as address
-    return address(t, dtype_bytes, name)
+_BF16 = (torch.bfloat16, torch.int16, torch.uint16)
 
 
 def _rows(t, heads, dim, name):
-    """Address and token stride of bf16 rows [tokens, heads, dim] whose heads are contiguous."""
+    """Address, token stride and tokens of bf16 rows [tokens, heads, dim] whose heads are contiguous."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if t.dtype not in _BF16:
         raise ValueError(f"{name} has type {t.dtype}, expected bf16 or its bits")
-    shape, stride = t.shape, t.stride()
+    shape = t.shape
     if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
         raise ValueError(f"{name} has shape {tuple(shape)}, expected [tokens, {heads}, {dim}]")
-    if shape[0] == 0:
-        return t.data_ptr(), heads * dim
-    if stride[2] != 1 or (stride[1] != dim and heads != 1):
+    n = shape[0]
+    if n == 0:
+        return t.data_ptr(), heads * dim, n
+    stride, head, one = t.stride()
+    if one != 1 or (head != dim and heads != 1):
         raise ValueError(f"{name}: a token's heads must be contiguous")
     # the stride of a single token is arbitrary
-    return t.data_ptr(), (stride[0] if shape[0] > 1 else heads * dim)
+    return t.data_ptr(), (stride if n > 1 else heads * dim), n
 
 
-def _same(t, n, name):
-    if t.shape[0] != n:
-        raise ValueError(f"{name} has {t.shape[0]} entries, expected {n}")
-
-
-_BF16 = (torch.bfloat16, torch.int16, torch.uint16)
+def _same(n, expected, name):
+    if n != expected:
+        raise ValueError(f"{name} has {n} entries, expected {expected}")
 
 
 def _out(t, tokens, heads, dim, name):
     p = _dev(t, 2, name)
     if t.dtype not in _BF16:
         raise ValueError(f"{name} has type {t.dtype}, expected bf16 or its bits")
-    if tuple(t.shape) != (tokens, heads, dim):
+    if t.shape != (tokens, heads, dim):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(tokens, heads, dim)}")
     return p
+
+
+def _ints(t, name):
+    """Address and entries of a contiguous int32 vector."""
+    return _dev(t, 4, name), t.numel()
 
 
 class KVCache:
@@ -99,42 +97,46 @@ def moe_rope_table(table, base: float = 10000.0, scaling: int = MOE_ROPE_PLAIN, 
 
 def moe_rope(dims: MoeAttnDims, q, k, positions, table, layout, q_out, k_out, dev_status=None, stream=None):
     """bf16 q [T, q_heads, head_dim] and k [T, kv_heads, head_dim] rotated into q_out and k_out (q or k None: left out)."""
-    T = positions.shape[0]
+    pos, T = _ints(positions, "positions")
+    hq, hkv, d = dims.q_heads, dims.kv_heads, dims.head_dim
     pq = sq = pk = sk = po = ko = 0
     if q is not None:
-        (pq, sq), po = _rows(q, dims.q_heads, dims.head_dim, "q"), _out(q_out, T, dims.q_heads, dims.head_dim, "q_out")
-        _same(q, T, "q")
+        (pq, sq, n), po = _rows(q, hq, d, "q"), _out(q_out, T, hq, d, "q_out")
+        _same(n, T, "q")
     if k is not None:
-        (pk, sk), ko = _rows(k, dims.kv_heads, dims.head_dim, "k"), _out(k_out, T, dims.kv_heads, dims.head_dim, "k_out")
-        _same(k, T, "k")
-    _check(lib.moe_rope(dims, T, pq, sq, pk, sk, _dev(positions, 4, "positions"), _dev(table, 4, "table"),
-                        table.shape[0], table.shape[1], layout, po, ko, _dev(dev_status, 4, "dev_status"),
-                        _stream(stream)))
+        (pk, sk, n), ko = _rows(k, hkv, d, "k"), _out(k_out, T, hkv, d, "k_out")
+        _same(n, T, "k")
+    n_pos, rot = table.shape
+    _check(lib.moe_rope(dims, T, pq, sq, pk, sk, pos, _dev(table, 4, "table"), n_pos, rot, layout, po, ko,
+                        _dev(dev_status, 4, "dev_status"), _stream(stream)))
 
 
 def moe_rope_cache(dims: MoeAttnDims, q, k, v, positions, table, layout, slots, cache: KVCache, q_out, k_out=None,
                    dev_status=None, stream=None):
     """moe_rope, and the rotated keys and the values quantized into the cache at each token's slot."""
-    T, hq, hkv, d = positions.shape[0], dims.q_heads, dims.kv_heads, dims.head_dim
-    (pq, sq), (pk, sk), (pv, sv) = _rows(q, hq, d, "q"), _rows(k, hkv, d, "k"), _rows(v, hkv, d, "v")
-    if not q.shape[0] == k.shape[0] == v.shape[0] == slots.shape[0] == T:
+    hq, hkv, d = dims.q_heads, dims.kv_heads, dims.head_dim
+    pos, T = _ints(positions, "positions")
+    slot, n = _ints(slots, "slots")
+    (pq, sq, nq), (pk, sk, nk), (pv, sv, nv) = _rows(q, hq, d, "q"), _rows(k, hkv, d, "k"), _rows(v, hkv, d, "v")
+    if not nq == nk == nv == n == T:
         raise ValueError("q, k, v, slots and positions must have one entry per token")
-    po = _out(q_out, T, hq, d, "q_out")
-    ko = 0 if k_out is None else _out(k_out, T, hkv, d, "k_out")
-    _check(lib.moe_rope_cache(dims, T, pq, sq, pk, sk, pv, sv, _dev(positions, 4, "positions"),
-                              _dev(table, 4, "table"), table.shape[0], table.shape[1], layout, _dev(slots, 4, "slots"),
-                              cache.check(dims), po, ko, _dev(dev_status, 4, "dev_status"), _stream(stream)))
+    n_pos, rot = table.shape
+    _check(lib.moe_rope_cache(dims, T, pq, sq, pk, sk, pv, sv, pos, _dev(table, 4, "table"), n_pos, rot, layout, slot,
+                              cache.check(dims), _out(q_out, T, hq, d, "q_out"),
+                              0 if k_out is None else _out(k_out, T, hkv, d, "k_out"),
+                              _dev(dev_status, 4, "dev_status"), _stream(stream)))
 
 
 def moe_cache_read(dims: MoeAttnDims, cache: KVCache, page_table, cu, k_out, v_out, dev_status=None, stream=None):
     """Sequences' first tokens (page_table int32 [B, width], cu int32 [B + 1]) as packed bf16 rows of k_out, v_out."""
     B, width = page_table.shape
-    _same(cu, B + 1, "cu")
+    offsets, n = _ints(cu, "cu")
+    _same(n, B + 1, "cu")
     T = k_out.shape[0]
-    pk = _out(k_out, T, dims.kv_heads, dims.head_dim, "k_out")
-    pv = _out(v_out, T, dims.kv_heads, dims.head_dim, "v_out")
-    _check(lib.moe_cache_read(dims, cache.check(dims), _dev(page_table, 4, "page_table"), B, width, _dev(cu, 4, "cu"), T,
-                              pk, pv, _dev(dev_status, 4, "dev_status"), _stream(stream)))
+    hkv, d = dims.kv_heads, dims.head_dim
+    _check(lib.moe_cache_read(dims, cache.check(dims), _dev(page_table, 4, "page_table"), B, width, offsets, T,
+                              _out(k_out, T, hkv, d, "k_out"), _out(v_out, T, hkv, d, "v_out"),
+                              _dev(dev_status, 4, "dev_status"), _stream(stream)))
 
 
 def moe_attn_prefill_workspace(dims: MoeAttnDims, B: int, T_q: int, max_k: int) -> int:
@@ -145,12 +147,11 @@ def moe_attn_prefill(dims: MoeAttnDims, q, k, v, cu_q, cu_k, max_k: int, scale: 
                      dev_status=None, stream=None):
     """Attention over packed prompts: q [T_q, q_heads, head_dim] over k, v [T_k, kv_heads, head_dim] -> out bf16."""
     hq, hkv, d = dims.q_heads, dims.kv_heads, dims.head_dim
-    (pq, sq), (pk, sk), (pv, sv) = _rows(q, hq, d, "q"), _rows(k, hkv, d, "k"), _rows(v, hkv, d, "v")
-    _same(v, k.shape[0], "v")
-    _same(cu_k, cu_q.shape[0], "cu_k")
-    T = q.shape[0]
-    _check(lib.moe_attn_prefill(dims, cu_q.shape[0] - 1, T, k.shape[0], max_k, pq, sq, pk, sk, pv, sv,
-                                _dev(cu_q, 4, "cu_q"), _dev(cu_k, 4, "cu_k"), scale, 1 if causal else 0,
+    (pq, sq, T), (pk, sk, nk), (pv, sv, nv) = _rows(q, hq, d, "q"), _rows(k, hkv, d, "k"), _rows(v, hkv, d, "v")
+    _same(nv, nk, "v")
+    (pcq, n), (pck, m) = _ints(cu_q, "cu_q"), _ints(cu_k, "cu_k")
+    _same(m, n, "cu_k")
+    _check(lib.moe_attn_prefill(dims, n - 1, T, nk, max_k, pq, sq, pk, sk, pv, sv, pcq, pck, scale, 1 if causal else 0,
                                 _out(out, T, hq, d, "out"), _dev(dev_status, 4, "dev_status"), _dev(ws, 1, "ws"),
                                 0 if ws is None else ws.numel(), _stream(stream)))
 
@@ -163,15 +164,17 @@ def moe_attn_decode(dims: MoeAttnDims, q, cache: KVCache, page_table, lens, max_
                     prefix_pages=None, prefix_len: int = 0, dev_status=None, stream=None):
     """Attention of one token per sequence, q [B, q_heads, head_dim], over the prefix's and its own cached keys."""
     B, width = page_table.shape
-    pq, sq = _rows(q, dims.q_heads, dims.head_dim, "q")
-    _same(q, B, "q")
-    _same(lens, B, "lens")
+    hq, d = dims.q_heads, dims.head_dim
+    pq, sq, nq = _rows(q, hq, d, "q")
+    plens, n = _ints(lens, "lens")
+    if not nq == n == B:
+        raise ValueError("q, lens and page_table must have one entry per sequence")
     if prefix_len > 0 and (prefix_pages is None or prefix_pages.numel() * cache.page_size < prefix_len):
         raise ValueError(f"prefix_pages must hold the pages of {prefix_len} tokens")
-    _check(lib.moe_attn_decode(dims, B, pq, sq, cache.check(dims), _dev(page_table, 4, "page_table"), width,
-                               _dev(lens, 4, "lens"), max_len, _dev(prefix_pages, 4, "prefix_pages"), prefix_len, scale,
-                               _out(out, B, dims.q_heads, dims.head_dim, "out"), _dev(dev_status, 4, "dev_status"),
-                               _dev(ws, 1, "ws"), 0 if ws is None else ws.numel(), _stream(stream)))
+    _check(lib.moe_attn_decode(dims, B, pq, sq, cache.check(dims), _dev(page_table, 4, "page_table"), width, plens,
+                               max_len, _dev(prefix_pages, 4, "prefix_pages"), prefix_len, scale,
+                               _out(out, B, hq, d, "out"), _dev(dev_status, 4, "dev_status"), _dev(ws, 1, "ws"),
+                               0 if ws is None else ws.numel(), _stream(stream)))
 
 
 class AttentionBuffers:
