@@ -29,8 +29,11 @@ struct PrefillArgs {
   int64_t q_stride, k_stride, v_stride;
   const int32_t *cu_q, *cu_k;
   uint16_t* out;
+  float* part_o;   // [T_q * q_heads][parts][D]: a part's sums, not divided
+  float* part_ml;  // [T_q * q_heads][parts][2]: its running maximum and sum (0: nothing in part_o)
   int32_t* status;
   int B, T_q, T_k, kv_heads, group, causal;
+  int parts, part_tiles;  // key tiles are cut into parts of this many, the last takes what is left
   float c;  // scale * log2(e): the softmax runs on powers of 2
 };
 
@@ -117,15 +120,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRing][kTileBytes];  // keys, values
 
   int b, local, n_tiles;
-  const int kvh = blockIdx.x % a.kv_heads;
-  if (!find_tile(a, kTileRows, blockIdx.x / a.kv_heads, b, local, n_tiles)) return;
+  const int kvh = blockIdx.x % a.kv_heads, part = blockIdx.x / a.kv_heads % a.parts;
+  if (!find_tile(a, kTileRows, blockIdx.x / a.kv_heads / a.parts, b, local, n_tiles)) return;
   // the same for the whole workgroup, and kept in scalar registers
   b = __builtin_amdgcn_readfirstlane(b);
   local = __builtin_amdgcn_readfirstlane(n_tiles - 1 - local);  // a sequence's longest rows first
   int q0, lq, k0, lk;
   sequence_rows(a.cu_q, b, a.T_q, q0, lq);
   sequence_rows(a.cu_k, b, a.T_k, k0, lk);
-  if (a.status && kvh == 0 && threadIdx.x == 0 &&
+  if (a.status && kvh == 0 && part == 0 && threadIdx.x == 0 &&
       (q0 != a.cu_q[b] || q0 + lq != a.cu_q[b + 1] || k0 != a.cu_k[b] || k0 + lk != a.cu_k[b + 1]))
     atomicOr(a.status, MOE_DEV_BAD_LENGTH);
 
@@ -147,13 +150,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
   const int first_limit = min(a.causal ? (int)(row0 / a.group) + lk - lq : lk - 1, lk - 1);
   const int tile_last = a.causal ? (int)((min(row0 + kTileRows, n_rows) - 1) / a.group) + lk - lq : lk - 1;
   const int n_key_tiles = tile_last < 0 ? 0 : tile_last / kKeys + 1;
+  // this part's tiles
+  const int kt0 = min(part * a.part_tiles, n_key_tiles);
+  const int kt1 = part == a.parts - 1 ? n_key_tiles : min(kt0 + a.part_tiles, n_key_tiles);
 
   v16f o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = v16f{};
   float m = kNoScore, l = 0.0f;
 
-  if (n_key_tiles > 0) {
+  if (kt0 < kt1) {
     v8bf qf[D / 16];
     const uint16_t* qrow = a.q + (q0 + (int64_t)tok) * a.q_stride + head * D + 8 * h;
 #pragma unroll
@@ -283,33 +289,47 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
       __builtin_amdgcn_sched_barrier(0);
     };
 
-    fetch_k(0);
-    fetch_k(1);
-    fetch_v(0);
-    fetch_k(2);
-    fetch_v(1);
+    fetch_k(kt0);
+    fetch_k(kt0 + 1);
+    fetch_v(kt0);
+    fetch_k(kt0 + 2);
+    fetch_v(kt0 + 1);
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kCalls) : "memory");
     s[0] = s[1] = v16f{};
 #pragma unroll
     for (int f = 0; f < kK; ++f)
-      s[f & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(k_place, v_place, f), qf[f >> 1], s[f & 1], 0, 0, 0);
+      s[f & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(k_place + kt0 % kRing * kTileBytes, v_place, f), qf[f >> 1],
+                                                         s[f & 1], 0, 0, 0);
     if (late) {
-      fetch_k(kRing - 1);
-      fetch_v(kRing - 2);
+      fetch_k(kt0 + kRing - 1);
+      fetch_v(kt0 + kRing - 2);
       asm volatile("s_barrier" : : : "memory");
     }
-    const int n_free = min((first_limit + 1) / kKeys, n_key_tiles);  // tiles without a masked key for any row
-    int kt = 0;
+    const int n_free = min((first_limit + 1) / kKeys, kt1);  // tiles before it have no masked key for any row
+    int kt = kt0;
     for (; kt < n_free; ++kt) step(std::false_type{}, kt);
-    for (; kt < n_key_tiles; ++kt) step(std::true_type{}, kt);
+    for (; kt < kt1; ++kt) step(std::true_type{}, kt);
     if (!late) asm volatile("s_barrier" : : : "memory");
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
   }
 
   l += __shfl_xor(l, 32, 64);
   if (!live) return;
+  const int64_t row = (q0 + (int64_t)tok) * (a.kv_heads * a.group) + head;
+  if (a.parts > 1) {
+    if (h == 0) *reinterpret_cast<float2*>(a.part_ml + (row * a.parts + part) * 2) = make_float2(m, l);
+    if (kt0 >= kt1) return;
+    float* prow = a.part_o + (row * a.parts + part) * D + 4 * h;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(prow + 32 * dt + 8 * i) =
+            make_float4(o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]);
+    return;
+  }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  uint16_t* orow = a.out + ((q0 + (int64_t)tok) * (a.kv_heads * a.group) + head) * D + 4 * h;
+  uint16_t* orow = a.out + row * D + 4 * h;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -319,15 +339,84 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
                      pack_bf16(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv));
 }
 
+// The parts' sums of a row, weighed by their maxima: D / 4 lanes a row, 16 bytes
+// each.  Rows outside all sequences have no parts and are left alone.
 template <int D>
-moe_status_t launch_prefill(const PrefillArgs& a, hipStream_t stream) {
-  constexpr int kWaves = 8;
-  // Row tiles (sequences may each add a part of one), heads fastest: workgroups that share keys have numbers equal
-  // mod 8 (one XCD's L2) where kv_heads is a multiple of 8, and all heads' longest rows come first.
-  const int64_t items = ((int64_t)a.T_q * a.group / (kWaves * kWaveRows) + a.B) * a.kv_heads;
-  if (items * kWaves * 64 >= (int64_t)1 << 32)
+__global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, int64_t n_rows) {
+  const int64_t row = (int64_t)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);
+  const int d = threadIdx.x % (D / 4) * 4;
+  if (row >= n_rows) return;
+  const int64_t t = row / (a.kv_heads * a.group);
+  if (t < a.cu_q[0] || t >= a.cu_q[a.B]) return;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + row * a.parts;
+  float m = kNoScore;
+  for (int p = 0; p < a.parts; ++p) m = fmaxf(m, ml[p].x);
+  float l = 0.0f;
+  v4f o = {};
+#pragma unroll 4
+  for (int p = 0; p < a.parts; ++p) {
+    const float2 x = ml[p];
+    if (x.y > 0.0f) {
+      const float f = __builtin_amdgcn_exp2f(x.x - m);
+      l += x.y * f;
+      o += *reinterpret_cast<const v4f*>(a.part_o + (row * a.parts + p) * D + d) * f;
+    }
+  }
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  *reinterpret_cast<uint2*>(a.out + row * D + d) =
+      make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+}
+
+constexpr int kWaves = 8;
+
+struct PrefillPlan {
+  int64_t tiles;  // bound on the row tiles
+  int parts, part_tiles;
+  size_t o_bytes, ml_bytes;
+};
+
+// How many parts the keys are cut into: the number whose estimated time is the
+// least.  A CU runs one workgroup at a time; one takes about 5 us and 1.4 us for
+// each of its key tiles (D = 128).  Joining costs a launch, 5 us, and the parts'
+// sums go to memory and back at about 4 TB/s.  509 tokens of 32 heads behind 8192
+// keys, 64 workgroups of 136 tiles: see the figures at launch_prefill.
+PrefillPlan plan_prefill(const moe_attn_dims_t& d, int32_t B, int32_t T_q, int32_t max_k) {
+  PrefillPlan p{};
+  const int group = d.q_heads / d.kv_heads;
+  p.tiles = (int64_t)T_q * group / (kWaves * kWaveRows) + B;  // sequences may each add a part of one
+  const int64_t items = p.tiles * d.kv_heads, rows = (int64_t)T_q * d.q_heads;
+  const int key_tiles = max_k / kKeys + 1;
+  double best = 0.0;
+  for (int parts = 1; parts <= 16; ++parts) {
+    const int part_tiles = (key_tiles + parts - 1) / parts;
+    const double rounds = (double)((items * parts + 255) / 256);
+    double us = rounds * (5.0 + 1.4 * part_tiles);
+    if (parts > 1) us += 5.0 + (double)rows * parts * d.head_dim * 8 / 4e6;
+    if (parts == 1 || us < best) {
+      best = us;
+      p.parts = parts;
+      p.part_tiles = part_tiles;
+    }
+  }
+  if (p.parts > 1) {
+    p.o_bytes = ((size_t)rows * p.parts * d.head_dim * sizeof(float) + 255) & ~(size_t)255;
+    p.ml_bytes = ((size_t)rows * p.parts * 2 * sizeof(float) + 255) & ~(size_t)255;
+  }
+  return p;
+}
+
+template <int D>
+moe_status_t launch_prefill(const PrefillArgs& a, const PrefillPlan& p, hipStream_t stream) {
+  // Heads fastest: workgroups that share keys have numbers equal mod 8 (one XCD's L2) where kv_heads is a multiple of
+  // 8, and all heads' longest rows come first.
+  const int64_t items = p.tiles * a.parts * a.kv_heads, rows = (int64_t)a.T_q * a.kv_heads * a.group;
+  constexpr int kJoinRows = 256 / (D / 4);
+  if (items * kWaves * 64 >= (int64_t)1 << 32 || (rows / kJoinRows + 1) * 256 >= (int64_t)1 << 32)
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_prefill: %lld row tiles", (long long)items);
   MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
+  if (a.parts > 1)
+    MOE_LAUNCH("attn_prefill_join", attn_prefill_join_kernel<D>, dim3((unsigned)((rows + kJoinRows - 1) / kJoinRows)),
+               dim3(256), 0, stream, a, rows);
   return check_launch("moe_attn_prefill");
 }
 
@@ -338,11 +427,9 @@ moe_status_t launch_prefill(const PrefillArgs& a, hipStream_t stream) {
 using namespace moe;
 
 extern "C" size_t moe_attn_prefill_workspace(moe_attn_dims_t d, int32_t B, int32_t T_q, int32_t max_k) {
-  (void)d;
-  (void)B;
-  (void)T_q;
-  (void)max_k;
-  return 0;
+  if (check_attn_dims(d, "moe_attn_prefill_workspace") != MOE_OK || B < 1 || T_q < 1 || max_k < 0) return 0;
+  const PrefillPlan p = plan_prefill(d, B, T_q, max_k);
+  return p.o_bytes + p.ml_bytes;
 }
 
 extern "C" moe_status_t moe_attn_prefill(moe_attn_dims_t d, int32_t B, int32_t T_q, int32_t T_k, int32_t max_k,
@@ -361,10 +448,14 @@ extern "C" moe_status_t moe_attn_prefill(moe_attn_dims_t d, int32_t B, int32_t T
   if (T_k > 0 && (st = check_rows(v, v_stride, d.kv_heads, d.head_dim, "moe_attn_prefill", "v")) != MOE_OK) return st;
   if (!cu_q || !cu_k || !out) return fail(MOE_ERR_INVALID_ARG, "moe_attn_prefill: null pointer");
   if (!aligned(out, 16)) return fail(MOE_ERR_INVALID_ARG, "moe_attn_prefill: out must be 16-byte aligned");
-  const size_t need = moe_attn_prefill_workspace(d, B, T_q, max_k);
+  const PrefillPlan p = plan_prefill(d, B, T_q, max_k);
+  const size_t need = p.o_bytes + p.ml_bytes;
   if (need && (!ws || ws_bytes < need || !aligned(ws, 256)))
     return fail(MOE_ERR_WORKSPACE, "moe_attn_prefill: workspace %zu bytes, needs %zu, 256-byte aligned", ws_bytes, need);
-  const PrefillArgs a{q, k, v, q_stride, k_stride, v_stride, cu_q, cu_k, out, dev_status,
-                      B, T_q, T_k, d.kv_heads, d.q_heads / d.kv_heads, causal != 0, scale * kLog2e};
-  return d.head_dim == 64 ? launch_prefill<64>(a, stream) : launch_prefill<128>(a, stream);
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  const PrefillArgs a{q, k, v, q_stride, k_stride, v_stride, cu_q, cu_k, out,
+                      p.parts > 1 ? reinterpret_cast<float*>(base) : nullptr,
+                      p.parts > 1 ? reinterpret_cast<float*>(base + p.o_bytes) : nullptr, dev_status,
+                      B, T_q, T_k, d.kv_heads, d.q_heads / d.kv_heads, causal != 0, p.parts, p.part_tiles, scale * kLog2e};
+  return d.head_dim == 64 ? launch_prefill<64>(a, p, stream) : launch_prefill<128>(a, p, stream);
 }
