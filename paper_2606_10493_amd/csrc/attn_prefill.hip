@@ -41,38 +41,54 @@ constexpr int kKeys = 64;  // keys per tile
 constexpr int kRing = 4;   // tiles of keys, and of values, in LDS
 constexpr int kWaveRows = 32;
 
-// Sequence b's rows of a packed tensor, cut to the tensor.
-__device__ __forceinline__ void sequence_rows(const int32_t* cu, int b, int total, int& first, int& count) {
-  const int lo = min(max(cu[b], 0), total), hi = min(max(cu[b + 1], 0), total);
-  first = lo;
-  count = max(hi - lo, 0);
+// Inclusive sum over the wave's lanes up to this one (register moves between
+// neighbouring lanes, rows of 16 and halves).
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
+  return x;
 }
 
-// The sequence and the place in it of row tile `tile`, tiles counted over the
-// sequences in order; false behind the last.  Every lane of a wave calls it.
-__device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile_rows, int64_t tile, int& b, int& local,
-                                          int& n_tiles) {
+// One row tile: its place in its sequence, the sequence's rows and keys, all the
+// same for the workgroup and in scalar registers.
+struct RowTile {
+  int local, n_tiles;      // place, and the sequence's number of tiles
+  int q0, lq, k0, lk;
+  bool cut;                // the offsets leave the tensors
+};
+
+// Row tile `tile`, counted over the sequences in order; false behind the last.
+// Every lane of a wave calls it.  32 bits hold the counts: the launch checks
+// that rows (T_q * group) and tiles do.
+__device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile_rows, int tile, RowTile& r) {
   const int lane = threadIdx.x & 63;
-  int64_t before = 0;
+  int before = 0;
   for (int base = 0; base < a.B; base += 64) {
-    int first, count = 0;
-    if (base + lane < a.B) sequence_rows(a.cu_q, base + lane, a.T_q, first, count);
-    const int n = (int)(((int64_t)count * a.group + tile_rows - 1) / tile_rows);
-    int64_t incl = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up(incl, d, 64);
-      if (lane >= d) incl += y;
-    }
+    const int b = min(base + lane, a.B - 1);
+    const int q_lo = a.cu_q[b], q_hi = a.cu_q[b + 1], k_lo = a.cu_k[b], k_hi = a.cu_k[b + 1];
+    const int q0 = min(max(q_lo, 0), a.T_q), k0 = min(max(k_lo, 0), a.T_k);
+    const int lq = base + lane < a.B ? max(min(max(q_hi, 0), a.T_q) - q0, 0) : 0;
+    const int lk = max(min(max(k_hi, 0), a.T_k) - k0, 0);
+    const bool cut = q0 != q_lo || q0 + lq != q_hi || k0 != k_lo || k0 + lk != k_hi;
+    const int n = (int)(((uint32_t)lq * a.group + tile_rows - 1) / tile_rows);
+    const int incl = wave_scan(n);
     const uint64_t past = __ballot(before + incl > tile);
     if (past) {
       const int w = __ffsll((unsigned long long)past) - 1;
-      b = base + w;
-      n_tiles = __shfl(n, w, 64);
-      local = (int)(tile - before - (__shfl(incl, w, 64) - n_tiles));
+      r.n_tiles = __builtin_amdgcn_readlane(n, w);
+      r.local = tile - before - (__builtin_amdgcn_readlane(incl, w) - r.n_tiles);
+      r.q0 = __builtin_amdgcn_readlane(q0, w);
+      r.lq = __builtin_amdgcn_readlane(lq, w);
+      r.k0 = __builtin_amdgcn_readlane(k0, w);
+      r.lk = __builtin_amdgcn_readlane(lk, w);
+      r.cut = __builtin_amdgcn_readlane(cut, w);
       return true;
     }
-    before += __shfl(incl, 63, 64);
+    before += __builtin_amdgcn_readlane(incl, 63);
   }
   return false;
 }
@@ -119,36 +135,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
   constexpr int kTileRows = kWaveRows * WAVES, kTileBytes = kKeys * D * 2;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRing][kTileBytes];  // keys, values
 
-  int b, local, n_tiles;
-  const int kvh = blockIdx.x % a.kv_heads, part = blockIdx.x / a.kv_heads % a.parts;
-  if (!find_tile(a, kTileRows, blockIdx.x / a.kv_heads / a.parts, b, local, n_tiles)) return;
-  // the same for the whole workgroup, and kept in scalar registers
-  b = __builtin_amdgcn_readfirstlane(b);
-  local = __builtin_amdgcn_readfirstlane(n_tiles - 1 - local);  // a sequence's longest rows first
-  int q0, lq, k0, lk;
-  sequence_rows(a.cu_q, b, a.T_q, q0, lq);
-  sequence_rows(a.cu_k, b, a.T_k, k0, lk);
-  if (a.status && kvh == 0 && part == 0 && threadIdx.x == 0 &&
-      (q0 != a.cu_q[b] || q0 + lq != a.cu_q[b + 1] || k0 != a.cu_k[b] || k0 + lk != a.cu_k[b + 1]))
-    atomicOr(a.status, MOE_DEV_BAD_LENGTH);
-
-  q0 = __builtin_amdgcn_readfirstlane(q0);
-  lq = __builtin_amdgcn_readfirstlane(lq);
-  k0 = __builtin_amdgcn_readfirstlane(k0);
-  lk = __builtin_amdgcn_readfirstlane(lk);
+  const uint32_t item = blockIdx.x / (uint32_t)a.kv_heads;
+  const int kvh = blockIdx.x - item * a.kv_heads, tile = item / (uint32_t)a.parts, part = item - tile * a.parts;
+  RowTile rt;
+  if (!find_tile(a, kTileRows, tile, rt)) return;
+  const int q0 = rt.q0, lq = rt.lq, k0 = rt.k0, lk = rt.lk;
+  if (rt.cut && a.status && kvh == 0 && part == 0 && threadIdx.x == 0) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
 
   const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t n_rows = (int64_t)lq * a.group;
-  const int64_t row0 = (int64_t)local * kTileRows;
-  const int64_t r = row0 + wave * kWaveRows + col;
+  const uint32_t group = a.group, n_rows = (uint32_t)lq * group;
+  const uint32_t row0 = (uint32_t)(rt.n_tiles - 1 - rt.local) * kTileRows;  // a sequence's longest rows first
+  const uint32_t r = row0 + wave * kWaveRows + col;
   const bool live = r < n_rows;
-  const int64_t rc = live ? r : n_rows - 1;
-  const int tok = (int)(rc / a.group), head = kvh * a.group + (int)(rc - (int64_t)tok * a.group);
+  const uint32_t rc = live ? r : n_rows - 1;
+  const int tok = rc / group, head = kvh * group + (rc - tok * group);
   // the last key that this row sees, that the tile's first row sees and that its last row sees
   const int limit = min(a.causal ? tok + lk - lq : lk - 1, lk - 1);
-  const int first_limit = min(a.causal ? (int)(row0 / a.group) + lk - lq : lk - 1, lk - 1);
-  const int tile_last = a.causal ? (int)((min(row0 + kTileRows, n_rows) - 1) / a.group) + lk - lq : lk - 1;
+  const int first_limit = min(a.causal ? (int)(row0 / group) + lk - lq : lk - 1, lk - 1);
+  const int tile_last = a.causal ? (int)((min(row0 + kTileRows, n_rows) - 1) / group) + lk - lq : lk - 1;
   const int n_key_tiles = tile_last < 0 ? 0 : tile_last / kKeys + 1;
   // this part's tiles
   const int kt0 = min(part * a.part_tiles, n_key_tiles);
