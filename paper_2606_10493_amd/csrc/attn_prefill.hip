@@ -33,7 +33,8 @@ struct PrefillArgs {
   float* part_ml;  // [T_q * q_heads][parts][2]: its running maximum and sum (0: nothing in part_o)
   int32_t* status;
   int B, T_q, T_k, kv_heads, group, causal;
-  int parts, part_tiles;  // key tiles are cut into parts of this many, the last takes what is left
+  uint32_t group_inverse;  // ceil(2^21 / group): n / group = n * group_inverse >> 21 for n < 1280, group <= 1024
+  int parts, part_tiles;   // key tiles are cut into parts of this many, the last takes what is left
   float c;  // scale * log2(e): the softmax runs on powers of 2
 };
 
@@ -146,14 +147,20 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t group = a.group, n_rows = (uint32_t)lq * group;
   const uint32_t row0 = (uint32_t)(rt.n_tiles - 1 - rt.local) * kTileRows;  // a sequence's longest rows first
-  const uint32_t r = row0 + wave * kWaveRows + col;
-  const bool live = r < n_rows;
-  const uint32_t rc = live ? r : n_rows - 1;
-  const int tok = rc / group, head = kvh * group + (rc - tok * group);
+  // row i of the tile, i < kTileRows: its token and head (rows behind the sequence's last are that row)
+  const uint32_t tok0 = row0 / group, head0 = row0 - tok0 * group, last_row = min((uint32_t)kTileRows, n_rows - row0) - 1;
+  const auto row_of = [&](uint32_t i, int& tok, int& head) __attribute__((always_inline)) {
+    const uint32_t n = head0 + min(i, last_row), t = n * a.group_inverse >> 21;
+    tok = tok0 + t;
+    head = kvh * group + (n - t * group);
+  };
+  int tok, head;
+  row_of(wave * kWaveRows + col, tok, head);
+  const bool live = (uint32_t)(wave * kWaveRows + col) <= last_row;
   // the last key that this row sees, that the tile's first row sees and that its last row sees
   const int limit = min(a.causal ? tok + lk - lq : lk - 1, lk - 1);
-  const int first_limit = min(a.causal ? (int)(row0 / group) + lk - lq : lk - 1, lk - 1);
-  const int tile_last = a.causal ? (int)((min(row0 + kTileRows, n_rows) - 1) / group) + lk - lq : lk - 1;
+  const int first_limit = min(a.causal ? (int)tok0 + lk - lq : lk - 1, lk - 1);
+  const int tile_last = a.causal ? (int)((row0 + last_row) / group) + lk - lq : lk - 1;
   const int n_key_tiles = tile_last < 0 ? 0 : tile_last / kKeys + 1;
   // this part's tiles
   const int kt0 = min(part * a.part_tiles, n_key_tiles);
@@ -165,11 +172,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
   float m = kNoScore, l = 0.0f;
 
   if (kt0 < kt1) {
-    v8bf qf[D / 16];
-    const uint16_t* qrow = a.q + (q0 + (int64_t)tok) * a.q_stride + head * D + 8 * h;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const v8bf*>(qrow + 16 * i);
-
     const uint16_t* kbase = a.k + (int64_t)k0 * a.k_stride + kvh * D;
     const uint16_t* vbase = a.v + (int64_t)k0 * a.v_stride + kvh * D;
     const uint32_t lds0 = lds_address(lds);
@@ -181,11 +183,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     };
     constexpr int kCalls = 2 * (kTileBytes / 1024 / WAVES);  // of a wave for one tile's keys and values
 
-    v16f s[2];  // scores of a tile
+    v8bf qf[D / 16];  // the row's query
+    v16f s[2];        // scores of a tile
     union {
       v8bf v[4];
       uint32_t x[16];
-    } p;  // its numerators
+    } p;              // its numerators
 
     // Operand f of a step: the next tile's keys (the first D / 8, the two blocks of 32 keys in turn), then this tile's
     // values.  The swizzle makes an operand's place the first one's with some bits flipped, plus a constant.
@@ -294,12 +297,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
       __builtin_amdgcn_sched_barrier(0);
     };
 
+    // The wave's rows of queries come the way that keys do, whole rows straight into LDS (its part of the values' ring,
+    // which is empty yet), and from there as operands.
+    const int q_lds = lds0 + kRing * kTileBytes + wave * (kWaveRows * D * 2);
+    constexpr int kQCalls = kWaveRows * D * 2 / 1024;
+#pragma unroll
+    for (int i = 0; i < kQCalls; ++i) {
+      const int row = i * (kWaveRows / kQCalls) + lane / (D / 8);
+      const int c = (staged<D>(row, lane % (D / 8)) % (D * 2)) / 16;
+      int t, hd;
+      row_of(wave * kWaveRows + row, t, hd);
+      async_load_1k(a.q + (int64_t)(q0 + t) * a.q_stride + hd * D + 8 * c, q_lds + 1024 * i);
+    }
     fetch_k(kt0);
     fetch_k(kt0 + 1);
-    fetch_v(kt0);
     fetch_k(kt0 + 2);
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kCalls / 2) : "memory");
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+      qf[i] = *(__attribute__((address_space(3))) const v8bf*)(uintptr_t)(q_lds + staged<D>(col, 2 * i + h));
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    fetch_v(kt0);
     fetch_v(kt0 + 1);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kCalls) : "memory");
     s[0] = s[1] = v16f{};
 #pragma unroll
     for (int f = 0; f < kK; ++f)
@@ -308,40 +327,62 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     if (late) {
       fetch_k(kt0 + kRing - 1);
       fetch_v(kt0 + kRing - 2);
-      asm volatile("s_barrier" : : : "memory");
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kCalls) : "memory");
     }
     const int n_free = min((first_limit + 1) / kKeys, kt1);  // tiles before it have no masked key for any row
     int kt = kt0;
     for (; kt < n_free; ++kt) step(std::false_type{}, kt);
     for (; kt < kt1; ++kt) step(std::true_type{}, kt);
     if (!late) asm volatile("s_barrier" : : : "memory");
-    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    wait_async_and_barrier<0>();  // no fetch is on its way to LDS, and no wave reads from it any more
   }
 
   l += __shfl_xor(l, 32, 64);
-  if (!live) return;
-  const int64_t row = (q0 + (int64_t)tok) * (a.kv_heads * a.group) + head;
+  // Whole rows go out: a lane has pieces of 4 elements of one row, which the wave's part of LDS turns into rows (stores
+  // of 16 or 32 bytes a row took three times as long as the rest of a short sequence's work).
+  const int64_t heads = a.kv_heads * group;
+  uint8_t* turn = &lds[0][0][0] + wave * (2 * kRing * kTileBytes / WAVES);
   if (a.parts > 1) {
-    if (h == 0) *reinterpret_cast<float2*>(a.part_ml + (row * a.parts + part) * 2) = make_float2(m, l);
+    const int64_t row = (q0 + (int64_t)tok) * heads + head;
+    if (live && h == 0) *reinterpret_cast<float2*>(a.part_ml + (row * a.parts + part) * 2) = make_float2(m, l);
     if (kt0 >= kt1) return;
-    float* prow = a.part_o + (row * a.parts + part) * D + 4 * h;
+    constexpr int kPieces = D / 4;  // of 16 bytes
+    static_assert(kWaveRows * D * 4 <= 2 * kRing * kTileBytes / WAVES, "a wave's rows in fp32 fit its part of LDS");
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(prow + 32 * dt + 8 * i) =
+        *reinterpret_cast<float4*>(turn + col * (D * 4) + (((8 * dt + 2 * i + h) ^ (col & 15)) * 16)) =
             make_float4(o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]);
+#pragma unroll
+    for (int i = 0; i < kWaveRows * kPieces / 64; ++i) {
+      const int at = 64 * i + lane, rr = at / kPieces, c = at % kPieces;
+      if ((uint32_t)(wave * kWaveRows + rr) > last_row) continue;
+      int t, hd;
+      row_of(wave * kWaveRows + rr, t, hd);
+      *reinterpret_cast<float4*>(a.part_o + (((q0 + (int64_t)t) * heads + hd) * a.parts + part) * D + 4 * c) =
+          *reinterpret_cast<const float4*>(turn + rr * (D * 4) + ((c ^ (rr & 15)) * 16));
+    }
     return;
   }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  uint16_t* orow = a.out + row * D + 4 * h;
+  constexpr int kPieces = D / 8;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<uint2*>(orow + 32 * dt + 8 * i) =
+      *reinterpret_cast<uint2*>(turn + staged<D>(col, 4 * dt + i) + 8 * h) =
           make_uint2(pack_bf16(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv),
                      pack_bf16(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv));
+#pragma unroll
+  for (int i = 0; i < kWaveRows * kPieces / 64; ++i) {
+    const int at = 64 * i + lane, rr = at / kPieces, c = at % kPieces;
+    if ((uint32_t)(wave * kWaveRows + rr) > last_row) continue;
+    int t, hd;
+    row_of(wave * kWaveRows + rr, t, hd);
+    *reinterpret_cast<uint4*>(a.out + ((q0 + (int64_t)t) * heads + hd) * D + 8 * c) =
+        *reinterpret_cast<const uint4*>(turn + staged<D>(rr, c));
+  }
 }
 
 // The parts' sums of a row, weighed by their maxima: D / 4 lanes a row, 16 bytes
@@ -461,6 +502,8 @@ extern "C" moe_status_t moe_attn_prefill(moe_attn_dims_t d, int32_t B, int32_t T
   const PrefillArgs a{q, k, v, q_stride, k_stride, v_stride, cu_q, cu_k, out,
                       p.parts > 1 ? reinterpret_cast<float*>(base) : nullptr,
                       p.parts > 1 ? reinterpret_cast<float*>(base + p.o_bytes) : nullptr, dev_status,
-                      B, T_q, T_k, d.kv_heads, d.q_heads / d.kv_heads, causal != 0, p.parts, p.part_tiles, scale * kLog2e};
+                      B, T_q, T_k, d.kv_heads, d.q_heads / d.kv_heads, causal != 0,
+                      (uint32_t)(((1 << 21) + d.q_heads / d.kv_heads - 1) / (d.q_heads / d.kv_heads)), p.parts, p.part_tiles,
+                      scale * kLog2e};
   return d.head_dim == 64 ? launch_prefill<64>(a, p, stream) : launch_prefill<128>(a, p, stream);
 }
