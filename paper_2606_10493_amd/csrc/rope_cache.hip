@@ -43,19 +43,19 @@ struct RopeArgs {
   const int32_t *positions, *slots;
   const float* table;
   moe_kv_cache_t cache;
-  uint16_t *q_out, *k_out;  // may be q, k: every lane reads its row before any lane writes it
+  uint16_t *q_out, *k_out;  // may be q, k: a lane reads what it writes before that, and nothing else
   int32_t* status;
   int32_t n_pos, rot_dim, page_shift;
   int T, q_heads, kv_heads, layout;
 };
 
-// Eight elements at offset 8 * sub of a head's row, rotated.  cs: this lane's
-// cosines and sines: HALF 8 + 8 (its elements' pairs), INTERLEAVED 4 + 4.
-// The definition rounds every product and sum: no FMA.
-__device__ __forceinline__ void rotate8(float (&x)[8], const uint16_t* row, int e, int rot, bool interleaved,
+// Eight elements at offset e of a head's row, rotated.  c, s: this lane's cosines
+// and sines: HALF 8 + 8 (its elements' pairs), INTERLEAVED 4 + 4.  partner: HALF,
+// the elements that lie half the rotated part away.  The definition rounds every
+// product and sum: no FMA.
+__device__ __forceinline__ void rotate8(float (&x)[8], const uint4 partner, bool interleaved, bool low,
                                         const float (&c)[8], const float (&s)[8]) {
 #pragma clang fp contract(off)
-  if (e >= rot) return;
   if (interleaved) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -66,10 +66,8 @@ __device__ __forceinline__ void rotate8(float (&x)[8], const uint16_t* row, int 
     }
     return;
   }
-  const int half = rot / 2;
-  const bool low = e < half;
   float p[8];
-  load8_f32(row + (low ? e + half : e - half), p);
+  bf16x8_to_f32(partner, p);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float xc = x[i] * c[i], ps = p[i] * s[i];
@@ -84,7 +82,10 @@ __device__ __forceinline__ uint4 to_bf16x8(const float (&x)[8]) {
 // A group of D / 8 lanes takes one token's rows PER * blockIdx.y .. + PER - 1,
 // counted over the query heads, the key heads and (with a cache) the value
 // heads.  The groups of a wave are consecutive tokens at the same rows, so a
-// wave's branches go one way.
+// wave's branches go one way.  Rows share the token's position, slot and table
+// row: four a group where that leaves the card 4096 workgroups (8192 tokens, 48
+// rows: 61 us with one a group, 48 with four), else one (16 tokens: 4.0 us, 6.4
+// with four).
 template <int D, int PER>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   constexpr int kLanes = D / 8, kTokens = 256 / kLanes;
@@ -124,6 +125,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     }
   }
 
+  const int half = a.rot_dim / 2;
+  const bool turns = e < a.rot_dim, low = e < half;
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const int r = blockIdx.y * PER + j;
@@ -134,8 +137,15 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     if (!base) continue;
     const uint16_t* row = base + t * (kind == 0 ? a.q_stride : kind == 1 ? a.k_stride : a.v_stride) + h * D;
     float x[8];
-    load8_f32(row + e, x);
-    if (kind < 2) rotate8(x, row, e, a.rot_dim, interleaved, c, s);
+    const uint4 raw = *reinterpret_cast<const uint4*>(row + e);
+    uint4 partner = raw;  // HALF: what the lane half the rotated part away has
+    if (kind < 2 && !interleaved) {
+      const int from = !turns ? sub : low ? sub + half / 8 : sub - half / 8;
+      partner = make_uint4(__shfl(raw.x, from, kLanes), __shfl(raw.y, from, kLanes), __shfl(raw.z, from, kLanes),
+                           __shfl(raw.w, from, kLanes));
+    }
+    bf16x8_to_f32(raw, x);
+    if (kind < 2 && turns) rotate8(x, partner, interleaved, low, c, s);
     if (kind == 0) *reinterpret_cast<uint4*>(a.q_out + (t * a.q_heads + h) * D + e) = to_bf16x8(x);
     if (kind == 1 && a.k_out) *reinterpret_cast<uint4*>(a.k_out + (t * a.kv_heads + h) * D + e) = to_bf16x8(x);
     if (kind > 0 && page >= 0) {
@@ -169,7 +179,10 @@ moe_status_t launch_rope(const RopeArgs& all, const char* name, hipStream_t stre
     a.positions += t0;
     if (a.slots) a.slots += t0;
     const unsigned gx = (unsigned)((a.T + 256 / (D / 8) - 1) / (256 / (D / 8)));
-    MOE_LAUNCH(name, (rope_kernel<D, 1>), dim3(gx, n_rows), dim3(256), 0, stream, a);
+    if ((int64_t)gx * n_rows < 4096)
+      MOE_LAUNCH(name, (rope_kernel<D, 1>), dim3(gx, n_rows), dim3(256), 0, stream, a);
+    else
+      MOE_LAUNCH(name, (rope_kernel<D, 4>), dim3(gx, (n_rows + 3) / 4), dim3(256), 0, stream, a);
   }
   return check_launch(name);
 }
@@ -189,10 +202,28 @@ moe_status_t check_rope(const moe_attn_dims_t& d, int32_t T, const int32_t* posi
 }
 
 // ------------------------------------------------------------------ read back
-// Rows of one token and kSeqHeads heads per group of D / 8 lanes, keys and
-// values.  The token's sequence is found by bisection of cu.
+// The sequence of token t: cu[lo] <= t < cu[lo + 1], cu[0] <= t < cu[B].  The
+// group's lanes look at as many places at once as they are, so that up to 17 (9)
+// sequences cost one round trip and 289 (81) two.  Offsets that decrease give
+// some lo in [0, B).
+template <int kLanes>
+__device__ __forceinline__ int sequence_of(const int32_t* __restrict__ cu, int B, int64_t t, int sub) {
+  int lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const int hop = (hi - lo + kLanes) / (kLanes + 1), probe = lo + (sub + 1) * hop;
+    const uint64_t below = __ballot(probe < hi && cu[min(probe, B)] <= t);
+    const int n = __popcll(below >> ((threadIdx.x & 63) - sub) & ((1u << kLanes) - 1));
+    lo += n * hop;
+    hi = min(hi, lo + hop);
+  }
+  return min(lo, B - 1);
+}
+
+// A group of D / 8 lanes takes one token's keys and values of `per` heads.  What
+// is written is read by another launch, if at all from a cache that holds all of
+// it: the stores are non-temporal (65k tokens of 8 heads of 128: 132 -> 123 us).
 template <int D>
-__global__ __launch_bounds__(256) void cache_read_kernel(moe_kv_cache_t cache, int page_shift, int kv_heads,
+__global__ __launch_bounds__(256) void cache_read_kernel(moe_kv_cache_t cache, int page_shift, int kv_heads, int per,
                                                          const int32_t* __restrict__ pages, int B, int width,
                                                          const int32_t* __restrict__ cu, int T,
                                                          uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out,
@@ -200,24 +231,22 @@ __global__ __launch_bounds__(256) void cache_read_kernel(moe_kv_cache_t cache, i
   constexpr int kLanes = D / 8, kTokens = 256 / kLanes;
   const int sub = threadIdx.x % kLanes;
   const int64_t t = (int64_t)blockIdx.x * kTokens + threadIdx.x / kLanes;
-  if (t >= T || t < cu[0] || t >= cu[B]) return;
-  int lo = 0, hi = B;  // cu[lo] <= t < cu[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (cu[mid] <= t) lo = mid; else hi = mid;
-  }
-  const int64_t at = t - cu[lo];
+  if (t >= T || t < cu[0] || t >= cu[B]) return;  // whole groups leave together
+  const int b = sequence_of<kLanes>(cu, B, t, sub);
+  const int64_t at = t - cu[b];
   int bad = 0;
   int64_t page = 0;
-  if ((at >> page_shift) >= width) {
+  if (at < 0 || (at >> page_shift) >= width) {
     bad = MOE_DEV_BAD_LENGTH;
   } else {
-    page = pages[(int64_t)lo * width + (at >> page_shift)];
+    page = pages[(int64_t)b * width + (at >> page_shift)];
     if (page < 0 || page >= cache.n_pages) bad = MOE_DEV_BAD_PAGE;
   }
   if (bad && status && sub == 0) atomicOr(status, bad);
   const int64_t place0 = ((page * kv_heads) << page_shift) + (at & (cache.page_size - 1));
-  for (int h = 0; h < kv_heads; ++h) {
+  const int h1 = min((int)(blockIdx.y + 1) * per, kv_heads);
+#pragma unroll 4
+  for (int h = blockIdx.y * per; h < h1; ++h) {
     const int64_t place = place0 + ((int64_t)h << page_shift);
     const int64_t out = (t * kv_heads + h) * D + sub * 8;
 #pragma unroll
@@ -232,7 +261,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(moe_kv_cache_t cache, i
         for (int i = 0; i < 8; ++i) x[i] = (float)y[i] * s;
         o = to_bf16x8(x);
       }
-      *reinterpret_cast<uint4*>((w ? v_out : k_out) + out) = o;
+      const u32x4_stream words = {o.x, o.y, o.z, o.w};
+      __builtin_nontemporal_store(words, reinterpret_cast<u32x4_stream*>((w ? v_out : k_out) + out));
     }
   }
 }
@@ -324,12 +354,16 @@ extern "C" moe_status_t moe_cache_read(moe_attn_dims_t d, moe_kv_cache_t cache, 
     return fail(MOE_ERR_INVALID_ARG, "moe_cache_read: outputs must be 16-byte aligned");
   const int shift = log2_of(cache.page_size), per = 256 / (d.head_dim / 8);
   if (T > kSpanTokens) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_cache_read: T=%d is over %lld", T, (long long)kSpanTokens);
-  const dim3 grid((unsigned)((T + per - 1) / per));
+  const unsigned gx = (unsigned)((T + per - 1) / per);
+  const int heads = gx < 1024 ? 1 : d.kv_heads;  // few tokens: more workgroups rather than longer ones
+  const dim3 grid(gx, (d.kv_heads + heads - 1) / heads);
   if (d.head_dim == 64)
-    MOE_LAUNCH("cache_read", cache_read_kernel<64>, grid, dim3(256), 0, stream, cache, shift, d.kv_heads, page_table, B,
+    MOE_LAUNCH("cache_read", cache_read_kernel<64>, grid, dim3(256), 0, stream, cache, shift, d.kv_heads, heads,
+               page_table, B,
                table_width, cu, T, k_out, v_out, dev_status);
   else
-    MOE_LAUNCH("cache_read", cache_read_kernel<128>, grid, dim3(256), 0, stream, cache, shift, d.kv_heads, page_table, B,
+    MOE_LAUNCH("cache_read", cache_read_kernel<128>, grid, dim3(256), 0, stream, cache, shift, d.kv_heads, heads,
+               page_table, B,
                table_width, cu, T, k_out, v_out, dev_status);
   return check_launch("moe_cache_read");
 }
