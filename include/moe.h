@@ -604,7 +604,7 @@ moe_status_t moe_attn_prefill(moe_attn_dims_t dims, int32_t B, int32_t T_q, int3
  * rows of one product.  page_table: device int32 [B, table_width], entries
  * behind a sequence's last page are not read.  lens: device int32 [B], 0 for
  * an idle slot (with no prefix either its output is zeros).  A length below 0
- * or beyond table_width pages is cut and sets MOE_DEV_BAD_LENGTH; a page id
+ * or beyond table_width pages (or 2^30) is cut and sets MOE_DEV_BAD_LENGTH; a page id
  * outside the cache sets MOE_DEV_BAD_PAGE and leaves the outputs that need it
  * unspecified.  max_len: the longest of lens; it decides how the work is split
  * and nothing else.  q: [B, q_heads, head_dim]; out contiguous, no overlap.

@@ -50,6 +50,7 @@ struct DecodeArgs {
 constexpr int kKeys = 32;  // keys per step of a wave
 constexpr int kWaves = 4;
 constexpr int kStride = kKeys * kWaves;
+constexpr int kMostKeys = 1 << 30;  // of a sequence: key indices and the steps behind them stay in 32 bits
 
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
@@ -84,85 +85,94 @@ __device__ __forceinline__ float quad_max(float x) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// 32 keys and values on their way.
+// 32 keys and values on their way: lane l has 16-byte chunk l % (D / 16) of rows
+// l / (D / 16) + ..., so that a load covers whole rows, and key l's scale (lanes
+// 0..31) or value l - 32's.
 template <int D>
 struct Tile {
-  uint4 k[2][D / 64], v[D / 32];
-  float4 ks[2], vs[2];
+  u32x4_stream k[D / 32], v[D / 32];
+  float scale;
 };
 
 // A part of one sequence's (or the prefix's) keys: [begin, end) of the `len`
-// that `pages` hold, key/value head kvh.
+// that the `width` entries of `pages` hold, key/value head kvh.
 struct Part {
   const int32_t* pages;
-  int len, begin, end, kvh;
+  int width, len, begin, end, kvh;
 };
 
-// Keys [t, t + 32) lie in one page or two: each half of 16 in one.
+// The pages of keys [t, t + 32): each half of 16 lies in one.  Entries behind the
+// sequence's last page may be looked at, and are not used.
 struct Pages {
   int id[2];
 };
 __device__ __forceinline__ Pages pages_of(const DecodeArgs& a, const Part& p, int t) {
   Pages r;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) r.id[u] = p.pages[min(t + 16 * u, p.len - 1) >> a.page_shift];
+  for (int u = 0; u < 2; ++u) r.id[u] = p.pages[min((t + 16 * u) >> a.page_shift, p.width - 1)];
   return r;
 }
 
+// A wave's part of LDS: keys, values (rows of D codes in 16-byte chunks), scales.
+// The swizzles spread what one instruction reads over the 256 bytes of the banks:
+// 16 keys at one chunk, or the 16 values' rows of two 8 x 16 blocks at one chunk.
 template <int D>
-__device__ __forceinline__ int value_place(int row, int c) {
-  const int f = D == 128 ? ((row >> 1) & 3) | ((row >> 2) & 4) : ((row >> 2) & 1) | ((row >> 3) & 2);
-  return row * D + ((c ^ f) * 16);
-}
+struct Staged {
+  static constexpr int kV = kKeys * D, kScale = 2 * kKeys * D, kBytes = kScale + 64 * 4;
+  static __device__ __forceinline__ int key(int row, int c) {
+    return row * D + ((c ^ (D == 128 ? (row >> 1) & 7 : (row >> 2) & 3)) * 16);
+  }
+  static __device__ __forceinline__ int value(int row, int c) {
+    return kV + row * D + ((c ^ (D == 128 ? ((row >> 1) & 3) | ((row >> 2) & 4) : ((row >> 2) & 1) | ((row >> 3) & 2))) * 16);
+  }
+};
 
-template <int D>
+// Loads keys [t0, t0 + 32), t0 < len.  Keys behind the end repeat the last, or
+// the first half where the second holds none.  kOnce: nothing else reads them in
+// this launch, so they need no place in the caches (64 ragged contexts: 90 us
+// without, 78 with, whole rows per load in both).
+template <int D, bool kOnce>
 __device__ __forceinline__ void load_tile(const DecodeArgs& a, const Part& p, int t0, const Pages& pg, bool& bad,
                                           Tile<D>& x) {
   constexpr int kChunks = D / 16;
-  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
-  const int mask = a.cache.page_size - 1, last = p.len - 1;
-  int64_t base[2];
-  int row0[2];  // keys behind the end repeat the last
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const bool wrong = pg.id[u] < 0 || pg.id[u] >= a.cache.n_pages;
-    bad |= wrong;
-    row0[u] = min(t0 + 16 * u, last) & ~15;
-    base[u] = ((int64_t)(wrong ? 0 : pg.id[u]) * a.kv_heads + p.kvh) << a.page_shift;
-  }
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int t = min(row0[u] + c16, last) & mask;
-    const uint8_t* krow = a.cache.k + (base[u] + t) * D + 16 * g;
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) x.k[u][i] = *reinterpret_cast<const uint4*>(krow + 64 * i);
-  }
+  const int lane = threadIdx.x & 63, mask = a.cache.page_size - 1, last = p.len - 1;
+  const bool two = t0 + 16 <= last;
+  const int id0 = pg.id[0], id1 = two ? pg.id[1] : id0;
+  const bool wrong0 = id0 < 0 || id0 >= a.cache.n_pages, wrong1 = id1 < 0 || id1 >= a.cache.n_pages;
+  bad |= wrong0 | wrong1;
+  // the first key of each half, counted in rows of the cache
+  const int64_t row0 = (((int64_t)(wrong0 ? 0 : id0) * a.kv_heads + p.kvh) << a.page_shift) + (t0 & mask);
+  const int64_t row1 = two ? (((int64_t)(wrong1 ? 0 : id1) * a.kv_heads + p.kvh) << a.page_shift) + ((t0 + 16) & mask) : row0;
+  const int left = last - t0, left1 = two ? left - 16 : left;  // rows behind these repeat them
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
-    const int at = 64 * i + lane, row = at / kChunks, c = at % kChunks, u = row >> 4;
-    const int t = min((u ? row0[1] : row0[0]) + (row & 15), last) & mask;
-    x.v[i] = *reinterpret_cast<const uint4*>(a.cache.v + ((u ? base[1] : base[0]) + t) * D + 16 * c);
+    const int at = 64 * i + lane, row = at / kChunks, c = at % kChunks;
+    const int64_t from = (row < 16 ? row0 + min(row, left) : row1 + min(row - 16, left1)) * D + 16 * c;
+    const u32x4_stream* k = reinterpret_cast<const u32x4_stream*>(a.cache.k + from);
+    const u32x4_stream* v = reinterpret_cast<const u32x4_stream*>(a.cache.v + from);
+    x.k[i] = kOnce ? __builtin_nontemporal_load(k) : *k;
+    x.v[i] = kOnce ? __builtin_nontemporal_load(v) : *v;
   }
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int64_t at = base[u] + (row0[u] & mask) + 4 * g;
-    x.ks[u] = *reinterpret_cast<const float4*>(a.cache.k_scale + at);
-    x.vs[u] = *reinterpret_cast<const float4*>(a.cache.v_scale + at);
-  }
+  const int row = lane & 31;
+  const float* scales = lane < 32 ? a.cache.k_scale : a.cache.v_scale;
+  x.scale = scales[row < 16 ? row0 + min(row, left) : row1 + min(row - 16, left1)];
 }
 
-// The step at t0, whose keys and values are in x; once they are taken from there,
-// `next` loads those of the next step.
+// The step at t0, whose keys and values are in x; once they are in LDS, `next`
+// loads those of the next step.
 template <int D, int NC, typename Next>
 __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int t0, const Tile<D>& x,
-                                         const v8bf (&qf)[NC][D / 32], uint8_t* lds_v, Running<D, NC>& run, Next next) {
+                                         const v8bf (&qf)[NC][D / 32], uint8_t* lds, Running<D, NC>& run, Next next) {
   constexpr int kChunks = D / 16;
   const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
     const int at = 64 * i + lane;
-    *reinterpret_cast<uint4*>(lds_v + value_place<D>(at / kChunks, at % kChunks)) = x.v[i];
+    *reinterpret_cast<u32x4_stream*>(lds + Staged<D>::key(at / kChunks, at % kChunks)) = x.k[i];
+    *reinterpret_cast<u32x4_stream*>(lds + Staged<D>::value(at / kChunks, at % kChunks)) = x.v[i];
   }
+  *reinterpret_cast<float*>(lds + Staged<D>::kScale + 4 * lane) = x.scale;
+  next();
   v4f s[NC][2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
@@ -170,7 +180,8 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
     for (int n = 0; n < NC; ++n) s[n][u] = v4f{};
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
-      const v8bf lo = e4m3x8_to_bf16(x.k[u][i].x, x.k[u][i].y), hi = e4m3x8_to_bf16(x.k[u][i].z, x.k[u][i].w);
+      const uint4 k = *reinterpret_cast<const uint4*>(lds + Staged<D>::key(16 * u + c16, g + 4 * i));
+      const v8bf lo = e4m3x8_to_bf16(k.x, k.y), hi = e4m3x8_to_bf16(k.z, k.w);
 #pragma unroll
       for (int n = 0; n < NC; ++n) {
         s[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, qf[n][2 * i], s[n][u], 0, 0, 0);
@@ -182,17 +193,17 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
   float vtop = run.vref;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    const float kk[4] = {x.ks[u].x, x.ks[u].y, x.ks[u].z, x.ks[u].w}, vv[4] = {x.vs[u].x, x.vs[u].y, x.vs[u].z, x.vs[u].w};
+    const v4f kk = *reinterpret_cast<const v4f*>(lds + Staged<D>::kScale + 4 * (16 * u + 4 * g));
+    const v4f vv = *reinterpret_cast<const v4f*>(lds + Staged<D>::kScale + 4 * (32 + 16 * u + 4 * g));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const bool there = t0 + 16 * u + 4 * g + i < p.len;  // a slot behind the end may hold any bits
-      ks[u][i] = there ? kk[i] * a.c : -1.0f;              // scales are not negative
+      const bool there = t0 + 16 * u + 4 * g + i < p.len;
+      ks[u][i] = there ? kk[i] * a.c : -1.0f;  // scales are not negative
       vs[u][i] = there ? vv[i] : 0.0f;
       vtop = fmaxf(vtop, vs[u][i]);
     }
   }
   vtop = quad_max(vtop);
-  next();
   const float inv = 1.0f / vtop, faded = run.vref * inv;
   run.vref = vtop;
 #pragma unroll
@@ -239,7 +250,7 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-        (__attribute__((address_space(3))) v2i*)(lds_v + value_place<D>(row, i) + 8 * (c16 & 1)));
+        (__attribute__((address_space(3))) v2i*)(lds + Staged<D>::value(row, i) + 8 * (c16 & 1)));
     const v8h vf = e4m3x8_to_f16(y[0], y[1]);
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
@@ -256,8 +267,9 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
 template <int D, int NC>
 __global__ __launch_bounds__(64 * kWaves, NC == 1 ? 3 : 2) void attn_decode_kernel(DecodeArgs a) {
   constexpr int kCols = 16 * NC;
-  __shared__ __attribute__((aligned(16))) uint8_t lds_v[kWaves][kKeys * D];
-  __shared__ __attribute__((aligned(16))) float lds_o[kWaves][16][D + 4];
+  // the waves' keys and values; behind the last step their sums
+  constexpr int kWaveBytes = Staged<D>::kBytes > 16 * (D + 4) * 4 ? Staged<D>::kBytes : 16 * (D + 4) * 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves][kWaveBytes];
   __shared__ float lds_m[kWaves][kCols], lds_l[kWaves][kCols];
   const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -277,20 +289,28 @@ __global__ __launch_bounds__(64 * kWaves, NC == 1 ? 3 : 2) void attn_decode_kern
   const int blocks = shared ? a.prefix_blocks : a.own_blocks;
   const int col0 = item % blocks * kCols, part = item / blocks;
   const int cols = min(kCols, (shared ? a.B * a.group : a.group) - col0);
-  bool bad_len = false;
   if (shared) {
     p.pages = a.prefix_pages;
+    p.width = ((a.prefix_len - 1) >> a.page_shift) + 1;
     p.len = a.prefix_len;
     slot = part;
   } else {
     p.pages = a.pages + (int64_t)b * a.width;
-    p.len = a.lens[b];
-    const int64_t most = min((int64_t)a.width << a.page_shift, (int64_t)0x7fffffff);
-    bad_len = p.len < 0 || p.len > most;
-    p.len = p.len < 0 ? 0 : (int)min((int64_t)p.len, most);
+    p.width = a.width;
     slot = a.prefix_parts + part;
   }
   const int64_t begin = (int64_t)part * a.part_keys;
+  if (begin >= min((int64_t)p.width << a.page_shift, (int64_t)kMostKeys) && part > 0) return;  // as below, whatever the length
+  // the first step's pages are on their way while the length is
+  Pages first = {};
+  if (p.width > 0) first = pages_of(a, p, (int)begin + wave * kKeys);
+  bool bad_len = false;
+  if (!shared) {
+    p.len = a.lens[b];
+    const int64_t most = min((int64_t)a.width << a.page_shift, (int64_t)kMostKeys);
+    bad_len = p.len < 0 || p.len > most;
+    p.len = p.len < 0 ? 0 : (int)min((int64_t)p.len, most);
+  }
   const bool last_part = part == (shared ? a.prefix_parts : a.own_parts) - 1;
   if (bad_len && a.status && part == 0 && threadIdx.x == 0) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
   if (begin >= p.len && part > 0) return;  // the join looks at lens, too
@@ -327,19 +347,25 @@ __global__ __launch_bounds__(64 * kWaves, NC == 1 ? 3 : 2) void attn_decode_kern
     }
     bool bad = false;
     Tile<D> x;
-    load_tile<D>(a, p, t, pages_of(a, p, t), bad, x);
-    Pages ahead = pages_of(a, p, t + kStride);
+    Pages ahead = first;
+    const auto load = [&](int at) __attribute__((always_inline)) {
+      if (shared || a.own_blocks > 1)
+        load_tile<D, false>(a, p, at, ahead, bad, x);
+      else
+        load_tile<D, true>(a, p, at, ahead, bad, x);
+      ahead = pages_of(a, p, at + kStride);
+    };
+    load(t);
     for (; t < p.end; t += kStride)
-      use_tile<D, NC>(a, p, t, x, qf, lds_v[wave], run, [&] {
-        if (t + kStride >= p.end) return;
-        load_tile<D>(a, p, t + kStride, ahead, bad, x);
-        ahead = pages_of(a, p, t + 2 * kStride);
+      use_tile<D, NC>(a, p, t, x, qf, lds[wave], run, [&]() __attribute__((always_inline)) {
+        if (t + kStride < p.end) load(t + kStride);
       });
     if (bad && a.status && lane == 0) atomicOr(a.status, MOE_DEV_BAD_PAGE);
   }
 
   // the waves' sums joined, one block of 16 columns at a time
   const bool whole = a.prefix_parts + a.own_parts == 1;
+  const auto sums = [&](int w, int col) { return reinterpret_cast<float*>(lds[w]) + col * (D + 4); };
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
     float l = run.l[n];
@@ -349,9 +375,9 @@ __global__ __launch_bounds__(64 * kWaves, NC == 1 ? 3 : 2) void attn_decode_kern
       lds_m[wave][16 * n + c16] = run.m[n];
       lds_l[wave][16 * n + c16] = l;
     }
-    if (n > 0) __syncthreads();
+    __syncthreads();  // no wave needs its keys and values, or the sums of the block before, any more
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<v4f*>(&lds_o[wave][c16][16 * i + 4 * g]) = run.o[n][i] * run.vref;
+    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<v4f*>(sums(wave, c16) + 16 * i + 4 * g) = run.o[n][i] * run.vref;
     __syncthreads();
     const int here = min(16, cols - 16 * n);
     for (int at = threadIdx.x; at < here * (D / 4); at += 64 * kWaves) {
@@ -365,7 +391,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 1 ? 3 : 2) void attn_decode_kern
       for (int w = 0; w < kWaves; ++w) {
         const float f = __builtin_amdgcn_exp2f(lds_m[w][16 * n + col] - m);
         sum += lds_l[w][16 * n + col] * f;
-        o += *reinterpret_cast<const v4f*>(&lds_o[w][col][d]) * f;
+        o += *reinterpret_cast<const v4f*>(sums(w, col) + d) * f;
       }
       int seq, head;
       split(16 * n + col, seq, head);
@@ -393,7 +419,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
   const int64_t r = blockIdx.x;
   const int slots = a.prefix_parts + a.own_parts;
   const int b = (int)(r / (a.kv_heads * a.group));
-  const int64_t len = min((int64_t)max(a.lens[b], 0), (int64_t)a.width << a.page_shift);
+  const int64_t len = min((int64_t)min(max(a.lens[b], 0), kMostKeys), (int64_t)a.width << a.page_shift);
   // parts that ran: all of the prefix's, and those of the sequence that begin before its end (the first always)
   const int used = a.prefix_parts +
                    (int)min((int64_t)a.own_parts, max((int64_t)1, (len + a.part_keys - 1) / a.part_keys));
@@ -473,7 +499,8 @@ moe_status_t launch_decode(const DecodeArgs& a, const DecodePlan& p, hipStream_t
 using namespace moe;
 
 extern "C" size_t moe_attn_decode_workspace(moe_attn_dims_t d, int32_t B, int32_t max_len, int32_t prefix_len) {
-  if (check_attn_dims(d, "moe_attn_decode_workspace") != MOE_OK || B < 1 || B > 65535 || max_len < 0 || prefix_len < 0)
+  if (check_attn_dims(d, "moe_attn_decode_workspace") != MOE_OK || B < 1 || B > 65535 || max_len < 0 || prefix_len < 0 ||
+      max_len > kMostKeys || prefix_len > kMostKeys)
     return 0;
   const DecodePlan p = plan_decode(d, B, max_len, prefix_len);
   return part_bytes(p, d.head_dim) + part_bytes(p, 2);
@@ -487,8 +514,10 @@ extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint
   moe_status_t st = check_attn_dims(d, "moe_attn_decode");
   if (st != MOE_OK) return st;
   if ((st = check_cache(cache, "moe_attn_decode")) != MOE_OK) return st;
-  if (B < 0 || B > 65535 || table_width < 0 || max_len < 0 || prefix_len < 0)
-    return fail(MOE_ERR_INVALID_ARG, "moe_attn_decode: B=%d (at most 65535) table_width=%d max_len=%d prefix_len=%d", B,
+  if (B < 0 || B > 65535 || table_width < 0 || max_len < 0 || prefix_len < 0 || max_len > kMostKeys ||
+      prefix_len > kMostKeys)
+    return fail(MOE_ERR_INVALID_ARG,
+                "moe_attn_decode: B=%d (at most 65535) table_width=%d max_len=%d prefix_len=%d (at most 2^30)", B,
                 table_width, max_len, prefix_len);
   if (!(scale > 0.0f) || !isfinite(scale * kLog2e)) return fail(MOE_ERR_INVALID_ARG, "moe_attn_decode: scale=%g", scale);
   if (B == 0) return MOE_OK;
