@@ -13,15 +13,22 @@
 //                 (ds_read_b64_tr_b8) in the order of keys that the scores have
 // Scales stay fp32: a key's multiplies its score, a value's its numerator.  The
 // numerators are rounded once for the product, to f16: a code is exact in f16 as
-// it is in bf16, and f16 has three bits more.  Its range is kept by dividing the
-// values' scales by their running maximum (`vref`), which rescales the
-// accumulator as the running maximum of the scores does; what underflows is
-// below 2^-25 of the largest term.
+// it is in bf16, and f16 has three bits more.  Its range is kept by what the
+// scores are taken against: the running maximum of a step's largest score plus the
+// logarithm of its largest value scale (numerators, sums and results share that
+// reference, so it cancels).  It grows only when it would by more than 2^8, so a
+// product is at most 2^8, and what underflows is below 2^-24 of the largest.
 //
 // Bound by memory: head_dim + 4 bytes per key, value and head against 4 * G *
-// head_dim flops.  One long context has few rows, so keys are cut into parts, one
-// workgroup each, whose waves take every fourth step of 32 keys; a second launch
-// joins the parts.
+// head_dim flops.
+//
+// A head's work is a line of steps of 128 keys (32 for each wave of a
+// workgroup): the prefix's for every block of columns, then the sequences' one
+// behind the other.  The workgroups that the card holds at once take equal pieces
+// of the heads' lines, so that one long context and a ragged batch both fill it
+// evenly; where a piece or a sequence ends, a segment ends, whose sums a second
+// launch joins.  Short contexts without a prefix take one workgroup a sequence
+// and head, and no second launch.
 #include <math.h>
 
 #include <algorithm>
@@ -38,18 +45,19 @@ struct DecodeArgs {
   moe_kv_cache_t cache;
   const int32_t *pages, *lens, *prefix_pages;
   uint16_t* out;
-  float* part_o;   // [B * q_heads][slots][D]: a part's sums, not divided
-  float* part_ml;  // [B * q_heads][slots][2]: its running maximum and sum
+  float* seg_o;     // [segments][columns][D]: a segment's sums, not divided
+  float2* seg_ml;   // [segments][columns]: its running maxima and sums
+  uint32_t* starts;  // [B + 1]: a sequence's first step in a head's line; [B]: the line's length
   int32_t* status;
   int B, width, prefix_len, kv_heads, group, page_shift;
-  int part_keys, prefix_parts, own_parts;  // slots: the prefix's parts, then a sequence's own
-  int prefix_blocks, own_blocks;           // column blocks of all sequences' and of one's queries
-  float c;                                 // scale * log2(e)
+  int prefix_blocks, own_blocks;  // column blocks of all sequences' and of one's queries
+  int pieces;                     // that a head's line is cut into
+  float c;                        // scale * log2(e)
 };
 
 constexpr int kKeys = 32;  // keys per step of a wave
 constexpr int kWaves = 4;
-constexpr int kStride = kKeys * kWaves;
+constexpr int kStride = kKeys * kWaves;  // keys per step of a workgroup
 constexpr int kMostKeys = 1 << 30;  // of a sequence: key indices and the steps behind them stay in 32 bits
 
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
@@ -71,9 +79,8 @@ __device__ __forceinline__ v8h e4m3x8_to_f16(uint32_t lo, uint32_t hi) {
 // lane % 16 of each block.
 template <int D, int NC>
 struct Running {
-  v4f o[NC][D / 16];     // O^T / vref: rows 16 i + 4 (lane / 16) + 0..3
-  float m[NC], l[NC];    // l: this lane's keys only, summed over the lane groups at the end
-  float vref;
+  v4f o[NC][D / 16];   // O^T: rows 16 i + 4 (lane / 16) + 0..3
+  float m[NC], l[NC];  // the reference; l: this lane's keys only, summed over the lane groups at the end
 };
 
 // The maximum over the four lanes that hold one query (lane, lane ^ 16, ^ 32,
@@ -189,60 +196,75 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
       }
     }
   }
-  float ks[2][4], vs[2][4];
-  float vtop = run.vref;
+  v4f ks[2], vs[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    const v4f kk = *reinterpret_cast<const v4f*>(lds + Staged<D>::kScale + 4 * (16 * u + 4 * g));
-    const v4f vv = *reinterpret_cast<const v4f*>(lds + Staged<D>::kScale + 4 * (32 + 16 * u + 4 * g));
+    ks[u] = *reinterpret_cast<const v4f*>(lds + Staged<D>::kScale + 4 * (16 * u + 4 * g));
+    vs[u] = *reinterpret_cast<const v4f*>(lds + Staged<D>::kScale + 4 * (32 + 16 * u + 4 * g));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool there = t0 + 16 * u + 4 * g + i < p.len;
-      ks[u][i] = there ? kk[i] * a.c : -1.0f;  // scales are not negative
-      vs[u][i] = there ? vv[i] : 0.0f;
-      vtop = fmaxf(vtop, vs[u][i]);
-    }
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[n][u][i] *= ks[u][i] * a.c;
   }
-  vtop = quad_max(vtop);
-  const float inv = 1.0f / vtop, faded = run.vref * inv;
-  run.vref = vtop;
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) vs[u][i] *= inv;
-
-  union {
-    v8h v;
-    v2h x[4];
-  } pf[NC];
-  float fade[NC];
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    float top = -INFINITY;
+  if (t0 + kKeys > p.len) {  // a slot behind the end may hold any bits
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[n][u][i] = ks[u][i] >= 0.0f ? s[n][u][i] * ks[u][i] : -INFINITY;
-        top = fmaxf(top, s[n][u][i]);
+        const bool there = t0 + 16 * u + 4 * g + i < p.len;
+        vs[u][i] = there ? vs[u][i] : 0.0f;
+#pragma unroll
+        for (int n = 0; n < NC; ++n) s[n][u][i] = there ? s[n][u][i] : -INFINITY;
       }
-    const float m = fmaxf(run.m[n], quad_max(top)), alpha = __builtin_amdgcn_exp2f(run.m[n] - m);
-    run.m[n] = m;
+  }
+  float vtop = 0x1p-100f, top[NC];  // (values that are all below 2^-100 lose digits)
+#pragma unroll
+  for (int n = 0; n < NC; ++n) top[n] = s[n][0][0];
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      vtop = fmaxf(vtop, vs[u][i]);
+#pragma unroll
+      for (int n = 0; n < NC; ++n) top[n] = fmaxf(top[n], s[n][u][i]);
+    }
+  const float vlog = __builtin_amdgcn_logf(quad_max(vtop));
+  bool grows = false;
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    top[n] = quad_max(top[n]) + vlog;
+    grows |= top[n] > run.m[n] + 8.0f;
+  }
+  if (__any(grows)) {
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      const float m = fmaxf(run.m[n], top[n]), alpha = __builtin_amdgcn_exp2f(run.m[n] - m);
+      run.m[n] = m;
+      run.l[n] *= alpha;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) run.o[n][i] *= alpha;
+    }
+  }
+  union {
+    v8h v;
+    v2h x[4];
+  } pf[NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
     float sum = 0.0f;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float e[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(s[n][u][i] - m);
+        e[i] = __builtin_amdgcn_exp2f(s[n][u][i] - run.m[n]);
         sum += e[i];
         e[i] *= vs[u][i];
       }
       pf[n].x[2 * u] = v2h{(_Float16)e[0], (_Float16)e[1]};
       pf[n].x[2 * u + 1] = v2h{(_Float16)e[2], (_Float16)e[3]};
     }
-    run.l[n] = run.l[n] * alpha + sum;
-    fade[n] = alpha * faded;
+    run.l[n] += sum;
   }
   // lane j of a 16-lane group gives the address of row j / 2, half j % 2 of an 8 x 16 block and gets column j:
   // rows 0..3 are keys 4 g + 0..3, rows 4..7 keys 16 + 4 g + 0..3
@@ -253,19 +275,63 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
         (__attribute__((address_space(3))) v2i*)(lds + Staged<D>::value(row, i) + 8 * (c16 & 1)));
     const v8h vf = e4m3x8_to_f16(y[0], y[1]);
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      run.o[n][i] *= fade[n];
-      run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n].v, run.o[n][i], 0, 0, 0);
-    }
+    for (int n = 0; n < NC; ++n) run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n].v, run.o[n][i], 0, 0, 0);
   }
 }
 
-// Workgroups: the prefix's parts (part, column block, head), then the sequences'
-// own (part, column block, sequence, head); heads fastest, so that workgroups
-// that share keys have numbers equal mod 8 (one XCD's L2) where kv_heads is a
-// multiple of 8.
-template <int D, int NC>
-__global__ __launch_bounds__(64 * kWaves, NC == 1 ? 3 : 2) void attn_decode_kernel(DecodeArgs a) {
+// A head's line of steps, and its pieces: prefix_blocks times the prefix's steps,
+// own_blocks times all sequences'.  (The host checks that it has less than 2^31
+// steps.)  A pair is one of its runs of keys for one block of columns: the
+// prefix's blocks, then (block, sequence).  Pieces and pairs end one at a time, so
+// that segments are numbered by the sum of their piece's and their pair's number.
+struct Line {
+  uint32_t prefix_steps, prefix_total, own_total;
+  uint32_t base, more;  // a piece has base steps, the first `more` have one more
+  int64_t segments;     // of a head, at most
+  __device__ __forceinline__ Line(const DecodeArgs& a, uint32_t own) {
+    prefix_steps = (a.prefix_len + kStride - 1) / kStride;
+    prefix_total = prefix_steps * a.prefix_blocks;
+    own_total = own;
+    const uint32_t all = prefix_total + own * a.own_blocks;
+    base = all / (uint32_t)a.pieces;
+    more = all - base * a.pieces;
+    segments = (int64_t)a.pieces + a.prefix_blocks + (int64_t)a.own_blocks * a.B;
+  }
+  __device__ __forceinline__ uint32_t begin(uint32_t piece) const { return piece * base + min(piece, more); }
+  __device__ __forceinline__ uint32_t piece_of(uint32_t step) const {
+    const uint32_t longer = more * (base + 1);
+    return step < longer ? step / (base + 1) : more + (step - longer) / max(base, 1u);
+  }
+};
+
+// A sequence's own keys, cut to its page table row, and its steps.
+__device__ __forceinline__ int keys_of(const DecodeArgs& a, int b, bool& bad) {
+  const int len = a.lens[b];
+  const int64_t most = min((int64_t)a.width << a.page_shift, (int64_t)kMostKeys);
+  bad = len < 0 || len > most;
+  return len < 0 ? 0 : (int)min((int64_t)len, most);
+}
+__device__ __forceinline__ int steps_of(int keys) { return (keys + kStride - 1) / kStride; }
+
+// 64 sequences' steps, a lane each, and their sum up to each.
+struct Chunk {
+  int base = -1, len, n, incl;
+  __device__ __forceinline__ void load(const DecodeArgs& a, int from, bool report) {
+    if (from == base) return;
+    base = from;
+    const int b = from + (threadIdx.x & 63);
+    bool bad = false;
+    len = b < a.B ? keys_of(a, b, bad) : 0;
+    if (report && bad && a.status) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
+    n = steps_of(len);
+    incl = wave_scan(n);
+  }
+};
+
+// kWhole: a workgroup takes all keys of one (sequence, head, block of columns)
+// and writes its output; otherwise a piece of the line.
+template <int D, int NC, bool kWhole>
+__global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs a) {
   constexpr int kCols = 16 * NC;
   // the waves' keys and values; behind the last step their sums
   constexpr int kWaveBytes = Staged<D>::kBytes > 16 * (D + 4) * 4 ? Staged<D>::kBytes : 16 * (D + 4) * 4;
@@ -274,178 +340,273 @@ __global__ __launch_bounds__(64 * kWaves, NC == 1 ? 3 : 2) void attn_decode_kern
   const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  int item = blockIdx.x;
-  const int n_prefix = a.prefix_parts * a.prefix_blocks * a.kv_heads;
-  const bool shared = item < n_prefix;
-  if (!shared) item -= n_prefix;
   Part p;
-  p.kvh = item % a.kv_heads;
-  item /= a.kv_heads;
-  int b = 0, slot;
-  if (!shared) {
-    b = item % a.B;
-    item /= a.B;
-  }
-  const int blocks = shared ? a.prefix_blocks : a.own_blocks;
-  const int col0 = item % blocks * kCols, part = item / blocks;
-  const int cols = min(kCols, (shared ? a.B * a.group : a.group) - col0);
-  if (shared) {
-    p.pages = a.prefix_pages;
-    p.width = ((a.prefix_len - 1) >> a.page_shift) + 1;
-    p.len = a.prefix_len;
-    slot = part;
-  } else {
-    p.pages = a.pages + (int64_t)b * a.width;
-    p.width = a.width;
-    slot = a.prefix_parts + part;
-  }
-  const int64_t begin = (int64_t)part * a.part_keys;
-  if (begin >= min((int64_t)p.width << a.page_shift, (int64_t)kMostKeys) && part > 0) return;  // as below, whatever the length
-  // the first step's pages are on their way while the length is
-  Pages first = {};
-  if (p.width > 0) first = pages_of(a, p, (int)begin + wave * kKeys);
-  bool bad_len = false;
-  if (!shared) {
-    p.len = a.lens[b];
-    const int64_t most = min((int64_t)a.width << a.page_shift, (int64_t)kMostKeys);
-    bad_len = p.len < 0 || p.len > most;
-    p.len = p.len < 0 ? 0 : (int)min((int64_t)p.len, most);
-  }
-  const bool last_part = part == (shared ? a.prefix_parts : a.own_parts) - 1;
-  if (bad_len && a.status && part == 0 && threadIdx.x == 0) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
-  if (begin >= p.len && part > 0) return;  // the join looks at lens, too
-  p.begin = (int)begin;
-  p.end = last_part ? p.len : (int)min((int64_t)p.len, begin + a.part_keys);
+  bool shared = false;
+  int b = 0, col0 = 0, cols = 0;
+  int64_t segment = 0;
+  // The segment's keys by p, the sums to `segment` or (kWhole) the output.
+  const auto run_segment = [&](const Pages& first) __attribute__((always_inline)) {
+    // column n of block col0: query head (col % G) of the group, of sequence col / G in the prefix
+    const auto split = [&](int col, int& seq, int& head) {
+      seq = shared ? (col0 + col) / a.group : b;
+      head = p.kvh * a.group + (shared ? col0 + col - seq * a.group : col0 + col);
+    };
+    Running<D, NC> run;
+  #pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      run.m[n] = kNoScore;
+      run.l[n] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) run.o[n][i] = v4f{};
+    }
+    int t = p.begin + wave * kKeys;
+    if (t < p.end) {
+      v8bf qf[NC][D / 32];
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        int seq, head;
+        split(min(16 * n + c16, cols - 1), seq, head);
+        const uint16_t* qrow = a.q + seq * a.q_stride + head * D + 16 * g;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          qf[n][2 * i] = *reinterpret_cast<const v8bf*>(qrow + 64 * i);
+          qf[n][2 * i + 1] = *reinterpret_cast<const v8bf*>(qrow + 64 * i + 8);
+        }
+      }
+      bool bad = false;
+      Tile<D> x;
+      Pages ahead = first;
+      const auto load = [&](int at) __attribute__((always_inline)) {
+        if (shared || a.own_blocks > 1)
+          load_tile<D, false>(a, p, at, ahead, bad, x);
+        else
+          load_tile<D, true>(a, p, at, ahead, bad, x);
+        ahead = pages_of(a, p, at + kStride);
+      };
+      load(t);
+      for (; t < p.end; t += kStride)
+        use_tile<D, NC>(a, p, t, x, qf, lds[wave], run, [&]() __attribute__((always_inline)) {
+          if (t + kStride < p.end) load(t + kStride);
+        });
+      if (bad && a.status && lane == 0) atomicOr(a.status, MOE_DEV_BAD_PAGE);
+    }
 
-  // column n of block col0: query head (col % G) of the group, of sequence col / G in the prefix
-  const auto split = [&](int col, int& seq, int& head) {
-    seq = shared ? (col0 + col) / a.group : b;
-    head = p.kvh * a.group + (shared ? col0 + col - seq * a.group : col0 + col);
-  };
-  Running<D, NC> run;
-  run.vref = 0x1p-126f;  // 1 / vref stays finite
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    run.m[n] = kNoScore;
-    run.l[n] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) run.o[n][i] = v4f{};
-  }
-  int t = p.begin + wave * kKeys;
-  if (t < p.end) {
-    v8bf qf[NC][D / 32];
+    // the waves' sums joined, one block of 16 columns at a time
+    const auto sums = [&](int w, int col) { return reinterpret_cast<float*>(lds[w]) + col * (D + 4); };
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-      int seq, head;
-      split(min(16 * n + c16, cols - 1), seq, head);
-      const uint16_t* qrow = a.q + seq * a.q_stride + head * D + 16 * g;
+      float l = run.l[n];
+      l += __shfl_xor(l, 16, 64);
+      l += __shfl_xor(l, 32, 64);
+      if (g == 0) {
+        lds_m[wave][16 * n + c16] = run.m[n];
+        lds_l[wave][16 * n + c16] = l;
+      }
+      __syncthreads();  // no wave needs its keys and values, or the sums of the block before, any more
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        qf[n][2 * i] = *reinterpret_cast<const v8bf*>(qrow + 64 * i);
-        qf[n][2 * i + 1] = *reinterpret_cast<const v8bf*>(qrow + 64 * i + 8);
+      for (int i = 0; i < D / 16; ++i) *reinterpret_cast<v4f*>(sums(wave, c16) + 16 * i + 4 * g) = run.o[n][i];
+      __syncthreads();
+      const int here = min(16, cols - 16 * n);
+      for (int at = threadIdx.x; at < here * (D / 4); at += 64 * kWaves) {
+        const int col = at / (D / 4), d = at % (D / 4) * 4;
+        float m = kNoScore;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, lds_m[w][16 * n + col]);
+        float sum = 0.0f;
+        v4f o = {};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float f = __builtin_amdgcn_exp2f(lds_m[w][16 * n + col] - m);
+          sum += lds_l[w][16 * n + col] * f;
+          o += *reinterpret_cast<const v4f*>(sums(w, col) + d) * f;
+        }
+        if (kWhole) {
+          int seq, head;
+          split(16 * n + col, seq, head);
+          const int64_t r = (int64_t)seq * (a.kv_heads * a.group) + head;
+          const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+          *reinterpret_cast<uint2*>(a.out + r * D + d) =
+              make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+        } else {
+          const int64_t place = segment * kCols + 16 * n + col;
+          *reinterpret_cast<v4f*>(a.seg_o + place * D + d) = o;
+          if (d == 0) a.seg_ml[place] = make_float2(m, sum);
+        }
       }
     }
-    bool bad = false;
-    Tile<D> x;
-    Pages ahead = first;
-    const auto load = [&](int at) __attribute__((always_inline)) {
-      if (shared || a.own_blocks > 1)
-        load_tile<D, false>(a, p, at, ahead, bad, x);
-      else
-        load_tile<D, true>(a, p, at, ahead, bad, x);
-      ahead = pages_of(a, p, at + kStride);
-    };
-    load(t);
-    for (; t < p.end; t += kStride)
-      use_tile<D, NC>(a, p, t, x, qf, lds[wave], run, [&]() __attribute__((always_inline)) {
-        if (t + kStride < p.end) load(t + kStride);
-      });
-    if (bad && a.status && lane == 0) atomicOr(a.status, MOE_DEV_BAD_PAGE);
+  };
+
+  if (kWhole) {
+    int item = blockIdx.x;
+    p.kvh = item % a.kv_heads;
+    item /= a.kv_heads;
+    b = item % a.B;
+    col0 = item / a.B * kCols;
+    cols = min(kCols, a.group - col0);
+    p.pages = a.pages + (int64_t)b * a.width;
+    p.width = a.width;
+    // the first step's pages are on their way while the length is
+    Pages first = {};
+    if (a.width > 0) first = pages_of(a, p, wave * kKeys);
+    bool bad;
+    p.len = keys_of(a, b, bad);
+    if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
+    p.begin = 0;
+    p.end = p.len;
+    run_segment(first);
+    return;
   }
 
-  // the waves' sums joined, one block of 16 columns at a time
-  const bool whole = a.prefix_parts + a.own_parts == 1;
-  const auto sums = [&](int w, int col) { return reinterpret_cast<float*>(lds[w]) + col * (D + 4); };
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    float l = run.l[n];
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    if (g == 0) {
-      lds_m[wave][16 * n + c16] = run.m[n];
-      lds_l[wave][16 * n + c16] = l;
+  // Heads fastest: the heads of a page are read at one time, and workgroups that share keys (the prefix's blocks of
+  // columns) have numbers equal mod 8 (one XCD's L2) where kv_heads is a multiple of 8.
+  p.kvh = blockIdx.x % (uint32_t)a.kv_heads;
+  const uint32_t piece = blockIdx.x / (uint32_t)a.kv_heads;
+  // The first wave finds the segments of this workgroup's piece, one at a time; the others take what it found, so that
+  // all leave together whatever the lengths in memory do.
+  __shared__ struct {
+    int more, shared, col0, cols, b, len, begin, end;
+    uint32_t pair;
+  } found;
+  Chunk chunk;
+  uint32_t own = 0;
+  if (wave == 0) {
+    // the line's length; the first workgroup leaves every sequence's place in it to the join
+    for (int from = 0; from < a.B; from += 64) {
+      chunk.load(a, from, blockIdx.x == 0);
+      if (blockIdx.x == 0 && from + lane < a.B) a.starts[from + lane] = own + chunk.incl - chunk.n;
+      own += __builtin_amdgcn_readlane(chunk.incl, 63);
     }
-    __syncthreads();  // no wave needs its keys and values, or the sums of the block before, any more
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<v4f*>(sums(wave, c16) + 16 * i + 4 * g) = run.o[n][i] * run.vref;
-    __syncthreads();
-    const int here = min(16, cols - 16 * n);
-    for (int at = threadIdx.x; at < here * (D / 4); at += 64 * kWaves) {
-      const int col = at / (D / 4), d = at % (D / 4) * 4;
-      float m = kNoScore;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, lds_m[w][16 * n + col]);
-      float sum = 0.0f;
-      v4f o = {};
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(lds_m[w][16 * n + col] - m);
-        sum += lds_l[w][16 * n + col] * f;
-        o += *reinterpret_cast<const v4f*>(sums(w, col) + d) * f;
-      }
-      int seq, head;
-      split(16 * n + col, seq, head);
-      const int64_t r = (int64_t)seq * (a.kv_heads * a.group) + head;
-      if (whole) {
-        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-        *reinterpret_cast<uint2*>(a.out + r * D + d) =
-            make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+    if (blockIdx.x == 0 && lane == 0) a.starts[a.B] = own;
+  }
+  const Line line(a, own);
+  const uint32_t end = line.begin(piece + 1);
+  uint32_t at = line.begin(piece), block_at = ~0u, before = 0;  // chunk is of this block's sequences, steps in front of it
+  while (true) {
+    if (wave == 0) {
+      uint32_t pair = 0, skip = 0, steps = 0;  // the pair, its steps in front of `at`, and those that are left
+      uint32_t block = 0;
+      int seq = 0, len = 0;
+      const bool front = at < line.prefix_total;
+      if (at >= end) {
+      } else if (front) {
+        pair = block = at / line.prefix_steps;
+        skip = at - block * line.prefix_steps;
+        steps = line.prefix_steps - skip;
+        len = a.prefix_len;
       } else {
-        const int64_t at_part = r * (a.prefix_parts + a.own_parts) + slot;
-        *reinterpret_cast<v4f*>(a.part_o + at_part * D + d) = o;
-        if (d == 0) *reinterpret_cast<float2*>(a.part_ml + at_part * 2) = make_float2(m, sum);
+        const uint32_t own_at = at - line.prefix_total;
+        block = a.own_blocks == 1 ? 0 : own_at / line.own_total;
+        const uint32_t in_block = own_at - block * line.own_total;
+        int from = block == block_at ? chunk.base : 0;
+        if (block != block_at) before = 0;
+        block_at = block;
+        for (; from < a.B; from += 64) {
+          chunk.load(a, from, false);
+          const uint64_t past = __ballot(before + chunk.incl > in_block);
+          if (past) {
+            const int w = __ffsll((unsigned long long)past) - 1, n = __builtin_amdgcn_readlane(chunk.n, w);
+            seq = from + w;
+            skip = in_block - (before + __builtin_amdgcn_readlane(chunk.incl, w) - n);
+            steps = n - skip;
+            len = __builtin_amdgcn_readlane(chunk.len, w);
+            break;
+          }
+          before += __builtin_amdgcn_readlane(chunk.incl, 63);
+        }
+        pair = a.prefix_blocks + block * a.B + seq;
       }
+      const uint32_t taken = min(steps, end - at);
+      if (lane == 0) {
+        found.more = taken > 0;
+        found.shared = front;
+        found.col0 = block * kCols;
+        found.cols = min(kCols, (front ? a.B * a.group : a.group) - (int)block * kCols);
+        found.b = seq;
+        found.len = len;
+        found.begin = (int)(skip * kStride);
+        found.end = min(len, (int)((skip + taken) * kStride));
+        found.pair = pair;
+      }
+      at += taken;
     }
+    __syncthreads();  // (and the sums' places may take the next segment's keys)
+    if (!found.more) return;
+    shared = __builtin_amdgcn_readfirstlane(found.shared);
+    col0 = __builtin_amdgcn_readfirstlane(found.col0);
+    cols = __builtin_amdgcn_readfirstlane(found.cols);
+    b = __builtin_amdgcn_readfirstlane(found.b);
+    p.len = __builtin_amdgcn_readfirstlane(found.len);
+    p.begin = __builtin_amdgcn_readfirstlane(found.begin);
+    p.end = __builtin_amdgcn_readfirstlane(found.end);
+    segment = p.kvh * line.segments + piece + (uint32_t)__builtin_amdgcn_readfirstlane(found.pair);
+    p.pages = shared ? a.prefix_pages : a.pages + (int64_t)b * a.width;
+    p.width = shared ? ((a.prefix_len - 1) >> a.page_shift) + 1 : a.width;
+    run_segment(pages_of(a, p, p.begin + wave * kKeys));
   }
 }
 
-// One workgroup per output row: its parts' sums, weighed by their maxima.  Eight
-// (D = 128) or sixteen parts at a time, 16 bytes a lane.
-template <int D>
+// A row's segments, weighed by their maxima: those of the prefix's pair that has
+// the row among its columns, then those of the row's own.  D / 4 lanes with 16
+// bytes each take a segment; kAtOnce of them work on one row.
+template <int D, int NC, int kAtOnce>
 __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
-  constexpr int kLanes = D / 4, kAtOnce = 256 / kLanes;
+  constexpr int kCols = 16 * NC, kLanes = D / 4, kRows = 256 / (kLanes * kAtOnce);
   __shared__ __attribute__((aligned(16))) float lds_o[kAtOnce][D];
-  __shared__ float lds_l[kAtOnce];
-  const int64_t r = blockIdx.x;
-  const int slots = a.prefix_parts + a.own_parts;
-  const int b = (int)(r / (a.kv_heads * a.group));
-  const int64_t len = min((int64_t)min(max(a.lens[b], 0), kMostKeys), (int64_t)a.width << a.page_shift);
-  // parts that ran: all of the prefix's, and those of the sequence that begin before its end (the first always)
-  const int used = a.prefix_parts +
-                   (int)min((int64_t)a.own_parts, max((int64_t)1, (len + a.part_keys - 1) / a.part_keys));
-  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + r * slots;
-  float m = kNoScore;
-  for (int s = threadIdx.x & 63; s < used; s += 64) m = fmaxf(m, ml[s].x);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-  const int sub = threadIdx.x % kLanes, first = threadIdx.x / kLanes;
+  __shared__ float lds_m[kAtOnce], lds_l[kAtOnce];
+  const int sub = threadIdx.x % kLanes, nth = threadIdx.x / kLanes % kAtOnce;
+  const int heads = a.kv_heads * a.group;
+  const int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / (kLanes * kAtOnce);
+  if (r >= (int64_t)a.B * heads) return;  // (kAtOnce > 1: one row a workgroup)
+  const int b = (int)((uint32_t)r / (uint32_t)heads), head = (int)(r - (int64_t)b * heads);
+  const int kvh = head / a.group, col = head - kvh * a.group;
+  const Line line(a, a.starts[a.B]);
+  float m = kNoScore, l = 0.0f;
   v4f o = {};
-  float l = 0.0f;
-#pragma unroll 4
-  for (int s = first; s < used; s += kAtOnce) {
-    const float2 x = ml[s];
-    const float f = __builtin_amdgcn_exp2f(x.x - m);
-    l += x.y * f;
-    o += *reinterpret_cast<const v4f*>(a.part_o + (r * slots + s) * D + 4 * sub) * f;
+  const auto take = [&](uint32_t pair, uint32_t first, uint32_t last, int column) __attribute__((always_inline)) {
+    const uint32_t w0 = line.piece_of(first), w1 = line.piece_of(last);
+    const int64_t place0 = (kvh * line.segments + pair) * kCols + column;
+#pragma unroll 2
+    for (uint32_t w = w0 + nth; w <= w1; w += kAtOnce) {
+      const int64_t place = place0 + (int64_t)w * kCols;
+      const float2 ml = a.seg_ml[place];
+      const v4f x = *reinterpret_cast<const v4f*>(a.seg_o + place * D + 4 * sub);
+      const float top = fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - top), e = __builtin_amdgcn_exp2f(ml.x - top);
+      m = top;
+      l = l * f + ml.y * e;
+      o = o * f + x * e;
+    }
+  };
+  if (a.prefix_len > 0) {
+    const int pcol = b * a.group + col;
+    const uint32_t block = pcol / kCols;
+    take(block, block * line.prefix_steps, (block + 1) * line.prefix_steps - 1, pcol % kCols);
   }
-  *reinterpret_cast<v4f*>(&lds_o[first][4 * sub]) = o;
-  if (sub == 0) lds_l[first] = l;
-  __syncthreads();
-  if (first > 0) return;
+  bool bad;
+  const int steps = steps_of(keys_of(a, b, bad));
+  if (steps > 0) {
+    const uint32_t block = col / kCols, first = line.prefix_total + block * line.own_total + a.starts[b];
+    take(a.prefix_blocks + block * a.B + b, first, first + steps - 1, col % kCols);
+  }
+  if (kAtOnce > 1) {
+    *reinterpret_cast<v4f*>(&lds_o[nth][4 * sub]) = o;
+    if (sub == 0) {
+      lds_m[nth] = m;
+      lds_l[nth] = l;
+    }
+    __syncthreads();
+    if (nth > 0) return;
+    float top = m;
 #pragma unroll
-  for (int w = 1; w < kAtOnce; ++w) {
-    o += *reinterpret_cast<const v4f*>(&lds_o[w][4 * sub]);
-    l += lds_l[w];
+    for (int w = 1; w < kAtOnce; ++w) top = fmaxf(top, lds_m[w]);
+    const float f = __builtin_amdgcn_exp2f(m - top);
+    o *= f;
+    l *= f;
+#pragma unroll
+    for (int w = 1; w < kAtOnce; ++w) {
+      const float e = __builtin_amdgcn_exp2f(lds_m[w] - top);
+      o += *reinterpret_cast<const v4f*>(&lds_o[w][4 * sub]) * e;
+      l += lds_l[w] * e;
+    }
   }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
   *reinterpret_cast<uint2*>(a.out + r * D + 4 * sub) =
@@ -453,42 +614,61 @@ __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
 }
 
 struct DecodePlan {
-  int part_keys, prefix_parts, own_parts, prefix_blocks, own_blocks, col_blocks;
-  int64_t slots_of_rows;  // B * q_heads * slots where there is more than one slot
+  bool whole;
+  int col_blocks;  // of 16 columns in a workgroup
+  int own_blocks, prefix_blocks, pieces;
+  int64_t workgroups;
+  size_t o_bytes, ml_bytes, start_bytes;
 };
+
+// Steps up to which a sequence's keys stay with one workgroup where there is no
+// prefix: a second launch and its trip through memory take about as long as 5
+// steps.
+constexpr int kWholeSteps = 5;
 
 DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int32_t prefix_len) {
   DecodePlan p{};
   const int group = d.q_heads / d.kv_heads;
   p.col_blocks = group > 16 || (prefix_len > 0 && (int64_t)B * group > 16) ? 2 : 1;
-  p.own_blocks = (group + 16 * p.col_blocks - 1) / (16 * p.col_blocks);
-  p.prefix_blocks = (int)(((int64_t)B * group + 16 * p.col_blocks - 1) / (16 * p.col_blocks));
-  const int64_t keys = ((int64_t)B * p.own_blocks * max_len + (int64_t)p.prefix_blocks * prefix_len) * d.kv_heads;
-  const int64_t even = (keys + 511) / 512;
-  p.part_keys = (int)std::min<int64_t>(1024, std::max<int64_t>(256, (even + kStride - 1) / kStride * kStride));
-  p.own_parts = std::max(1, (int)(((int64_t)max_len + p.part_keys - 1) / p.part_keys));
-  p.prefix_parts = (int)(((int64_t)prefix_len + p.part_keys - 1) / p.part_keys);
-  const int slots = p.own_parts + p.prefix_parts;
-  p.slots_of_rows = slots > 1 ? (int64_t)B * d.q_heads * slots : 0;
+  const int cols = 16 * p.col_blocks;
+  p.own_blocks = (group + cols - 1) / cols;
+  p.prefix_blocks = prefix_len > 0 ? (int)(((int64_t)B * group + cols - 1) / cols) : 0;
+  const int64_t own_pairs = (int64_t)p.own_blocks * B;
+  const int64_t own_steps = ((int64_t)max_len + kStride - 1) / kStride;
+  p.whole = prefix_len == 0 && own_steps <= kWholeSteps;
+  p.workgroups = own_pairs * d.kv_heads;
+  if (!p.whole) {
+    const int64_t steps = own_pairs * own_steps + p.prefix_blocks * (((int64_t)prefix_len + kStride - 1) / kStride);
+    // Two workgroups a CU (64 ragged contexts: 77 us with 512 workgroups, 81 with 768, 84 with 1536; one context of 65536:
+    // 27, 29 and 31 us, and a longer join).
+    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>(512 / d.kv_heads, steps));
+    p.workgroups = (int64_t)p.pieces * d.kv_heads;
+    const size_t places = (size_t)d.kv_heads * (p.pieces + p.prefix_blocks + own_pairs) * cols;
+    p.o_bytes = (places * d.head_dim * sizeof(float) + 255) & ~(size_t)255;
+    p.ml_bytes = (places * sizeof(float2) + 255) & ~(size_t)255;
+    p.start_bytes = ((size_t)(B + 1) * sizeof(uint32_t) + 255) & ~(size_t)255;
+  }
   return p;
 }
 
-size_t part_bytes(const DecodePlan& p, int width) {
-  return ((size_t)p.slots_of_rows * width * sizeof(float) + 255) & ~(size_t)255;
-}
-
-template <int D>
+template <int D, int NC>
 moe_status_t launch_decode(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream) {
-  const int64_t items = ((int64_t)p.prefix_parts * p.prefix_blocks + (int64_t)p.own_parts * p.own_blocks * a.B) * a.kv_heads;
+  constexpr int kAtOnce = 256 / (D / 4);
   const int64_t rows = (int64_t)a.B * a.kv_heads * a.group;
-  if (items * 64 * kWaves >= (int64_t)1 << 32 || rows * 256 >= (int64_t)1 << 32)
-    return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_decode: %lld parts", (long long)items);
-  if (p.col_blocks == 1)
-    MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, 1>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
+  if (std::max(p.workgroups, rows) * 64 * kWaves >= (int64_t)1 << 32)
+    return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_decode: %lld rows", (long long)rows);
+  const dim3 grid((unsigned)p.workgroups);
+  if (p.whole) {
+    MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, NC, true>), grid, dim3(64 * kWaves), 0, stream, a);
+    return check_launch("moe_attn_decode");
+  }
+  MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, NC, false>), grid, dim3(64 * kWaves), 0, stream, a);
+  // A row has about as many segments as its pairs have pieces: a workgroup a row for many, lanes of their own for few.
+  if (p.pieces >= 4 * (p.prefix_blocks + p.own_blocks * a.B))
+    MOE_LAUNCH("attn_join", (attn_join_kernel<D, NC, kAtOnce>), dim3((unsigned)rows), dim3(256), 0, stream, a);
   else
-    MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, 2>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
-  if (p.slots_of_rows)
-    MOE_LAUNCH("attn_join", attn_join_kernel<D>, dim3((unsigned)rows), dim3(256), 0, stream, a);
+    MOE_LAUNCH("attn_join", (attn_join_kernel<D, NC, 1>), dim3((unsigned)((rows + kAtOnce - 1) / kAtOnce)), dim3(256), 0,
+               stream, a);
   return check_launch("moe_attn_decode");
 }
 
@@ -503,7 +683,7 @@ extern "C" size_t moe_attn_decode_workspace(moe_attn_dims_t d, int32_t B, int32_
       max_len > kMostKeys || prefix_len > kMostKeys)
     return 0;
   const DecodePlan p = plan_decode(d, B, max_len, prefix_len);
-  return part_bytes(p, d.head_dim) + part_bytes(p, 2);
+  return p.o_bytes + p.ml_bytes + p.start_bytes;
 }
 
 extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint16_t* q, int64_t q_stride,
@@ -525,15 +705,25 @@ extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint
   if (!page_table || !lens || !out || (prefix_len > 0 && !prefix_pages))
     return fail(MOE_ERR_INVALID_ARG, "moe_attn_decode: null pointer");
   if (!aligned(out, 16)) return fail(MOE_ERR_INVALID_ARG, "moe_attn_decode: out must be 16-byte aligned");
-  const size_t need = moe_attn_decode_workspace(d, B, max_len, prefix_len);
+  const DecodePlan p = plan_decode(d, B, max_len, prefix_len);
+  const int64_t row_keys = std::min<int64_t>((int64_t)table_width * cache.page_size, kMostKeys);
+  const int64_t prefix_steps = ((int64_t)prefix_len + kStride - 1) / kStride, row_steps = (row_keys + kStride - 1) / kStride;
+  if (p.prefix_blocks * prefix_steps + (int64_t)p.own_blocks * B * row_steps > 0x7fffffff)
+    return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_decode: %d sequences of %lld keys and a prefix of %d: over 2^31 steps", B,
+                (long long)row_keys, prefix_len);
+  const size_t need = p.o_bytes + p.ml_bytes + p.start_bytes;
   if (need && (!ws || ws_bytes < need || !aligned(ws, 256)))
     return fail(MOE_ERR_WORKSPACE, "moe_attn_decode: workspace %zu bytes, needs %zu, 256-byte aligned", ws_bytes, need);
-  const DecodePlan p = plan_decode(d, B, max_len, prefix_len);
   uint8_t* base = static_cast<uint8_t*>(ws);
-  float* part_o = p.slots_of_rows ? reinterpret_cast<float*>(base) : nullptr;
-  float* part_ml = p.slots_of_rows ? reinterpret_cast<float*>(base + part_bytes(p, d.head_dim)) : nullptr;
-  const DecodeArgs a{q, q_stride, cache, page_table, lens, prefix_pages, out, part_o, part_ml, dev_status, B, table_width,
-                     prefix_len, d.kv_heads, d.q_heads / d.kv_heads, __builtin_ctz((unsigned)cache.page_size),
-                     p.part_keys, p.prefix_parts, p.own_parts, p.prefix_blocks, p.own_blocks, scale * kLog2e};
-  return d.head_dim == 64 ? launch_decode<64>(a, p, stream) : launch_decode<128>(a, p, stream);
+  DecodeArgs a{q, q_stride, cache, page_table, lens, prefix_pages, out, nullptr, nullptr, nullptr, dev_status, B,
+               table_width, prefix_len, d.kv_heads, d.q_heads / d.kv_heads, __builtin_ctz((unsigned)cache.page_size),
+               p.prefix_blocks, p.own_blocks, p.pieces, scale * kLog2e};
+  if (need) {
+    a.seg_o = reinterpret_cast<float*>(base);
+    a.seg_ml = reinterpret_cast<float2*>(base + p.o_bytes);
+    a.starts = reinterpret_cast<uint32_t*>(base + p.o_bytes + p.ml_bytes);
+  }
+  if (d.head_dim == 64)
+    return p.col_blocks == 1 ? launch_decode<64, 1>(a, p, stream) : launch_decode<64, 2>(a, p, stream);
+  return p.col_blocks == 1 ? launch_decode<128, 1>(a, p, stream) : launch_decode<128, 2>(a, p, stream);
 }

@@ -42,18 +42,6 @@ constexpr int kKeys = 64;  // keys per tile
 constexpr int kRing = 4;   // tiles of keys, and of values, in LDS
 constexpr int kWaveRows = 32;
 
-// Inclusive sum over the wave's lanes up to this one (register moves between
-// neighbouring lanes, rows of 16 and halves).
-__device__ __forceinline__ int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);   // row_shr:2
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);   // row_shr:4
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);   // row_shr:8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
-  return x;
-}
-
 // One row tile: its place in its sequence, the sequence's rows and keys, all the
 // same for the workgroup and in scalar registers.
 struct RowTile {
