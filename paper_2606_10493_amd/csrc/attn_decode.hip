@@ -559,13 +559,14 @@ __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
   if (r >= (int64_t)a.B * heads) return;  // (kAtOnce > 1: one row a workgroup)
   const int b = (int)((uint32_t)r / (uint32_t)heads), head = (int)(r - (int64_t)b * heads);
   const int kvh = head / a.group, col = head - kvh * a.group;
+  const uint32_t start = a.starts[b], steps = a.starts[b + 1] - start;
   const Line line(a, a.starts[a.B]);
   float m = kNoScore, l = 0.0f;
   v4f o = {};
   const auto take = [&](uint32_t pair, uint32_t first, uint32_t last, int column) __attribute__((always_inline)) {
     const uint32_t w0 = line.piece_of(first), w1 = line.piece_of(last);
     const int64_t place0 = (kvh * line.segments + pair) * kCols + column;
-#pragma unroll 2
+#pragma unroll 4
     for (uint32_t w = w0 + nth; w <= w1; w += kAtOnce) {
       const int64_t place = place0 + (int64_t)w * kCols;
       const float2 ml = a.seg_ml[place];
@@ -581,10 +582,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
     const uint32_t block = pcol / kCols;
     take(block, block * line.prefix_steps, (block + 1) * line.prefix_steps - 1, pcol % kCols);
   }
-  bool bad;
-  const int steps = steps_of(keys_of(a, b, bad));
   if (steps > 0) {
-    const uint32_t block = col / kCols, first = line.prefix_total + block * line.own_total + a.starts[b];
+    const uint32_t block = col / kCols, first = line.prefix_total + block * line.own_total + start;
     take(a.prefix_blocks + block * a.B + b, first, first + steps - 1, col % kCols);
   }
   if (kAtOnce > 1) {
