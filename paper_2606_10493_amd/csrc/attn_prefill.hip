@@ -157,7 +157,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
   v16f o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = v16f{};
-  float m = kNoScore, l = 0.0f;
+  float m = kNoScore;
+  v16f total{};  // the sum of the rounded numerators in all 16
 
   if (kt0 < kt1) {
     const uint16_t* kbase = a.k + (int64_t)k0 * a.k_stride + kvh * D;
@@ -222,22 +223,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
       if (__any(top > m + 8.0f)) {
         const float m_new = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - m_new);
         m = m_new;
-        l *= alpha;
+        total *= alpha;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) o[i] *= alpha;
       }
-      float sum[2] = {};
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
           const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.c, -m));
           const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i + 1], a.c, -m));
-          sum[0] += x;
-          sum[1] += y;
           p.x[8 * u + i / 2] = pack_bf16(x, y);
         }
-      l += sum[0] + sum[1];
     };
     // A step is a vector phase (`weigh`) and a matrix phase: the next tile's scores, then this tile's numerators times
     // its values, with the operands read from LDS kAhead products early, the first ones before the phase begins.
@@ -253,6 +250,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     // arrive, and the barrier after that wait comes before the first read.  (Behind the end the last row is fetched;
     // the scores of the tile behind the last are not used.)
     const bool late = wave >= WAVES / 2;
+    v8bf ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
     const auto step = [&](auto masked, int kt) __attribute__((always_inline)) {
       const int ft = late ? kt : kt - 1;
       fetch_k(ft + kRing);
@@ -278,6 +278,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
           s[f & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[f >> 1], s[f & 1], 0, 0, 0);
         else
           o[g % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p.v[g / (D / 32)], o[g % (D / 32)], 0, 0, 0);
+        // denominators: one product more for every 16 keys, which costs less than 32 additions in the vector phase
+        if (f >= kK && g % (D / 32) == 0)
+          total = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones, p.v[g / (D / 32)], total, 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_s_setprio(0);
@@ -325,7 +328,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     wait_async_and_barrier<0>();  // no fetch is on its way to LDS, and no wave reads from it any more
   }
 
-  l += __shfl_xor(l, 32, 64);
+  const float l = total[0];
   // Whole rows go out: a lane has pieces of 4 elements of one row, which the wave's part of LDS turns into rows (stores
   // of 16 or 32 bytes a row took three times as long as the rest of a short sequence's work).
   const int64_t heads = a.kv_heads * group;
@@ -476,6 +479,7 @@ extern "C" moe_status_t moe_attn_prefill(moe_attn_dims_t d, int32_t B, int32_t T
   if (B < 0 || T_q < 0 || T_k < 0 || max_k < 0)
     return fail(MOE_ERR_INVALID_ARG, "moe_attn_prefill: B=%d T_q=%d T_k=%d max_k=%d", B, T_q, T_k, max_k);
   if (!(scale > 0.0f) || !isfinite(scale * kLog2e)) return fail(MOE_ERR_INVALID_ARG, "moe_attn_prefill: scale=%g", scale);
+  if (T_k > 1 << 30) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_prefill: T_k=%d is over 2^30", T_k);
   if (B == 0 || T_q == 0) return MOE_OK;
   if ((st = check_rows(q, q_stride, d.q_heads, d.head_dim, "moe_attn_prefill", "q")) != MOE_OK) return st;
   if (T_k > 0 && (st = check_rows(k, k_stride, d.kv_heads, d.head_dim, "moe_attn_prefill", "k")) != MOE_OK) return st;
