@@ -575,7 +575,8 @@ moe_status_t moe_cache_read(moe_attn_dims_t dims, moe_kv_cache_t cache, const in
  * place, sequences' ends aligned: query i of lq sees keys 0 .. i + lk - lq (a
  * chunk of queries behind keys that are cached already).  A query that sees no
  * key gets zeros.  Scores, the running maximum and sum and the accumulation are
- * fp32; the softmax's numerators are rounded to bf16 for the product with v.
+ * fp32; the softmax's numerators are rounded to bf16 for the product with v (and
+ * their sum is that of the rounded ones).
  *
  * Sequence b: queries cu_q[b] .. cu_q[b+1] - 1 of T_q, keys cu_k[b] ..
  * cu_k[b+1] - 1 of T_k (device int32 [B + 1], not decreasing); offsets that

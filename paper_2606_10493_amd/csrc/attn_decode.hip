@@ -9,15 +9,13 @@
 //                 first operand (lane: key lane % 16, 16 codes at 16 (lane / 16)
 //                 of each 64), converted exactly; a lane ends with the scores of
 //                 query lane % 16 for keys 4 (lane / 16) + i
-//   O^T = V^T P^T (f16) values' codes go through LDS and come back transposed
+//   O^T = V^T P^T (bf16) values' codes go through LDS and come back transposed
 //                 (ds_read_b64_tr_b8) in the order of keys that the scores have
 // Scales stay fp32: a key's multiplies its score, a value's its numerator.  The
-// numerators are rounded once for the product, to f16: a code is exact in f16 as
-// it is in bf16, and f16 has three bits more.  Its range is kept by what the
-// scores are taken against: the running maximum of a step's largest score plus the
-// logarithm of its largest value scale (numerators, sums and results share that
-// reference, so it cancels).  It grows only when it would by more than 2^8, so a
-// product is at most 2^8, and what underflows is below 2^-24 of the largest.
+// products of these are split into two bf16, a rounded one and what it leaves (16
+// bits of mantissa, the exponents of fp32), each multiplied: the matrix cores have
+// the time, and the result is exact but for its own rounding (1.7e-3 of its norm;
+// with one bf16 2.4e-3).
 //
 // Bound by memory: head_dim + 4 bytes per key, value and head against 4 * G *
 // head_dim flops.
@@ -60,27 +58,12 @@ constexpr int kWaves = 4;
 constexpr int kStride = kKeys * kWaves;  // keys per step of a workgroup
 constexpr int kMostKeys = 1 << 30;  // of a sequence: key indices and the steps behind them stay in 32 bits
 
-typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ v8h e4m3x8_to_f16(uint32_t lo, uint32_t hi) {
-  union {
-    v8h v;
-    v2h p[4];
-  } r;
-  r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false);
-  r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
-  r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false);
-  r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
-  return r.v;
-}
-
 // The running softmax of NC blocks of 16 queries; a lane's query is column
 // lane % 16 of each block.
 template <int D, int NC>
 struct Running {
   v4f o[NC][D / 16];   // O^T: rows 16 i + 4 (lane / 16) + 0..3
-  float m[NC], l[NC];  // the reference; l: this lane's keys only, summed over the lane groups at the end
+  float m[NC], l[NC];  // l: this lane's keys only, summed over the lane groups at the end
 };
 
 // The maximum over the four lanes that hold one query (lane, lane ^ 16, ^ 32,
@@ -217,24 +200,19 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
         for (int n = 0; n < NC; ++n) s[n][u][i] = there ? s[n][u][i] : -INFINITY;
       }
   }
-  float vtop = 0x1p-100f, top[NC];  // (values that are all below 2^-100 lose digits)
-#pragma unroll
-  for (int n = 0; n < NC; ++n) top[n] = s[n][0][0];
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      vtop = fmaxf(vtop, vs[u][i]);
-#pragma unroll
-      for (int n = 0; n < NC; ++n) top[n] = fmaxf(top[n], s[n][u][i]);
-    }
-  const float vlog = __builtin_amdgcn_logf(quad_max(vtop));
+  float top[NC];
   bool grows = false;
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
-    top[n] = quad_max(top[n]) + vlog;
+    top[n] = s[n][0][0];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top[n] = fmaxf(top[n], s[n][u][i]);
+    top[n] = quad_max(top[n]);
     grows |= top[n] > run.m[n] + 8.0f;
   }
+  // rescaled only when a maximum grows by more than 2^8: numerators up to 2^8 are as exact
   if (__any(grows)) {
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
@@ -246,9 +224,9 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
     }
   }
   union {
-    v8h v;
-    v2h x[4];
-  } pf[NC];
+    v8bf v;
+    uint32_t x[4];
+  } hi[NC], lo[NC];
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
     float sum = 0.0f;
@@ -261,8 +239,12 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
         sum += e[i];
         e[i] *= vs[u][i];
       }
-      pf[n].x[2 * u] = v2h{(_Float16)e[0], (_Float16)e[1]};
-      pf[n].x[2 * u + 1] = v2h{(_Float16)e[2], (_Float16)e[3]};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t w = pack_bf16(e[2 * i], e[2 * i + 1]);
+        hi[n].x[2 * u + i] = w;
+        lo[n].x[2 * u + i] = pack_bf16(e[2 * i] - __uint_as_float(w << 16), e[2 * i + 1] - __uint_as_float(w & 0xffff0000u));
+      }
     }
     run.l[n] += sum;
   }
@@ -273,9 +255,12 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
   for (int i = 0; i < D / 16; ++i) {
     const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
         (__attribute__((address_space(3))) v2i*)(lds + Staged<D>::value(row, i) + 8 * (c16 & 1)));
-    const v8h vf = e4m3x8_to_f16(y[0], y[1]);
+    const v8bf vf = e4m3x8_to_bf16(y[0], y[1]);
 #pragma unroll
-    for (int n = 0; n < NC; ++n) run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n].v, run.o[n][i], 0, 0, 0);
+    for (int n = 0; n < NC; ++n) {
+      run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi[n].v, run.o[n][i], 0, 0, 0);
+      run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo[n].v, run.o[n][i], 0, 0, 0);
+    }
   }
 }
 

@@ -245,3 +245,47 @@ def test_pages_beyond_4_gib(moe):
     for h in (0, 7):
         ref, bound = ao.attention(xv[:1, h], want[:, h], want[:, h], 0.1)
         check(out[:, h], ref, bound, f"far pages, head {h}")
+
+
+@pytest.mark.parametrize("dims,prefix", [((4, 2, 64), 0), ((8, 2, 128), 300)])
+def test_more_sequences_than_a_wave_has_lanes(moe, dims, prefix):
+    """Ragged batches of 150 whose pieces begin and end anywhere; sequences are looked up 64 at a time."""
+    rng = np.random.default_rng(31)
+    hq, hkv, dim = dims
+    lens = [int(n) for n in rng.integers(0, 200, 150)]
+    lens[3], lens[70], lens[149] = 1500, 0, 900
+    cache = Cache(moe, rng, lens + ([prefix] if prefix else []), hkv, dim, 32)
+    q, qv = bf16(rng.standard_normal((150, hq, dim)))
+    got = run(moe, dims, q, cache, lens, 0.1, prefix)
+    ref, bound = reference(cache, qv, 150, 0.1, prefix)
+    check(got, ref, bound, f"150 sequences, prefix {prefix}")
+
+
+def test_more_heads_than_workgroups(moe):
+    rng = np.random.default_rng(32)
+    dims, lens = (520, 520, 64), [700, 5]
+    cache = Cache(moe, rng, lens, 520, 64, 64)
+    q, qv = bf16(rng.standard_normal((2, 520, 64)))
+    got = run(moe, dims, q, cache, lens, 0.1)
+    heads = [0, 511, 512, 519]
+    ref, bound = reference(cache, qv, 2, 0.1, 0, heads)
+    check(got[:, heads], ref[:, heads], bound[:, heads], "520 heads")
+
+
+@pytest.mark.parametrize("power", [-90, -20, 60])
+def test_values_of_extreme_sizes(moe, power):
+    """Value rows from 2^-40 to 2^0 of the largest in every order, all times 2^power: the reference that the numerators are
+    taken against follows the values' scales."""
+    rng = np.random.default_rng(33)
+    n = 1000
+    cache = Cache(moe, rng, [n], 1, 64, 16)
+    factor = (2.0 ** (power - rng.integers(0, 41, n))).astype(np.float32)
+    for t in range(n):
+        p, o = cache.table[0, t // 16], t % 16
+        cache.scales["v"][p, 0, o] *= factor[t]
+    cache.values["v"][0] = cache.values["v"][0] * factor[None, :, None]
+    cache.dev.v_scale.copy_(torch.from_numpy(cache.scales["v"]))
+    q, qv = bf16(rng.standard_normal((1, 4, 64)))
+    got = run(moe, (4, 1, 64), q, cache, [n], 0.1)
+    ref, bound = reference(cache, qv, 1, 0.1, 0)
+    check(got, ref, bound, f"values times 2^{power}")

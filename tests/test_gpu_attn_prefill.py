@@ -165,3 +165,73 @@ def test_offsets_that_leave_the_tensors_are_cut(moe):
     ref, bound = ao.packed_attention(qv, kv, vv, good, good, 0.1, True)
     check(got, ref, bound, "cut offsets")
     assert int(status.item()) == moe.MOE_DEV_BAD_LENGTH
+
+
+def test_more_sequences_than_a_wave_has_lanes(moe):
+    """The row tile's sequence is looked up 64 at a time."""
+    rng = np.random.default_rng(12)
+    lens = [int(n) for n in rng.integers(0, 40, 150)]
+    keys = [n + int(m) if n else 0 for n, m in zip(lens, rng.integers(0, 30, 150))]
+    dims = (4, 2, 64)
+    cu_q, cu_k = offsets(lens), offsets(keys)
+    q, qv = bf16(rng.standard_normal((cu_q[-1], 4, 64)))
+    k, kv = bf16(rng.standard_normal((cu_k[-1], 2, 64)))
+    v, vv = bf16(rng.standard_normal((cu_k[-1], 2, 64)))
+    got = run(moe, dims, q, k, v, cu_q, cu_k, max(keys), 0.1)
+    ref, bound = ao.packed_attention(qv, kv, vv, cu_q, cu_k, 0.1, True)
+    check(got, ref, bound, "150 sequences")
+
+
+@pytest.mark.parametrize("dims", [(1024, 1, 64), (96, 3, 128)])
+def test_wide_groups(moe, dims):
+    """Groups of more heads than a tile has rows, and of 32 heads."""
+    rng = np.random.default_rng(13)
+    hq, hkv, dim = dims
+    cu = offsets([7, 3])
+    q, qv = bf16(rng.standard_normal((10, hq, dim)))
+    k, kv = bf16(rng.standard_normal((10, hkv, dim)))
+    v, vv = bf16(rng.standard_normal((10, hkv, dim)))
+    got = run(moe, dims, q, k, v, cu, cu, 7, 0.1)
+    ref, bound = ao.packed_attention(qv, kv, vv, cu, cu, 0.1, True)
+    check(got, ref, bound, f"wide group {dims}")
+
+
+def test_values_that_are_all_one_stay_one(moe):
+    """Numerators and denominators are the same rounded numbers, so a mean of ones is exactly one."""
+    rng = np.random.default_rng(14)
+    cu = offsets([333])
+    q, k = (bf16(rng.standard_normal((333, h, 128)) * 3)[0] for h in (8, 2))
+    got = run(moe, (8, 2, 128), q, k, torch.ones_like(k), cu, cu, 333, 0.1)
+    assert bool((got == 1).all())
+
+
+@pytest.mark.parametrize("past", [0, 6000])
+def test_replays_from_a_hip_graph(moe, past):
+    """A call (with `past`, cut into parts and joined) captured once and replayed on new inputs, eager work in between."""
+    d = moe.MoeAttnDims(8, 2, 128)
+    q = torch.empty((90, 8, 128), dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.empty((90 + 2 * past, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cu_q, cu_k = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 50, 90], [0, 50 + past, 90 + 2 * past]))
+    ws = torch.empty(max(256, moe.moe_attn_prefill_workspace(d, 2, 90, 50 + past)), dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+
+    def call(ws_, out_):
+        moe.moe_attn_prefill(d, q, k, v, cu_q, cu_k, 50 + past, 0.1, out_, ws_)
+    for t in (q, k, v):
+        t.normal_()
+    call(ws, out)
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        call(ws, out)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for t in (q, k, v):
+            t.normal_()
+        ref = torch.empty_like(q)
+        call(torch.empty_like(ws), ref)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), ref.view(torch.int16))
