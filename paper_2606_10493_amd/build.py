@@ -1,4 +1,5 @@
-"""Build libmoe.so (the HIP kernels and the C ABI) in-tree for gfx950.
+"""Build libmoe.so (the HIP kernels and the C ABI) in-tree for gfx950, and
+_binding.so, the attention calls' native Python binding.
 
     python paper_2606_10493_amd/build.py
 
@@ -6,7 +7,8 @@
 
 Every .hip file under csrc/ is compiled with hipcc in parallel and linked
 into paper_2606_10493_amd/libmoe.so.  It compiles on a machine without a
-GPU (hipcc cross-compiles for gfx950).
+GPU (hipcc cross-compiles for gfx950).  csrc/binding.cpp is compiled with g++
+against the Python and torch headers and linked with libmoe.so.
 """
 from __future__ import annotations
 
@@ -16,6 +18,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -23,6 +26,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmoe.so")
+BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
@@ -48,6 +52,23 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _build_binding() -> None:
+    import torch  # its headers and its ABI flag
+    lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
+    include = os.path.join(os.path.dirname(torch.__file__), "include")
+    tmp = BINDING + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE, "-isystem", include,
+           "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", "/opt/rocm/include",
+           os.path.join(CSRC, "binding.cpp"), "-o", tmp,
+           "-L", PKG, "-lmoe", "-L", lib_dir, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"building binding.cpp failed:\n{res.stdout}\n{res.stderr}")
+    os.replace(tmp, BINDING)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
@@ -59,8 +80,9 @@ def build(verbose: bool = False) -> str:
     if res.returncode != 0:
         raise RuntimeError(f"link failed:\n{res.stdout}\n{res.stderr}")
     os.replace(tmp, LIB)
+    _build_binding()
     if verbose:
-        print(f"built {LIB} from {len(srcs)} sources")
+        print(f"built {LIB} from {len(srcs)} sources, and {BINDING}")
     return LIB
 
 
