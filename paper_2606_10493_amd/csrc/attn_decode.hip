@@ -30,6 +30,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attention.h"
 
@@ -264,6 +265,9 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
   }
 }
 
+// Steps of a run of keys.
+__host__ __device__ __forceinline__ int steps_of(int keys) { return (keys + kStride - 1) / kStride; }
+
 // A head's line of steps, and its pieces: prefix_blocks times the prefix's steps,
 // own_blocks times all sequences'.  (The host checks that it has less than 2^31
 // steps.)  A pair is one of its runs of keys for one block of columns: the
@@ -274,7 +278,7 @@ struct Line {
   uint32_t base, more;  // a piece has base steps, the first `more` have one more
   int64_t segments;     // of a head, at most
   __device__ __forceinline__ Line(const DecodeArgs& a, uint32_t own) {
-    prefix_steps = (a.prefix_len + kStride - 1) / kStride;
+    prefix_steps = steps_of(a.prefix_len);
     prefix_total = prefix_steps * a.prefix_blocks;
     own_total = own;
     const uint32_t all = prefix_total + own * a.own_blocks;
@@ -296,7 +300,6 @@ __device__ __forceinline__ int keys_of(const DecodeArgs& a, int b, bool& bad) {
   bad = len < 0 || len > most;
   return len < 0 ? 0 : (int)min((int64_t)len, most);
 }
-__device__ __forceinline__ int steps_of(int keys) { return (keys + kStride - 1) / kStride; }
 
 // 64 sequences' steps, a lane each, and their sum up to each.
 struct Chunk {
@@ -315,9 +318,10 @@ struct Chunk {
 
 // kWhole: a workgroup takes all keys of one (sequence, head, block of columns)
 // and writes its output; otherwise a piece of the line.
-template <int D, int NC, bool kWhole>
+// NCP, NCO: blocks of 16 columns on the prefix's keys and on a sequence's own.
+template <int D, int NCP, int NCO, bool kWhole>
 __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs a) {
-  constexpr int kCols = 16 * NC;
+  constexpr int kCols = 16 * (NCP > NCO ? NCP : NCO);
   // the waves' keys and values; behind the last step their sums
   constexpr int kWaveBytes = Staged<D>::kBytes > 16 * (D + 4) * 4 ? Staged<D>::kBytes : 16 * (D + 4) * 4;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves][kWaveBytes];
@@ -325,12 +329,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
   const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
+  using Front = std::integral_constant<int, NCP>;
+  using Own = std::integral_constant<int, NCO>;
   Part p;
   bool shared = false;
   int b = 0, col0 = 0, cols = 0;
   int64_t segment = 0;
   // The segment's keys by p, the sums to `segment` or (kWhole) the output.
-  const auto run_segment = [&](const Pages& first) __attribute__((always_inline)) {
+  const auto run_segment = [&](auto blocks, const Pages& first) __attribute__((always_inline)) {
+    constexpr int NC = decltype(blocks)::value;
     // column n of block col0: query head (col % G) of the group, of sequence col / G in the prefix
     const auto split = [&](int col, int& seq, int& head) {
       seq = shared ? (col0 + col) / a.group : b;
@@ -426,8 +433,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
     p.kvh = item % a.kv_heads;
     item /= a.kv_heads;
     b = item % a.B;
-    col0 = item / a.B * kCols;
-    cols = min(kCols, a.group - col0);
+    col0 = item / a.B * 16 * NCO;
+    cols = min(16 * NCO, a.group - col0);
     p.pages = a.pages + (int64_t)b * a.width;
     p.width = a.width;
     // the first step's pages are on their way while the length is
@@ -438,7 +445,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
     if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
     p.begin = 0;
     p.end = p.len;
-    run_segment(first);
+    run_segment(Own{}, first);
     return;
   }
 
@@ -504,8 +511,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
       if (lane == 0) {
         found.more = taken > 0;
         found.shared = front;
-        found.col0 = block * kCols;
-        found.cols = min(kCols, (front ? a.B * a.group : a.group) - (int)block * kCols);
+        const int width = 16 * (front ? NCP : NCO);
+        found.col0 = block * width;
+        found.cols = min(width, (front ? a.B * a.group : a.group) - (int)block * width);
         found.b = seq;
         found.len = len;
         found.begin = (int)(skip * kStride);
@@ -526,16 +534,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
     segment = p.kvh * line.segments + piece + (uint32_t)__builtin_amdgcn_readfirstlane(found.pair);
     p.pages = shared ? a.prefix_pages : a.pages + (int64_t)b * a.width;
     p.width = shared ? ((a.prefix_len - 1) >> a.page_shift) + 1 : a.width;
-    run_segment(pages_of(a, p, p.begin + wave * kKeys));
+    const Pages first = pages_of(a, p, p.begin + wave * kKeys);
+    if (NCP != NCO && shared)
+      run_segment(Front{}, first);
+    else
+      run_segment(Own{}, first);
   }
 }
 
 // A row's segments, weighed by their maxima: those of the prefix's pair that has
 // the row among its columns, then those of the row's own.  D / 4 lanes with 16
 // bytes each take a segment; kAtOnce of them work on one row.
-template <int D, int NC, int kAtOnce>
+template <int D, int NCP, int NCO, int kAtOnce>
 __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
-  constexpr int kCols = 16 * NC, kLanes = D / 4, kRows = 256 / (kLanes * kAtOnce);
+  constexpr int kCols = 16 * (NCP > NCO ? NCP : NCO), kPrefixCols = 16 * NCP, kOwnCols = 16 * NCO, kLanes = D / 4, kRows = 256 / (kLanes * kAtOnce);
   __shared__ __attribute__((aligned(16))) float lds_o[kAtOnce][D];
   __shared__ float lds_m[kAtOnce], lds_l[kAtOnce];
   const int sub = threadIdx.x % kLanes, nth = threadIdx.x / kLanes % kAtOnce;
@@ -564,12 +576,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
   };
   if (a.prefix_len > 0) {
     const int pcol = b * a.group + col;
-    const uint32_t block = pcol / kCols;
-    take(block, block * line.prefix_steps, (block + 1) * line.prefix_steps - 1, pcol % kCols);
+    const uint32_t block = pcol / kPrefixCols;
+    take(block, block * line.prefix_steps, (block + 1) * line.prefix_steps - 1, pcol % kPrefixCols);
   }
   if (steps > 0) {
-    const uint32_t block = col / kCols, first = line.prefix_total + block * line.own_total + start;
-    take(a.prefix_blocks + block * a.B + b, first, first + steps - 1, col % kCols);
+    const uint32_t block = col / kOwnCols, first = line.prefix_total + block * line.own_total + start;
+    take(a.prefix_blocks + block * a.B + b, first, first + steps - 1, col % kOwnCols);
   }
   if (kAtOnce > 1) {
     *reinterpret_cast<v4f*>(&lds_o[nth][4 * sub]) = o;
@@ -599,7 +611,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
 
 struct DecodePlan {
   bool whole;
-  int col_blocks;  // of 16 columns in a workgroup
+  int front, own;  // blocks of 16 columns in a workgroup, on the prefix's keys and on a sequence's own
   int own_blocks, prefix_blocks, pieces;
   int64_t workgroups;
   size_t o_bytes, ml_bytes, start_bytes;
@@ -613,21 +625,24 @@ constexpr int kWholeSteps = 5;
 DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int32_t prefix_len) {
   DecodePlan p{};
   const int group = d.q_heads / d.kv_heads;
-  p.col_blocks = group > 16 || (prefix_len > 0 && (int64_t)B * group > 16) ? 2 : 1;
-  const int cols = 16 * p.col_blocks;
-  p.own_blocks = (group + cols - 1) / cols;
-  p.prefix_blocks = prefix_len > 0 ? (int)(((int64_t)B * group + cols - 1) / cols) : 0;
+  const int64_t all = (int64_t)B * group;
+  p.own = group > 16 ? 2 : 1;
+  // two blocks of columns a wave on the prefix (48 sequences of 4 columns each, 8191 keys: 28 us; one block 39, four, with
+  // one workgroup a CU, 40)
+  p.front = prefix_len > 0 && all > 16 ? 2 : p.own;
+  p.own_blocks = (group + 16 * p.own - 1) / (16 * p.own);
+  p.prefix_blocks = prefix_len > 0 ? (int)((all + 16 * p.front - 1) / (16 * p.front)) : 0;
   const int64_t own_pairs = (int64_t)p.own_blocks * B;
   const int64_t own_steps = ((int64_t)max_len + kStride - 1) / kStride;
   p.whole = prefix_len == 0 && own_steps <= kWholeSteps;
   p.workgroups = own_pairs * d.kv_heads;
   if (!p.whole) {
-    const int64_t steps = own_pairs * own_steps + p.prefix_blocks * (((int64_t)prefix_len + kStride - 1) / kStride);
+    const int64_t steps = own_pairs * steps_of(max_len) + (int64_t)p.prefix_blocks * steps_of(prefix_len);
     // Two workgroups a CU (64 ragged contexts: 77 us with 512 workgroups, 81 with 768, 84 with 1536; one context of 65536:
     // 27, 29 and 31 us, and a longer join).
     p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>(512 / d.kv_heads, steps));
     p.workgroups = (int64_t)p.pieces * d.kv_heads;
-    const size_t places = (size_t)d.kv_heads * (p.pieces + p.prefix_blocks + own_pairs) * cols;
+    const size_t places = (size_t)d.kv_heads * (p.pieces + p.prefix_blocks + own_pairs) * 16 * std::max(p.front, p.own);
     p.o_bytes = (places * d.head_dim * sizeof(float) + 255) & ~(size_t)255;
     p.ml_bytes = (places * sizeof(float2) + 255) & ~(size_t)255;
     p.start_bytes = ((size_t)(B + 1) * sizeof(uint32_t) + 255) & ~(size_t)255;
@@ -635,7 +650,7 @@ DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int
   return p;
 }
 
-template <int D, int NC>
+template <int D, int NCP, int NCO>
 moe_status_t launch_decode(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream) {
   constexpr int kAtOnce = 256 / (D / 4);
   const int64_t rows = (int64_t)a.B * a.kv_heads * a.group;
@@ -643,17 +658,23 @@ moe_status_t launch_decode(const DecodeArgs& a, const DecodePlan& p, hipStream_t
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_decode: %lld rows", (long long)rows);
   const dim3 grid((unsigned)p.workgroups);
   if (p.whole) {
-    MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, NC, true>), grid, dim3(64 * kWaves), 0, stream, a);
+    MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, NCO, NCO, true>), grid, dim3(64 * kWaves), 0, stream, a);
     return check_launch("moe_attn_decode");
   }
-  MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, NC, false>), grid, dim3(64 * kWaves), 0, stream, a);
+  MOE_LAUNCH("attn_decode", (attn_decode_kernel<D, NCP, NCO, false>), grid, dim3(64 * kWaves), 0, stream, a);
   // A row has about as many segments as its pairs have pieces: a workgroup a row for many, lanes of their own for few.
   if (p.pieces >= 4 * (p.prefix_blocks + p.own_blocks * a.B))
-    MOE_LAUNCH("attn_join", (attn_join_kernel<D, NC, kAtOnce>), dim3((unsigned)rows), dim3(256), 0, stream, a);
+    MOE_LAUNCH("attn_join", (attn_join_kernel<D, NCP, NCO, kAtOnce>), dim3((unsigned)rows), dim3(256), 0, stream, a);
   else
-    MOE_LAUNCH("attn_join", (attn_join_kernel<D, NC, 1>), dim3((unsigned)((rows + kAtOnce - 1) / kAtOnce)), dim3(256), 0,
+    MOE_LAUNCH("attn_join", (attn_join_kernel<D, NCP, NCO, 1>), dim3((unsigned)((rows + kAtOnce - 1) / kAtOnce)), dim3(256), 0,
                stream, a);
   return check_launch("moe_attn_decode");
+}
+
+template <int D>
+moe_status_t dispatch_decode(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream) {
+  if (p.own == 2) return launch_decode<D, 2, 2>(a, p, stream);
+  return p.front == 1 ? launch_decode<D, 1, 1>(a, p, stream) : launch_decode<D, 2, 1>(a, p, stream);
 }
 
 }  // namespace
@@ -691,8 +712,7 @@ extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint
   if (!aligned(out, 16)) return fail(MOE_ERR_INVALID_ARG, "moe_attn_decode: out must be 16-byte aligned");
   const DecodePlan p = plan_decode(d, B, max_len, prefix_len);
   const int64_t row_keys = std::min<int64_t>((int64_t)table_width * cache.page_size, kMostKeys);
-  const int64_t prefix_steps = ((int64_t)prefix_len + kStride - 1) / kStride, row_steps = (row_keys + kStride - 1) / kStride;
-  if (p.prefix_blocks * prefix_steps + (int64_t)p.own_blocks * B * row_steps > 0x7fffffff)
+  if ((int64_t)p.prefix_blocks * steps_of(prefix_len) + (int64_t)p.own_blocks * B * steps_of((int)row_keys) > 0x7fffffff)
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_decode: %d sequences of %lld keys and a prefix of %d: over 2^31 steps", B,
                 (long long)row_keys, prefix_len);
   const size_t need = p.o_bytes + p.ml_bytes + p.start_bytes;
@@ -707,7 +727,5 @@ extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint
     a.seg_ml = reinterpret_cast<float2*>(base + p.o_bytes);
     a.starts = reinterpret_cast<uint32_t*>(base + p.o_bytes + p.ml_bytes);
   }
-  if (d.head_dim == 64)
-    return p.col_blocks == 1 ? launch_decode<64, 1>(a, p, stream) : launch_decode<64, 2>(a, p, stream);
-  return p.col_blocks == 1 ? launch_decode<128, 1>(a, p, stream) : launch_decode<128, 2>(a, p, stream);
+  return d.head_dim == 64 ? dispatch_decode<64>(a, p, stream) : dispatch_decode<128>(a, p, stream);
 }
