@@ -94,14 +94,13 @@ struct Part {
 
 // The pages of keys [t, t + 32): each half of 16 lies in one.  Entries behind the
 // sequence's last page may be looked at, and are not used.
-struct Pages {
-  int id[2];
-};
-__device__ __forceinline__ Pages pages_of(const DecodeArgs& a, const Part& p, int t) {
-  Pages r;
-#pragma unroll
-  for (int u = 0; u < 2; ++u) r.id[u] = p.pages[min((t + 16 * u) >> a.page_shift, p.width - 1)];
-  return r;
+// Each half of the wave looks at one: a value of the lanes, which becomes a scalar
+// where the loads behind it need it.  (A load of one address for all lanes is made
+// a scalar at once, behind a wait for every load in front of it, the step's keys
+// and values among them.)
+__device__ __forceinline__ int pages_of(const DecodeArgs& a, const Part& p, int t) {
+  const int lane = threadIdx.x;
+  return p.pages[min((t + ((lane & 32) >> 1)) >> a.page_shift, p.width - 1)];
 }
 
 // A wave's part of LDS: keys, values (rows of D codes in 16-byte chunks), scales.
@@ -123,12 +122,12 @@ struct Staged {
 // this launch, so they need no place in the caches (64 ragged contexts: 90 us
 // without, 78 with, whole rows per load in both).
 template <int D, bool kOnce>
-__device__ __forceinline__ void load_tile(const DecodeArgs& a, const Part& p, int t0, const Pages& pg, bool& bad,
+__device__ __forceinline__ void load_tile(const DecodeArgs& a, const Part& p, int t0, int pages, bool& bad,
                                           Tile<D>& x) {
   constexpr int kChunks = D / 16;
   const int lane = threadIdx.x & 63, mask = a.cache.page_size - 1, last = p.len - 1;
   const bool two = t0 + 16 <= last;
-  const int id0 = pg.id[0], id1 = two ? pg.id[1] : id0;
+  const int id0 = __builtin_amdgcn_readlane(pages, 0), id1 = two ? __builtin_amdgcn_readlane(pages, 32) : id0;
   const bool wrong0 = id0 < 0 || id0 >= a.cache.n_pages, wrong1 = id1 < 0 || id1 >= a.cache.n_pages;
   bad |= wrong0 | wrong1;
   // the first key of each half, counted in rows of the cache
@@ -336,7 +335,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
   int b = 0, col0 = 0, cols = 0;
   int64_t segment = 0;
   // The segment's keys by p, the sums to `segment` or (kWhole) the output.
-  const auto run_segment = [&](auto blocks, const Pages& first) __attribute__((always_inline)) {
+  const auto run_segment = [&](auto blocks, int first) __attribute__((always_inline)) {
     constexpr int NC = decltype(blocks)::value;
     // column n of block col0: query head (col % G) of the group, of sequence col / G in the prefix
     const auto split = [&](int col, int& seq, int& head) {
@@ -367,7 +366,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
       }
       bool bad = false;
       Tile<D> x;
-      Pages ahead = first;
+      int ahead = first;
       const auto load = [&](int at) __attribute__((always_inline)) {
         if (shared || a.own_blocks > 1)
           load_tile<D, false>(a, p, at, ahead, bad, x);
@@ -438,7 +437,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
     p.pages = a.pages + (int64_t)b * a.width;
     p.width = a.width;
     // the first step's pages are on their way while the length is
-    Pages first = {};
+    int first = 0;
     if (a.width > 0) first = pages_of(a, p, wave * kKeys);
     bool bad;
     p.len = keys_of(a, b, bad);
@@ -534,7 +533,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
     segment = p.kvh * line.segments + piece + (uint32_t)__builtin_amdgcn_readfirstlane(found.pair);
     p.pages = shared ? a.prefix_pages : a.pages + (int64_t)b * a.width;
     p.width = shared ? ((a.prefix_len - 1) >> a.page_shift) + 1 : a.width;
-    const Pages first = pages_of(a, p, p.begin + wave * kKeys);
+    const int first = pages_of(a, p, p.begin + wave * kKeys);
     if (NCP != NCO && shared)
       run_segment(Front{}, first);
     else
