@@ -99,21 +99,21 @@ struct Part {
 // a scalar at once, behind a wait for every load in front of it, the step's keys
 // and values among them.)
 __device__ __forceinline__ int pages_of(const DecodeArgs& a, const Part& p, int t) {
-  const int lane = threadIdx.x;
-  return p.pages[min((t + ((lane & 32) >> 1)) >> a.page_shift, p.width - 1)];
+  const int lane = threadIdx.x, half = (lane & 32) >> 1;
+  return p.pages[(uint32_t)min((t + half) >> a.page_shift, p.width - 1)];
 }
 
-// A wave's part of LDS: keys, values (rows of D codes in 16-byte chunks), scales.
-// The swizzles spread what one instruction reads over the 256 bytes of the banks:
-// 16 keys at one chunk, or the 16 values' rows of two 8 x 16 blocks at one chunk.
+// A wave's part of LDS: keys, values (rows of D codes), scales.  Rows are 16 bytes
+// longer than their codes, so that 16 of them at one chunk of 16 bytes lie in
+// different banks, and all places of a lane are one register and constants.
+// Values stand in the order in which a transposed read takes them: keys 4 g + 0..3
+// and 16 + 4 g + 0..3 as rows 8 g + 0..7.
 template <int D>
 struct Staged {
-  static constexpr int kV = kKeys * D, kScale = 2 * kKeys * D, kBytes = kScale + 64 * 4;
-  static __device__ __forceinline__ int key(int row, int c) {
-    return row * D + ((c ^ (D == 128 ? (row >> 1) & 7 : (row >> 2) & 3)) * 16);
-  }
+  static constexpr int kPitch = D + 16, kV = kKeys * kPitch, kScale = 2 * kV, kBytes = kScale + 64 * 4;
+  static __device__ __forceinline__ int key(int row, int c) { return row * kPitch + 16 * c; }
   static __device__ __forceinline__ int value(int row, int c) {
-    return kV + row * D + ((c ^ (D == 128 ? ((row >> 1) & 3) | ((row >> 2) & 4) : ((row >> 2) & 1) | ((row >> 3) & 2))) * 16);
+    return kV + (((row & 12) << 1) | ((row & 16) >> 2) | (row & 3)) * kPitch + 16 * c;
   }
 };
 
@@ -136,16 +136,23 @@ __device__ __forceinline__ void load_tile(const DecodeArgs& a, const Part& p, in
   const int left = last - t0, left1 = two ? left - 16 : left;  // rows behind these repeat them
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
-    const int at = 64 * i + lane, row = at / kChunks, c = at % kChunks;
-    const int64_t from = (row < 16 ? row0 + min(row, left) : row1 + min(row - 16, left1)) * D + 16 * c;
-    const u32x4_stream* k = reinterpret_cast<const u32x4_stream*>(a.cache.k + from);
-    const u32x4_stream* v = reinterpret_cast<const u32x4_stream*>(a.cache.v + from);
+    // scalar bases and 32-bit offsets
+    const bool second = i >= D / 64;
+    const int row = 64 / kChunks * (i % (D / 64)) + lane / kChunks;
+    const uint32_t from = min(row, second ? left1 : left) * D + lane % kChunks * 16;
+    const int64_t base = (second ? row1 : row0) * D;
+    const u32x4_stream* k = reinterpret_cast<const u32x4_stream*>(a.cache.k + base + from);
+    const u32x4_stream* v = reinterpret_cast<const u32x4_stream*>(a.cache.v + base + from);
     x.k[i] = kOnce ? __builtin_nontemporal_load(k) : *k;
     x.v[i] = kOnce ? __builtin_nontemporal_load(v) : *v;
   }
-  const int row = lane & 31;
+  const int row = lane & 15;
   const float* scales = lane < 32 ? a.cache.k_scale : a.cache.v_scale;
-  x.scale = scales[row < 16 ? row0 + min(row, left) : row1 + min(row - 16, left1)];
+  x.scale = scales[(lane & 16 ? row1 : row0) + min(row, lane & 16 ? left1 : left)];
+}
+
+__device__ __forceinline__ float most(v4f a, v4f b) {
+  return fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3])));
 }
 
 // The step at t0, whose keys and values are in x; once they are in LDS, `next`
@@ -161,7 +168,7 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
     *reinterpret_cast<u32x4_stream*>(lds + Staged<D>::key(at / kChunks, at % kChunks)) = x.k[i];
     *reinterpret_cast<u32x4_stream*>(lds + Staged<D>::value(at / kChunks, at % kChunks)) = x.v[i];
   }
-  *reinterpret_cast<float*>(lds + Staged<D>::kScale + 4 * lane) = x.scale;
+  *reinterpret_cast<float*>(lds + Staged<D>::kScale + 4 * lane) = lane < 32 ? x.scale * a.c : x.scale;
   next();
   v4f s[NC][2];
 #pragma unroll
@@ -173,10 +180,10 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
       const uint4 k = *reinterpret_cast<const uint4*>(lds + Staged<D>::key(16 * u + c16, g + 4 * i));
       const v8bf lo = e4m3x8_to_bf16(k.x, k.y), hi = e4m3x8_to_bf16(k.z, k.w);
 #pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        s[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, qf[n][2 * i], s[n][u], 0, 0, 0);
+      for (int n = 0; n < NC; ++n) s[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, qf[n][2 * i], s[n][u], 0, 0, 0);
+#pragma unroll
+      for (int n = 0; n < NC; ++n)
         s[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, qf[n][2 * i + 1], s[n][u], 0, 0, 0);
-      }
     }
   }
   v4f ks[2], vs[2];
@@ -184,43 +191,48 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
   for (int u = 0; u < 2; ++u) {
     ks[u] = *reinterpret_cast<const v4f*>(lds + Staged<D>::kScale + 4 * (16 * u + 4 * g));
     vs[u] = *reinterpret_cast<const v4f*>(lds + Staged<D>::kScale + 4 * (32 + 16 * u + 4 * g));
-#pragma unroll
-    for (int n = 0; n < NC; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[n][u][i] *= ks[u][i] * a.c;
   }
   if (t0 + kKeys > p.len) {  // a slot behind the end may hold any bits
+    asm volatile("");        // one step of many: no selects in the others
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const bool there = t0 + 16 * u + 4 * g + i < p.len;
+        ks[u][i] = there ? ks[u][i] : 1.0f;
         vs[u][i] = there ? vs[u][i] : 0.0f;
 #pragma unroll
         for (int n = 0; n < NC; ++n) s[n][u][i] = there ? s[n][u][i] : -INFINITY;
       }
   }
-  float top[NC];
+  // the logarithms of the numerators under the maxima so far
+  v4f e[NC][2];
   bool grows = false;
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
-    top[n] = s[n][0][0];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top[n] = fmaxf(top[n], s[n][u][i]);
-    top[n] = quad_max(top[n]);
-    grows |= top[n] > run.m[n] + 8.0f;
+      for (int i = 0; i < 4; ++i) e[n][u][i] = fmaf(s[n][u][i], ks[u][i], -run.m[n]);
+    grows |= most(e[n][0], e[n][1]) > 8.0f;
   }
-  // rescaled only when a maximum grows by more than 2^8: numerators up to 2^8 are as exact
+  // Rescaled only when a maximum grows by more than 2^8: numerators up to 2^8 are as exact.  The lanes of a query have
+  // one maximum, so that only then do they have to agree on another.
   if (__any(grows)) {
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-      const float m = fmaxf(run.m[n], top[n]), alpha = __builtin_amdgcn_exp2f(run.m[n] - m);
+      v4f x[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) x[u] = s[n][u] * ks[u];
+      const float m = fmaxf(run.m[n], quad_max(most(x[0], x[1]))), alpha = __builtin_amdgcn_exp2f(run.m[n] - m);
       run.m[n] = m;
       run.l[n] *= alpha;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) run.o[n][i] *= alpha;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[n][u][i] = fmaf(s[n][u][i], ks[u][i], -m);
     }
   }
   union {
@@ -232,35 +244,32 @@ __device__ __forceinline__ void use_tile(const DecodeArgs& a, const Part& p, int
     float sum = 0.0f;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      float e[4];
+      float w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(s[n][u][i] - run.m[n]);
-        sum += e[i];
-        e[i] *= vs[u][i];
+        w[i] = __builtin_amdgcn_exp2f(e[n][u][i]);
+        sum += w[i];
+        w[i] *= vs[u][i];
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t w = pack_bf16(e[2 * i], e[2 * i + 1]);
-        hi[n].x[2 * u + i] = w;
-        lo[n].x[2 * u + i] = pack_bf16(e[2 * i] - __uint_as_float(w << 16), e[2 * i + 1] - __uint_as_float(w & 0xffff0000u));
+        const uint32_t x = pack_bf16(w[2 * i], w[2 * i + 1]);
+        hi[n].x[2 * u + i] = x;
+        lo[n].x[2 * u + i] = pack_bf16(w[2 * i] - __uint_as_float(x << 16), w[2 * i + 1] - __uint_as_float(x & 0xffff0000u));
       }
     }
     run.l[n] += sum;
   }
-  // lane j of a 16-lane group gives the address of row j / 2, half j % 2 of an 8 x 16 block and gets column j:
-  // rows 0..3 are keys 4 g + 0..3, rows 4..7 keys 16 + 4 g + 0..3
-  const int j = c16 >> 1, row = (j < 4 ? 0 : 12) + 4 * g + j;
+  // lane j of a 16-lane group gives the address of row j / 2, half j % 2 of an 8 x 16 block and gets column j
+  const uint8_t* at = lds + Staged<D>::kV + (8 * g + (c16 >> 1)) * Staged<D>::kPitch + 8 * (c16 & 1);
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
-    const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-        (__attribute__((address_space(3))) v2i*)(lds + Staged<D>::value(row, i) + 8 * (c16 & 1)));
+    const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)(at + 16 * i));
     const v8bf vf = e4m3x8_to_bf16(y[0], y[1]);
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi[n].v, run.o[n][i], 0, 0, 0);
-      run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo[n].v, run.o[n][i], 0, 0, 0);
-    }
+    for (int n = 0; n < NC; ++n) run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi[n].v, run.o[n][i], 0, 0, 0);
+#pragma unroll
+    for (int n = 0; n < NC; ++n) run.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo[n].v, run.o[n][i], 0, 0, 0);
   }
 }
 
