@@ -18,7 +18,11 @@
 // with one bf16 2.4e-3).
 //
 // Bound by memory: head_dim + 4 bytes per key, value and head against 4 * G *
-// head_dim flops.
+// head_dim flops.  64 sequences of up to 8192 keys: 77 us, 5.2 TB/s (a kernel that
+// only loads the same takes as long); one of 65536: 25 us, 5.5 TB/s.  On a prefix,
+// where a key serves 16 NCP columns, bound by the vector instructions of a step:
+// 48 sequences behind 8191 shared keys 26 us, of which 15 are eight steps of about
+// 330 instructions beside 48 MFMAs, two waves to a SIMD.
 //
 // A head's work is a line of steps of 128 keys (32 for each wave of a
 // workgroup): the prefix's for every block of columns, then the sequences' one

@@ -282,16 +282,7 @@ __device__ __forceinline__ void async_load_1k(const void* src, uint32_t lds) {
                : "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src)
                : "memory");
 }
-// The same from base + offset (base uniform, offset the lane's).  A vector memory
-// instruction needs five wait states after a vector instruction wrote its scalar
-// base.
-__device__ __forceinline__ void async_load_1k_at(const void* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2"
-               :
-               : "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(base)
-               : "memory");
-}
-// The same if `on`
+// The same from base + offset (base uniform, offset the lane's) if `on`
 // (uniform), without a branch that the compiler sees: between matrix
 // instructions a basic block's end costs it the registers' order.
 __device__ __forceinline__ void async_load_1k_if(int on, const void* base, uint32_t offset, uint32_t lds) {
