@@ -29,8 +29,8 @@
 // behind the other.  The workgroups that the card holds at once take equal pieces
 // of the heads' lines, so that one long context and a ragged batch both fill it
 // evenly; where a piece or a sequence ends, a segment ends, whose sums a second
-// launch joins.  Short contexts without a prefix take one workgroup a sequence
-// and head, and no second launch.
+// launch joins.  Short contexts take one workgroup a sequence and head, which walks
+// the prefix for itself, and no second launch.
 #include <math.h>
 
 #include <algorithm>
@@ -126,8 +126,8 @@ struct Staged {
 // this launch, so they need no place in the caches (64 ragged contexts: 90 us
 // without, 78 with, whole rows per load in both).
 template <int D, bool kOnce>
-__device__ __forceinline__ void load_tile(const DecodeArgs& a, const Part& p, int t0, int pages, bool& bad,
-                                          Tile<D>& x) {
+__device__ __forceinline__ void load_tile(const DecodeArgs& a, const Part& p, const float* scales, int t0, int pages,
+                                          bool& bad, Tile<D>& x) {
   constexpr int kChunks = D / 16;
   const int lane = threadIdx.x & 63, mask = a.cache.page_size - 1, last = p.len - 1;
   const bool two = t0 + 16 <= last;
@@ -151,7 +151,6 @@ __device__ __forceinline__ void load_tile(const DecodeArgs& a, const Part& p, in
     x.v[i] = kOnce ? __builtin_nontemporal_load(v) : *v;
   }
   const int row = lane & 15;
-  const float* scales = lane < 32 ? a.cache.k_scale : a.cache.v_scale;
   x.scale = scales[(lane & 16 ? row1 : row0) + min(row, lane & 16 ? left1 : left)];
 }
 
@@ -328,8 +327,8 @@ struct Chunk {
   }
 };
 
-// kWhole: a workgroup takes all keys of one (sequence, head, block of columns)
-// and writes its output; otherwise a piece of the line.
+// kWhole: a workgroup takes all keys of one (sequence, head, block of columns),
+// the prefix's first, and writes its output; otherwise a piece of the line.
 // NCP, NCO: blocks of 16 columns on the prefix's keys and on a sequence's own.
 template <int D, int NCP, int NCO, bool kWhole>
 __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs a) {
@@ -341,13 +340,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
   const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
+  // keys' scales for the lanes that load those, values' for the others
+  const float* scales = lane < 32 ? a.cache.k_scale : a.cache.v_scale;
   using Front = std::integral_constant<int, NCP>;
   using Own = std::integral_constant<int, NCO>;
   Part p;
+  const auto prefix_part = [&](int begin, int end) __attribute__((always_inline)) {
+    return Part{a.prefix_pages, ((a.prefix_len - 1) >> a.page_shift) + 1, a.prefix_len, begin, end, p.kvh};
+  };
   bool shared = false;
   int b = 0, col0 = 0, cols = 0;
   int64_t segment = 0;
-  // The segment's keys by p, the sums to `segment` or (kWhole) the output.
+  // The segment's keys by p, the sums to `segment` or (kWhole) the output.  kWhole: the prefix's keys in front of them.
   const auto run_segment = [&](auto blocks, int first) __attribute__((always_inline)) {
     constexpr int NC = decltype(blocks)::value;
     // column n of block col0: query head (col % G) of the group, of sequence col / G in the prefix
@@ -356,15 +360,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
       head = p.kvh * a.group + (shared ? col0 + col - seq * a.group : col0 + col);
     };
     Running<D, NC> run;
-  #pragma unroll
+#pragma unroll
     for (int n = 0; n < NC; ++n) {
       run.m[n] = kNoScore;
       run.l[n] = 0.0f;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) run.o[n][i] = v4f{};
     }
-    int t = p.begin + wave * kKeys;
-    if (t < p.end) {
+    if (kWhole || p.begin + wave * kKeys < p.end) {
       v8bf qf[NC][D / 32];
 #pragma unroll
       for (int n = 0; n < NC; ++n) {
@@ -378,20 +381,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
         }
       }
       bool bad = false;
-      Tile<D> x;
-      int ahead = first;
-      const auto load = [&](int at) __attribute__((always_inline)) {
-        if (shared || a.own_blocks > 1)
-          load_tile<D, false>(a, p, at, ahead, bad, x);
-        else
-          load_tile<D, true>(a, p, at, ahead, bad, x);
-        ahead = pages_of(a, p, at + kStride);
+      const auto walk = [&](const Part& p, bool again, int ahead) __attribute__((always_inline)) {
+        int t = p.begin + wave * kKeys;
+        if (t >= p.end) return;
+        Tile<D> x;
+        const auto load = [&](int at) __attribute__((always_inline)) {
+          if (again)
+            load_tile<D, false>(a, p, scales, at, ahead, bad, x);
+          else
+            load_tile<D, true>(a, p, scales, at, ahead, bad, x);
+          ahead = pages_of(a, p, at + kStride);
+        };
+        load(t);
+        for (; t < p.end; t += kStride)
+          use_tile<D, NC>(a, p, t, x, qf, lds[wave], run, [&]() __attribute__((always_inline)) {
+            if (t + kStride < p.end) load(t + kStride);
+          });
       };
-      load(t);
-      for (; t < p.end; t += kStride)
-        use_tile<D, NC>(a, p, t, x, qf, lds[wave], run, [&]() __attribute__((always_inline)) {
-          if (t + kStride < p.end) load(t + kStride);
-        });
+      if (kWhole && a.prefix_len > 0) {
+        const Part front = prefix_part(0, a.prefix_len);
+        walk(front, true, pages_of(a, front, wave * kKeys));
+      }
+      walk(p, shared || a.own_blocks > 1, first);
       if (bad && a.status && lane == 0) atomicOr(a.status, MOE_DEV_BAD_PAGE);
     }
 
@@ -544,8 +555,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_decode_kernel(DecodeArgs 
     p.begin = __builtin_amdgcn_readfirstlane(found.begin);
     p.end = __builtin_amdgcn_readfirstlane(found.end);
     segment = p.kvh * line.segments + piece + (uint32_t)__builtin_amdgcn_readfirstlane(found.pair);
-    p.pages = shared ? a.prefix_pages : a.pages + (int64_t)b * a.width;
-    p.width = shared ? ((a.prefix_len - 1) >> a.page_shift) + 1 : a.width;
+    if (shared) {
+      p = prefix_part(p.begin, p.end);
+    } else {
+      p.pages = a.pages + (int64_t)b * a.width;
+      p.width = a.width;
+    }
     const int first = pages_of(a, p, p.begin + wave * kKeys);
     if (NCP != NCO && shared)
       run_segment(Front{}, first);
@@ -629,10 +644,23 @@ struct DecodePlan {
   size_t o_bytes, ml_bytes, start_bytes;
 };
 
-// Steps up to which a sequence's keys stay with one workgroup where there is no
-// prefix: a second launch and its trip through memory take about as long as 5
-// steps.
-constexpr int kWholeSteps = 5;
+// Whether one launch, in which a workgroup walks all keys of a sequence and head,
+// the prefix's for each sequence anew, is faster than equal pieces and a join.
+// Estimates in us, of D = 128 (D = 64 is quicker on both sides).  One launch: 0.9 a
+// step, more when more than 256 workgroups share the card (a sequence's own steps,
+// most of them fewer than the longest's, when more than 384).  Two: 5 us more to
+// begin with, 6 with a prefix, what a sequence costs to begin and end, and the
+// pieces' steps, a prefix's with twice the columns.  32 heads over 8, one launch
+// against two: 1 sequence of 512 keys 6.8 against 8.2, of 1024 10.6 against 8.4; 32
+// of up to 1024 11.9 against 14.6, of up to 2048 19.3 against 18.6; 48 of up to 500
+// behind 120 shared ones 11.5 against 16.4, of up to 250 behind 1500 23 against 19.
+bool whole_is_faster(const DecodePlan& p, const moe_attn_dims_t& d, int32_t B, int32_t own_steps, int32_t prefix_steps) {
+  const double groups = (double)p.workgroups;
+  const double line = 2.0 * p.prefix_blocks * prefix_steps + (double)p.own_blocks * B * own_steps;
+  const double one = 3.2 + 0.9 * (own_steps * std::max(1.0, groups / 384) + prefix_steps * std::max(1.0, groups / 256));
+  const double two = (prefix_steps > 0 ? 9.5 : 8.2) + 3.2 * groups / 512 + 0.9 * line * d.kv_heads / 512;
+  return one <= two;
+}
 
 DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int32_t prefix_len) {
   DecodePlan p{};
@@ -645,9 +673,8 @@ DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int
   p.own_blocks = (group + 16 * p.own - 1) / (16 * p.own);
   p.prefix_blocks = prefix_len > 0 ? (int)((all + 16 * p.front - 1) / (16 * p.front)) : 0;
   const int64_t own_pairs = (int64_t)p.own_blocks * B;
-  const int64_t own_steps = ((int64_t)max_len + kStride - 1) / kStride;
-  p.whole = prefix_len == 0 && own_steps <= kWholeSteps;
   p.workgroups = own_pairs * d.kv_heads;
+  p.whole = whole_is_faster(p, d, B, steps_of(max_len), steps_of(prefix_len));
   if (!p.whole) {
     const int64_t steps = own_pairs * steps_of(max_len) + (int64_t)p.prefix_blocks * steps_of(prefix_len);
     // Two workgroups a CU (64 ragged contexts: 77 us with 512 workgroups, 81 with 768, 84 with 1536; one context of 65536:

@@ -289,3 +289,73 @@ def test_values_of_extreme_sizes(moe, power):
     got = run(moe, (4, 1, 64), q, cache, [n], 0.1)
     ref, bound = reference(cache, qv, 1, 0.1, 0)
     check(got, ref, bound, f"values times 2^{power}")
+
+
+def one_launch(moe, dims, batch, longest, prefix):
+    return moe.moe_attn_decode_workspace(moe.MoeAttnDims(*dims), batch, longest, prefix) == 0
+
+
+@pytest.mark.parametrize("dims", [(8, 2, 128), (40, 2, 64), (4, 1, 64)])
+@pytest.mark.parametrize("prefix,longest,one", [
+    (1, 512, True), (127, 1, True), (129, 384, True), (300, 256, True), (512, 128, True), (513, 0, True), (512, 129, True),
+    (1024, 300, False), (512, 700, False), (1290, 0, False), (0, 1024, False)])
+def test_one_launch_and_two(moe, dims, prefix, longest, one):
+    """Few steps of 128 keys, the prefix's among them, take one launch and no workspace."""
+    rng = np.random.default_rng(prefix + longest)
+    hq, hkv, dim = dims
+    lens = [longest, 0, min(longest, 1), longest // 2]
+    assert one_launch(moe, dims, len(lens), longest, prefix) == one
+    cache = Cache(moe, rng, lens + [prefix], hkv, dim, 32)
+    q, qv = bf16(rng.standard_normal((len(lens), hq, dim)))
+    scale = 1 / math.sqrt(dim)
+    out = run(moe, dims, q, cache, lens, scale, prefix, max_len=longest)
+    ref, bound = reference(cache, qv, len(lens), scale, prefix)
+    check(out, ref, bound, f"{dims} prefix {prefix} longest {longest}")
+
+
+ODD = [0, 1, 15, 16, 17, 31, 33, 127, 128, 129]
+TWO = [
+    ((8, 2, 128), ODD, 16, 1100),
+    ((8, 2, 64), ODD, 64, 1500),
+    ((8, 1, 128), [5, 90, 0, 64, 1, 1, 1, 300], 16, 1157),   # 64 rows on the prefix
+    ((28, 4, 128), [30] * 33, 32, 1700),                     # 231 rows on the prefix
+    ((40, 2, 64), [17, 3], 16, 1300),                        # more than one product's columns for one sequence
+    ((34, 1, 128), [77, 2000], 16, 0),
+    ((4, 2, 64), [7 * i % 90 for i in range(150)] + [4000], 16, 0),
+    ((8, 2, 128), [5 * i % 70 for i in range(130)] + [3000, 0], 32, 300),
+]
+
+
+@pytest.mark.parametrize("dims,lens,page,prefix", TWO)
+def test_pieces_of_a_line(moe, dims, lens, page, prefix):
+    assert not one_launch(moe, dims, len(lens), max(lens), prefix)
+    rng = np.random.default_rng(33)
+    hq, hkv, dim = dims
+    cache = Cache(moe, rng, list(lens) + ([prefix] if prefix else []), hkv, dim, page)
+    q, qv = bf16(rng.standard_normal((len(lens), hq, dim)))
+    scale = 1 / math.sqrt(dim)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = run(moe, dims, q, cache, lens, scale, prefix, status=status)
+    ref, bound = reference(cache, qv, len(lens), scale, prefix)
+    check(got, ref, bound, f"{dims} {len(lens)} sequences page {page} prefix {prefix}")
+    assert int(status.item()) == 0
+
+
+def test_a_longer_call_never_needs_less_workspace(moe):
+    """A workspace for the longest context serves shorter ones."""
+    for dims in ((8, 2, 128), (32, 8, 128), (40, 2, 64), (16, 16, 64), (64, 1, 128)):
+        for batch in (1, 7, 64, 500, 4000):
+            for prefix in (0, 100, 5000):
+                need = [moe.moe_attn_decode_workspace(moe.MoeAttnDims(*dims), batch, n, prefix) for n in range(0, 9000, 64)]
+                assert need == sorted(need), (dims, batch, prefix)
+
+
+def test_a_bad_page_of_a_short_prefix_is_reported(moe):
+    rng = np.random.default_rng(5)
+    cache = Cache(moe, rng, [20, 3, 100], 2, 64, 32)
+    q, _ = bf16(rng.standard_normal((2, 4, 64)))
+    for page in (-1, cache.dev.n_pages, 1 << 30):
+        cache.table[2, 1] = page
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        run(moe, (4, 2, 64), q, cache, [20, 3], 0.125, 100, status=status)
+        assert int(status.item()) == moe.MOE_DEV_BAD_PAGE
