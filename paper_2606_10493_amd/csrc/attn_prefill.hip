@@ -137,9 +137,13 @@ __device__ __forceinline__ void stage(const uint16_t* base, int64_t stride, int 
   }
 }
 
-template <int D, int WAVES>
+// kSplit: the two halves of the waves take the same rows, one the even key tiles
+// and the other the odd ones, and their sums are joined at the end: half the rows
+// a workgroup and half the steps, for launches that leave CUs without work.
+template <int D, int WAVES, bool kSplit>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs a) {
-  constexpr int kTileRows = kWaveRows * WAVES, kTileBytes = kKeys * D * 2;
+  constexpr int kHalf = WAVES / 2;
+  constexpr int kTileRows = kWaveRows * (kSplit ? kHalf : WAVES), kTileBytes = kKeys * D * 2;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRing][kTileBytes];  // keys, values
 
   const uint32_t item = blockIdx.x / (uint32_t)a.kv_heads;
@@ -151,6 +155,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
 
   const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool late = wave >= kHalf;
+  const int wave_row = kWaveRows * (kSplit && late ? wave - kHalf : wave);  // of the tile, the wave's first
   const uint32_t group = a.group, n_rows = (uint32_t)lq * group;
   const uint32_t row0 = (uint32_t)(rt.n_tiles - 1 - rt.local) * kTileRows;  // a sequence's longest rows first
   // row i of the tile, i < kTileRows: its token and head (rows behind the sequence's last are that row)
@@ -161,16 +167,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     head = kvh * group + (n - t * group);
   };
   int tok, head;
-  row_of(wave * kWaveRows + col, tok, head);
-  const bool live = (uint32_t)(wave * kWaveRows + col) <= last_row;
+  row_of(wave_row + col, tok, head);
+  const bool live = (uint32_t)(wave_row + col) <= last_row;
   // the last key that this row sees, that the tile's first row sees and that its last row sees
-  const int limit = min(a.causal ? tok + lk - lq : lk - 1, lk - 1);
+  int limit = min(a.causal ? tok + lk - lq : lk - 1, lk - 1);
   const int first_limit = min(a.causal ? (int)tok0 + lk - lq : lk - 1, lk - 1);
   const int tile_last = a.causal ? (int)((row0 + last_row) / group) + lk - lq : lk - 1;
   const int n_key_tiles = tile_last < 0 ? 0 : tile_last / kKeys + 1;
   // this part's tiles
   const int kt0 = min(part * a.part_tiles, n_key_tiles);
   const int kt1 = part == a.parts - 1 ? n_key_tiles : min(kt0 + a.part_tiles, n_key_tiles);
+  if (kSplit) limit = min(limit, kt1 * kKeys - 1);  // one half may take a tile behind the last
 
   v16f o[D / 32];
 #pragma unroll
@@ -267,23 +274,33 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     // Every vector phase ends by waiting for all fetches but its own, so a fetch has two phases or more to
     // arrive, and the barrier after that wait comes before the first read.  (Behind the end the last row is fetched;
     // the scores of the tile behind the last are not used.)
-    const bool late = wave >= WAVES / 2;
+    //
+    // kSplit: phase t multiplies tile t, in the early half for even t (counted from kt0) and in the late one for odd t,
+    // while the other half weighs tile t + 1.  Keys t + 2 and values t are read in phase t (the first of those keys at the
+    // end of phase t - 1) and by nothing else.  Both halves fetch keys t + 5 and values t + 3 at the start of phase t, to
+    // the places of keys t + 1 and values t - 1, and every phase ends by waiting for all fetches but its own: they have two
+    // phases to arrive, and keys t + 5 one more before the end of phase t + 2.
     v8bf ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
     const auto step = [&](auto masked, int kt) __attribute__((always_inline)) {
-      const int ft = late ? kt : kt - 1;
+      constexpr int kNext = kSplit ? 2 : 1;  // the half's next tile
+      const int ft = kSplit || late ? kt : kt - 1;
       fetch_k(ft + kRing);
-      fetch_v(ft + kRing - 1);
+      fetch_v(ft + kRing - kNext);
       weigh(masked, kt);
       // opaque: the operands' places are computed in every step, which costs less than the registers to keep them
-      int kp = k_place + (kt + 1) % kRing * kTileBytes, vp = v_place + kt % kRing * kTileBytes;
+      int kp = k_place + (kt + kNext) % kRing * kTileBytes, vp = v_place + kt % kRing * kTileBytes;
       asm volatile("" : "+v"(kp), "+v"(vp));
       v8bf ops[kAhead + 1];
 #pragma unroll
       for (int f = 0; f < kAhead; ++f) ops[f] = operand(kp, vp, f);
       __builtin_amdgcn_sched_barrier(0);
       asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kCalls) : "memory");
+      if (kSplit) {
+        fetch_k(kt + kRing + 1);
+        fetch_v(kt + kRing - 1);
+      }
       __builtin_amdgcn_s_setprio(1);
       __builtin_amdgcn_sched_barrier(0);
       s[0] = s[1] = v16f{};
@@ -302,7 +319,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
         __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_s_setprio(0);
-      asm volatile("s_barrier" : : : "memory");
+      if (kSplit)
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kCalls) : "memory");
+      else
+        asm volatile("s_barrier" : : : "memory");
       __builtin_amdgcn_sched_barrier(0);
     };
 
@@ -315,38 +335,69 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
       const int row = i * (kWaveRows / kQCalls) + lane / (D / 8);
       const int c = (staged<D>(row, lane % (D / 8)) % (D * 2)) / 16;
       int t, hd;
-      row_of(wave * kWaveRows + row, t, hd);
+      row_of(wave_row + row, t, hd);
       async_load_1k(a.q + (int64_t)(q0 + t) * a.q_stride + hd * D + 8 * c, q_lds + 1024 * i);
     }
     fetch_k(kt0);
     fetch_k(kt0 + 1);
     fetch_k(kt0 + 2);
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kCalls / 2) : "memory");
+    if (kSplit) fetch_k(kt0 + 3);
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kSplit ? kCalls : kCalls / 2) : "memory");
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
       qf[i] = *(__attribute__((address_space(3))) const v8bf*)(uintptr_t)(q_lds + staged<D>(col, 2 * i + h));
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
     fetch_v(kt0);
     fetch_v(kt0 + 1);
+    const int first = kSplit && late ? kt0 + 1 : kt0;  // the half's first tile
     s[0] = s[1] = v16f{};
 #pragma unroll
     for (int f = 0; f < kK; ++f)
-      s[f & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(k_place + kt0 % kRing * kTileBytes, v_place, f), qf[f >> 1],
+      s[f & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(k_place + first % kRing * kTileBytes, v_place, f), qf[f >> 1],
                                                          s[f & 1], 0, 0, 0);
+    // keys kt0 and kt0 + 1 have been read, and keys kt0 + 2 are there
+    if (kSplit) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(3 * kCalls / 2) : "memory");
     if (late) {
-      fetch_k(kt0 + kRing - 1);
+      fetch_k(kSplit ? kt0 + kRing : kt0 + kRing - 1);
       fetch_v(kt0 + kRing - 2);
       asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kCalls) : "memory");
     }
     const int n_free = min((first_limit + 1) / kKeys, kt1);  // tiles before it have no masked key for any row
-    int kt = kt0;
-    for (; kt < n_free; ++kt) step(std::false_type{}, kt);
-    for (; kt < kt1; ++kt) step(std::true_type{}, kt);
+    int kt = first;
+    const int end = kSplit ? first + ((kt1 - kt0 + 1) & ~1) : kt1;  // both halves take as many steps
+    for (; kt < min(n_free, end); kt += kSplit ? 2 : 1) step(std::false_type{}, kt);
+    for (; kt < end; kt += kSplit ? 2 : 1) step(std::true_type{}, kt);
     if (!late) asm volatile("s_barrier" : : : "memory");
     wait_async_and_barrier<0>();  // no fetch is on its way to LDS, and no wave reads from it any more
   }
 
-  const float l = total[0];
+  float l = total[0];
+  if (kSplit) {
+    // the late half's sums by way of LDS to the early half, lane by lane
+    __shared__ float2 late_ml[kHalf][64];
+    v4f* late_o = reinterpret_cast<v4f*>(&lds[0][0][0] + (wave & (kHalf - 1)) * (kWaveRows * D * 4)) + lane;
+    if (late) {
+      late_ml[wave - kHalf][lane] = make_float2(m, l);
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) late_o[64 * (4 * i + j)] = v4f{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
+    }
+    __syncthreads();
+    if (late) return;
+    const float2 ml = late_ml[wave][lane];
+    const float top = fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - top), e = __builtin_amdgcn_exp2f(ml.x - top);
+    m = top;
+    l = l * f + ml.y * e;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const v4f x = late_o[64 * (4 * i + j)];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[i][4 * j + k] = o[i][4 * j + k] * f + x[k] * e;
+      }
+  }
   // Whole rows go out: a lane has pieces of 4 elements of one row, which the wave's part of LDS turns into rows (with
   // stores of 16 or 32 bytes a row the eight prompts took 168 us, with whole rows in and out 152).
   const int64_t heads = a.kv_heads * group;
@@ -366,9 +417,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
 #pragma unroll
     for (int i = 0; i < kWaveRows * kPieces / 64; ++i) {
       const int at = 64 * i + lane, rr = at / kPieces, c = at % kPieces;
-      if ((uint32_t)(wave * kWaveRows + rr) > last_row) continue;
+      if ((uint32_t)(wave_row + rr) > last_row) continue;
       int t, hd;
-      row_of(wave * kWaveRows + rr, t, hd);
+      row_of(wave_row + rr, t, hd);
       *reinterpret_cast<float4*>(a.part_o + (((q0 + (int64_t)t) * heads + hd) * a.parts + part) * D + 4 * c) =
           *reinterpret_cast<const float4*>(turn + rr * (D * 4) + ((c ^ (rr & 15)) * 16));
     }
@@ -386,9 +437,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
 #pragma unroll
   for (int i = 0; i < kWaveRows * kPieces / 64; ++i) {
     const int at = 64 * i + lane, rr = at / kPieces, c = at % kPieces;
-    if ((uint32_t)(wave * kWaveRows + rr) > last_row) continue;
+    if ((uint32_t)(wave_row + rr) > last_row) continue;
     int t, hd;
-    row_of(wave * kWaveRows + rr, t, hd);
+    row_of(wave_row + rr, t, hd);
     *reinterpret_cast<uint4*>(a.out + ((q0 + (int64_t)t) * heads + hd) * D + 8 * c) =
         *reinterpret_cast<const uint4*>(turn + staged<D>(rr, c));
   }
@@ -426,31 +477,43 @@ constexpr int kWaves = 8;
 
 struct PrefillPlan {
   int64_t tiles;  // bound on the row tiles
+  bool split;     // waves of a workgroup share rows
   int parts, part_tiles;
   size_t o_bytes, ml_bytes;
 };
 
-// How many parts the keys are cut into: the number whose estimated time is the
-// least.  A CU runs one workgroup at a time; one takes about 5 us and 1.4 us for
-// each of its key tiles (D = 128).  Joining costs a launch, 5 us, and the parts'
-// sums go to memory and back at about 4 TB/s.  509 tokens of 32 heads behind 8192
-// keys are 64 workgroups of 136 tiles: 184 us whole, 71 us in four parts and 8 us to join them.
+// The height of the row tiles and the number of parts that the keys are cut into:
+// those whose estimated time is the least.  A CU runs one workgroup at a time; one
+// takes about 5 us and a step for each of its key tiles, or 6.3 us and a longer
+// step for each two of them.  Joining parts costs a launch, 5 us, and their sums go
+// to memory and back at about 4 TB/s.  Whole rows against halves: 1040 tokens of 16
+// heads of 64 23.7 and 17.1 us, 206 tokens of 40 heads over 8 of 128 behind 320
+// keys 18.5 and 15.5; where the card is full, eight prompts of up to 2048 tokens,
+// 157 and 208 (twice the keys go through LDS).  509 tokens of 32 heads over 8
+// behind 8192 keys are 64 workgroups of 136 tiles: 184 us whole, 72 us in four
+// parts and 8 us to join them.
 PrefillPlan plan_prefill(const moe_attn_dims_t& d, int32_t B, int32_t T_q, int32_t max_k) {
   PrefillPlan p{};
   const int group = d.q_heads / d.kv_heads;
-  p.tiles = (int64_t)T_q * group / (kWaves * kWaveRows) + B;  // sequences may each add a part of one
-  const int64_t items = p.tiles * d.kv_heads, rows = (int64_t)T_q * d.q_heads;
+  const int64_t rows = (int64_t)T_q * d.q_heads;
   const int key_tiles = max_k / kKeys + 1;
+  const double start[2] = {5.0, 6.3};
+  const double step[2] = {d.head_dim == 128 ? 1.45 : 1.1, d.head_dim == 128 ? 1.8 : 1.25};
   double best = 0.0;
-  for (int parts = 1; parts <= 16; ++parts) {
-    const int part_tiles = (key_tiles + parts - 1) / parts;
-    const double rounds = (double)((items * parts + 255) / 256);
-    double us = rounds * (5.0 + 1.4 * part_tiles);
-    if (parts > 1) us += 5.0 + (double)rows * parts * d.head_dim * 8 / 4e6;
-    if (parts == 1 || us < best) {
-      best = us;
-      p.parts = parts;
-      p.part_tiles = part_tiles;
+  for (int split = 0; split < 2; ++split) {
+    const int64_t tiles = (int64_t)T_q * group / (kWaves * kWaveRows >> split) + B;  // sequences may each add a part of one
+    for (int parts = 1; parts <= 16; ++parts) {
+      const int part_tiles = (key_tiles + parts - 1) / parts;
+      const double rounds = (double)((tiles * d.kv_heads * parts + 255) / 256);
+      double us = rounds * (start[split] + step[split] * ((part_tiles + split) >> split));
+      if (parts > 1) us += 5.0 + (double)rows * parts * d.head_dim * 8 / 4e6;
+      if (p.parts == 0 || us < best) {
+        best = us;
+        p.tiles = tiles;
+        p.split = split != 0;
+        p.parts = parts;
+        p.part_tiles = part_tiles;
+      }
     }
   }
   if (p.parts > 1) {
@@ -468,7 +531,10 @@ moe_status_t launch_prefill(const PrefillArgs& a, const PrefillPlan& p, hipStrea
   constexpr int kJoinRows = 256 / (D / 4);
   if (items * kWaves * 64 >= (int64_t)1 << 32 || (rows / kJoinRows + 1) * 256 >= (int64_t)1 << 32)
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_prefill: %lld row tiles", (long long)items);
-  MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
+  if (p.split)
+    MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves, true>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
+  else
+    MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves, false>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
   if (a.parts > 1)
     MOE_LAUNCH("attn_prefill_join", attn_prefill_join_kernel<D>, dim3((unsigned)((rows + kJoinRows - 1) / kJoinRows)),
                dim3(256), 0, stream, a, rows);

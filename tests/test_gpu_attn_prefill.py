@@ -235,3 +235,37 @@ def test_replays_from_a_hip_graph(moe, past):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out.view(torch.int16), ref.view(torch.int16))
+
+
+@pytest.mark.parametrize("max_k", [0, 640, 20000])
+@pytest.mark.parametrize("dims,lens,more,causal", CASES)
+def test_every_way_to_share_the_work(moe, dims, lens, more, causal, max_k):
+    """The announced longest length alone chooses between tiles of whole and of shared rows, and cuts keys into parts."""
+    rng = np.random.default_rng(35)
+    hq, hkv, dim = dims
+    keys = [max(0, n + more) if n else 0 for n in lens]
+    cu_q, cu_k = offsets(lens), offsets(keys)
+    q, qv = bf16(rng.standard_normal((cu_q[-1], hq, dim)))
+    k, kv = bf16(rng.standard_normal((cu_k[-1], hkv, dim)))
+    v, vv = bf16(rng.standard_normal((cu_k[-1], hkv, dim)))
+    scale = 1 / math.sqrt(dim)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = run(moe, dims, q, k, v, cu_q, cu_k, max_k, scale, causal, status)
+    ref, bound = ao.packed_attention(qv, kv, vv, cu_q, cu_k, scale, causal)
+    check(got, ref, bound, f"{dims} {lens} {more:+d} causal={causal} max_k={max_k}")
+    assert int(status.item()) == 0
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("keys", [1, 63, 64, 65, 128, 129, 191, 192, 193, 256, 257, 320, 321, 449, 513])
+def test_key_tiles_of_both_halves(moe, dim, keys):
+    """Odd and even numbers of key tiles, the last one full or not: rows shared by two halves of the waves."""
+    rng = np.random.default_rng(keys)
+    cu_q, cu_k = offsets([5, 150]), offsets([keys, keys])
+    q, qv = bf16(rng.standard_normal((155, 4, dim)))
+    k, kv = bf16(rng.standard_normal((2 * keys, 2, dim)))
+    v, vv = bf16(rng.standard_normal((2 * keys, 2, dim)))
+    for causal in (False, True):
+        got = run(moe, (4, 2, dim), q, k, v, cu_q, cu_k, 640, 0.1, causal)
+        ref, bound = ao.packed_attention(qv, kv, vv, cu_q, cu_k, 0.1, causal)
+        check(got, ref, bound, f"{keys} keys of {dim} causal={causal}")
