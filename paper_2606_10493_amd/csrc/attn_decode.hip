@@ -679,7 +679,11 @@ DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int
     const int64_t steps = own_pairs * steps_of(max_len) + (int64_t)p.prefix_blocks * steps_of(prefix_len);
     // Two workgroups a CU (64 ragged contexts: 77 us with 512 workgroups, 81 with 768, 84 with 1536; one context of 65536:
     // 27, 29 and 31 us, and a longer join).
-    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>(512 / d.kv_heads, steps));
+    // Fewer where a row would have many segments of few steps: steps / pieces in the first launch and pieces / runs of keys
+    // in the second cost about as much at this number (16 heads over 1, one context of 65536, 80 pieces 11.6 + 5.3 us, 512
+    // 8.1 + 24.4; 28 over 4, two of up to 16583, 80 pieces 8.6 + 6.4, 128 9.1 + 8.2).
+    const int64_t few = (int64_t)ceil(3.5 * sqrt((double)steps * (double)(p.prefix_blocks + own_pairs)));
+    p.pieces = (int)std::max<int64_t>(1, std::min(std::min<int64_t>(512 / d.kv_heads, few), steps));
     p.workgroups = (int64_t)p.pieces * d.kv_heads;
     const size_t places = (size_t)d.kv_heads * (p.pieces + p.prefix_blocks + own_pairs) * 16 * std::max(p.front, p.own);
     p.o_bytes = (places * d.head_dim * sizeof(float) + 255) & ~(size_t)255;
