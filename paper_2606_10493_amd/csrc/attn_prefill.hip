@@ -18,10 +18,13 @@
 // to 1 (error 2.0e-3 of the result's norm, 1.6e-3 of it the output's rounding).
 //
 // Bound by the matrix cores, 4 * head_dim flops per row and key, and by the power
-// that they draw when all are busy (the clock falls to 1.7 - 2.0 GHz).  16384
-// causal tokens of 32 heads of 128: 1.85 ms, 1190 TFLOP/s, where the largest
-// library products reach 1340.  Eight prompts of 357 to 2048 tokens: 148 us, 830
-// TFLOP/s; their 1248 workgroups of unequal length end unevenly.
+// that they draw when all are busy (the clock falls to 1.6 - 2.0 GHz).  16384
+// causal tokens of 32 heads of 128: 1.88 ms, 1170 TFLOP/s, where the largest
+// library products reach 1340.  Eight prompts of 357 to 2048 tokens: 150 us, 820
+// TFLOP/s; their 1248 workgroups of unequal length end unevenly.  Where there are
+// fewer workgroups than CUs, a call takes 5 us and 1.4 us for each key tile of the
+// longest rows: rows are then shared by two halves of a workgroup's waves, and keys
+// cut into parts.
 #include <math.h>
 
 #include <algorithm>
