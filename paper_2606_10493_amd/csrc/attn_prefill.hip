@@ -148,6 +148,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
   constexpr int kHalf = WAVES / 2;
   constexpr int kTileRows = kWaveRows * (kSplit ? kHalf : WAVES), kTileBytes = kKeys * D * 2;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRing][kTileBytes];  // keys, values
+  __shared__ __attribute__((aligned(1024))) uint8_t late_q[kHalf * kWaveRows * D * 2];
 
   const uint32_t item = blockIdx.x / (uint32_t)a.kv_heads;
   const int kvh = blockIdx.x - item * a.kv_heads, tile = item / (uint32_t)a.parts, part = item - tile * a.parts;
@@ -289,22 +290,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     // t + kRing and values t + kRing - 1 take their places, fetched in phase 2 t by the late half and in phase 2 t + 1 by
     // the early one, at the start of their vector phases.  They are first read at the end of phase 2 (t + kRing) - 3.
     // Every vector phase ends by waiting for all fetches but its own, so a fetch has two phases or more to
-    // arrive, and the barrier after that wait comes before the first read.  (Behind the end the last row is fetched;
-    // the scores of the tile behind the last are not used.)
+    // arrive, and the barrier after that wait comes before the first read.  (The scores of the tile behind the last are
+    // not used.)
     //
     // kSplit: phase t multiplies tile t, in the early half for even t (counted from kt0) and in the late one for odd t,
     // while the other half weighs tile t + 1.  Keys t + 2 and values t are read in phase t (the first of those keys at the
     // end of phase t - 1) and by nothing else.  Both halves fetch keys t + 5 and values t + 3 at the start of phase t, to
     // the places of keys t + 1 and values t - 1, and every phase ends by waiting for all fetches but its own: they have two
     // phases to arrive, and keys t + 5 one more before the end of phase t + 2.
+    const int end = kSplit ? kt0 + ((kt1 - kt0 + 1) & ~1) : kt1;  // kSplit: both halves take as many steps
     v8bf ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
     const auto step = [&](auto masked, int kt) __attribute__((always_inline)) {
       constexpr int kNext = kSplit ? 2 : 1;  // the half's next tile
       const int ft = kSplit || late ? kt : kt - 1;
-      fetch_k(ft + kRing);
-      fetch_v(ft + kRing - kNext);
+      // nothing behind the end, but where the branch costs more (kSplit: two prompts of up to 1950 tokens 32.7 us without,
+      // 34.8 with)
+      const bool more = kSplit || ft + kRing - kNext < end;
+      if (more) {
+        fetch_k(ft + kRing);
+        fetch_v(ft + kRing - kNext);
+      }
       weigh(masked, kt);
       // opaque: the operands' places are computed in every step, which costs less than the registers to keep them
       int kp = k_place + (kt + kNext) % kRing * kTileBytes, vp = v_place + kt % kRing * kTileBytes;
@@ -313,6 +320,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
 #pragma unroll
       for (int f = 0; f < kAhead; ++f) ops[f] = operand(kp, vp, f);
       __builtin_amdgcn_sched_barrier(0);
+      if (!more) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
       asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kCalls) : "memory");
       if (kSplit) {
         fetch_k(kt + kRing + 1);
@@ -342,9 +350,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
       __builtin_amdgcn_sched_barrier(0);
     };
 
-    // The wave's rows of queries come the way that keys do, whole rows straight into LDS (its part of the values' ring,
-    // which is empty yet), and from there as operands.
-    const int q_lds = lds0 + kRing * kTileBytes + wave * (kWaveRows * D * 2);
+    // The wave's rows of queries come the way that keys do, whole rows straight into LDS (the early half's into the places
+    // of values kt0 + 2 and kt0 + 3, the late one's into a place of their own), and from there as operands.
+    constexpr int kQBytes = kWaveRows * D * 2;
+    static_assert(kHalf * kQBytes == 2 * kTileBytes, "half the waves' queries are two tiles");
+    const int q_lds = late ? lds_address(late_q) + (wave - kHalf) * kQBytes
+                           : lds0 + (kRing + (kt0 + 2 + wave / 2) % kRing) * kTileBytes + (wave & 1) * kQBytes;
     constexpr int kQCalls = kWaveRows * D * 2 / 1024;
 #pragma unroll
     for (int i = 0; i < kQCalls; ++i) {
@@ -357,14 +368,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     fetch_k(kt0);
     fetch_k(kt0 + 1);
     fetch_k(kt0 + 2);
+    fetch_v(kt0);
+    fetch_v(kt0 + 1);
     if (kSplit) fetch_k(kt0 + 3);
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kSplit ? kCalls : kCalls / 2) : "memory");
+    // queries, keys kt0 and keys kt0 + 1
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kSplit ? 2 * kCalls : 3 * kCalls / 2) : "memory");
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
       qf[i] = *(__attribute__((address_space(3))) const v8bf*)(uintptr_t)(q_lds + staged<D>(col, 2 * i + h));
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
-    fetch_v(kt0);
-    fetch_v(kt0 + 1);
     const int first = kSplit && late ? kt0 + 1 : kt0;  // the half's first tile
     s[0] = s[1] = v16f{};
 #pragma unroll
@@ -380,7 +392,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     }
     const int n_free = min((first_limit + 1) / kKeys, kt1);  // tiles before it have no masked key for any row
     int kt = first;
-    const int end = kSplit ? first + ((kt1 - kt0 + 1) & ~1) : kt1;  // both halves take as many steps
     for (; kt < min(n_free, end); kt += kSplit ? 2 : 1) step(std::false_type{}, kt);
     for (; kt < end; kt += kSplit ? 2 : 1) step(std::true_type{}, kt);
     if (!late) asm volatile("s_barrier" : : : "memory");
@@ -394,10 +405,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
   }
   if (kSplit) {
     // the late half's sums by way of LDS to the early half, lane by lane
-    __shared__ float2 late_ml[kHalf][64];
+    float2* late_ml = reinterpret_cast<float2*>(late_q) + (wave & (kHalf - 1)) * 64 + lane;
     v4f* late_o = reinterpret_cast<v4f*>(&lds[0][0][0] + (wave & (kHalf - 1)) * (kWaveRows * D * 4)) + lane;
     if (late) {
-      late_ml[wave - kHalf][lane] = make_float2(m, l);
+      *late_ml = make_float2(m, l);
 #pragma unroll
       for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -405,7 +416,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     }
     __syncthreads();
     if (late) return;
-    const float2 ml = late_ml[wave][lane];
+    const float2 ml = *late_ml;
     const float top = fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - top), e = __builtin_amdgcn_exp2f(ml.x - top);
     m = top;
     l = l * f + ml.y * e;
