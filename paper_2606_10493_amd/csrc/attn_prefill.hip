@@ -396,6 +396,38 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     for (; kt < end; kt += kSplit ? 2 : 1) step(std::true_type{}, kt);
     if (!late) asm volatile("s_barrier" : : : "memory");
     wait_async_and_barrier<0>();  // no fetch is on its way to LDS, and no wave reads from it any more
+
+    // A product multiplies a hidden key's value by 0, which an infinite or NaN value does not survive.  If a sum is not
+    // finite, the wave takes its sums again, key by key, from what each row sees; maxima and denominators stand.
+    float finite = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) finite = fmaf(o[i][j], 0.0f, finite);
+    if (__any(finite != 0.0f)) {
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) o[i] = v16f{};
+      for (int tile = first; tile < kt1; tile += kSplit ? 2 : 1)
+        for (int j = tile * kKeys; j <= min(tile * kKeys + kKeys - 1, tile_last); ++j) {
+          float score = 0.0f;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            const v8bf key = *reinterpret_cast<const v8bf*>(kbase + j * a.k_stride + 16 * i + 8 * h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) score = fmaf((float)qf[i][e], (float)key[e], score);
+          }
+          score += __shfl_xor(score, 32, 64);
+          const float w = (float)(__bf16)__builtin_amdgcn_exp2f(fmaf(score, a.c, -m));
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) {
+            const uint2 x = *reinterpret_cast<const uint2*>(vbase + j * a.v_stride + 8 * i + 4 * h);
+            const float v[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
+                                __uint_as_float(x.y & 0xffff0000u)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i / 4][4 * (i % 4) + e] += j <= limit ? w * v[e] : 0.0f;
+          }
+        }
+    }
   }
 
   float l = total[0];
@@ -512,7 +544,7 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, i
     o *= f;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const bool there = x[i].y > 0.0f;  // a part without keys has written no sums
+      const bool there = x[i].y != 0.0f;  // a part without keys has written no sums; one with NaN keeps it
       const float e = there ? __builtin_amdgcn_exp2f(x[i].x - m) : 0.0f;
       l += x[i].y * e;
 #pragma unroll

@@ -269,3 +269,36 @@ def test_key_tiles_of_both_halves(moe, dim, keys):
         got = run(moe, (4, 2, dim), q, k, v, cu_q, cu_k, 640, 0.1, causal)
         ref, bound = ao.packed_attention(qv, kv, vv, cu_q, cu_k, 0.1, causal)
         check(got, ref, bound, f"{keys} keys of {dim} causal={causal}")
+
+
+@pytest.mark.parametrize("max_k", [0, 640, 20000])
+@pytest.mark.parametrize("dims,lens,past", [((8, 2, 128), [300], 0), ((4, 4, 64), [70, 200], 0), ((4, 1, 128), [37, 5], 150)])
+def test_hidden_keys_and_values_may_hold_anything(moe, dims, lens, past, max_k):
+    """Infinite and NaN elements of keys and values stay with the rows that see them; a value's with its column."""
+    rng = np.random.default_rng(36)
+    hq, hkv, dim = dims
+    keys = [n + past for n in lens]
+    cu_q, cu_k = offsets(lens), offsets(keys)
+    q, qv = bf16(rng.standard_normal((cu_q[-1], hq, dim)))
+    k, kv = bf16(rng.standard_normal((cu_k[-1], hkv, dim)))
+    v, vv = bf16(rng.standard_normal((cu_k[-1], hkv, dim)))
+    scale = 1 / math.sqrt(dim)
+    clean_v = vv.copy()
+    touched = np.zeros(qv.shape, bool)
+    for b, n in enumerate(lens):
+        c, a = cu_k[b], cu_q[b]
+        # values: an element of a middle token and of the last one
+        for j, d, x in ((past + n // 2, 3, np.inf), (past + n - 1, dim - 1, np.nan), (past + n - 2, 40, -np.inf)):
+            v[c + j, :, d] = x
+            clean_v[c + j, :, d] = 0.0
+            touched[a + j - past:cu_q[b + 1], :, d] = True
+        # a whole key of the last token: only its own row sees it
+        k[c + past + n - 1] = np.nan
+        touched[cu_q[b + 1] - 1] = True
+    kv = np.nan_to_num(k.double().cpu().numpy())
+    got = run(moe, dims, q, k, v, cu_q, cu_k, max_k, scale).double().cpu().numpy()
+    ref, bound = ao.packed_attention(qv, kv, clean_v, cu_q, cu_k, scale, True)
+    assert np.array_equal(np.isfinite(got), ~touched)
+    worst = float(np.max(np.abs(got - ref)[~touched] / np.maximum(bound, 1e-30)[~touched]))
+    log(f"{dims} {lens} behind {past}, max_k {max_k}: worst error {worst:.3f} of its bound")
+    assert worst <= 1.0
