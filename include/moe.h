@@ -574,7 +574,8 @@ moe_status_t moe_cache_read(moe_attn_dims_t dims, moe_kv_cache_t cache, const in
  * over the keys j of i's own sequence; with causal != 0 over those up to i's
  * place, sequences' ends aligned: query i of lq sees keys 0 .. i + lk - lq (a
  * chunk of queries behind keys that are cached already).  A query that sees no
- * key gets zeros.  Scores, the running maximum and sum and the accumulation are
+ * key gets zeros, and keys and values that a query does not see may hold
+ * anything, NaN too.  Scores, the running maximum and sum and the accumulation are
  * fp32; the softmax's numerators are rounded to bf16 for the product with v (and
  * their sum is that of the rounded ones).
  *
@@ -601,16 +602,17 @@ moe_status_t moe_attn_prefill(moe_attn_dims_t dims, int32_t B, int32_t T_q, int3
  *
  * prefix_pages: device int32, the pages of the first prefix_len tokens that
  * all sequences share (a prompt's prefix written once); NULL with prefix_len
- * 0.  The prefix is read once for the whole batch: every sequence's queries are
- * rows of one product.  page_table: device int32 [B, table_width], entries
- * behind a sequence's last page are not read.  lens: device int32 [B], 0 for
+ * 0.  A long prefix is read once for the whole batch, every sequence's queries
+ * being rows of one product (a short one by each sequence for itself, which
+ * costs less).  page_table: device int32 [B, table_width], entries behind a
+ * sequence's last page are not used.  lens: device int32 [B], 0 for
  * an idle slot (with no prefix either its output is zeros).  A length below 0
  * or beyond table_width pages (or 2^30) is cut and sets MOE_DEV_BAD_LENGTH; a page id
  * outside the cache sets MOE_DEV_BAD_PAGE and leaves the outputs that need it
  * unspecified.  max_len: the longest of lens; it decides how the work is split
  * and nothing else.  q: [B, q_heads, head_dim]; out contiguous, no overlap.
  * ws: moe_attn_decode_workspace(dims, B, max_len, prefix_len) bytes, 256-byte
- * aligned.
+ * aligned; what the longest max_len needs is enough for every shorter one.
  */
 size_t moe_attn_decode_workspace(moe_attn_dims_t dims, int32_t B, int32_t max_len, int32_t prefix_len);
 moe_status_t moe_attn_decode(moe_attn_dims_t dims, int32_t B, const uint16_t* q, int64_t q_stride, moe_kv_cache_t cache,
