@@ -19,8 +19,8 @@
 //
 // Bound by the matrix cores, 4 * head_dim flops per row and key, and by the power
 // that they draw when all are busy (the clock falls to 1.6 - 2.0 GHz).  16384
-// causal tokens of 32 heads of 128: 1.88 ms, 1170 TFLOP/s, where the largest
-// library products reach 1340.  Eight prompts of 357 to 2048 tokens: 150 us, 820
+// causal tokens of 32 heads of 128: 1.86 ms, 1180 TFLOP/s, where the largest
+// library products reach 1340.  Eight prompts of 357 to 2048 tokens: 143 us, 860
 // TFLOP/s; their 1248 workgroups of unequal length end unevenly.  Where there are
 // fewer workgroups than CUs, a call takes 5 us and 1.4 us for each key tile of the
 // longest rows: rows are then shared by two halves of a workgroup's waves, and keys
