@@ -581,7 +581,9 @@ moe_status_t moe_cache_read(moe_attn_dims_t dims, moe_kv_cache_t cache, const in
  *
  * Sequence b: queries cu_q[b] .. cu_q[b+1] - 1 of T_q, keys cu_k[b] ..
  * cu_k[b+1] - 1 of T_k (device int32 [B + 1], not decreasing); offsets that
- * leave the tensors are cut to them and set MOE_DEV_BAD_LENGTH.  Rows
+ * leave the tensors are cut to them.  Any that do, or that decrease, set
+ * MOE_DEV_BAD_LENGTH, also those of a sequence that is left with nothing (a call
+ * with B or T_q 0 launches nothing and looks at nothing).  Rows
  * of out outside all sequences are not written.  max_k: the longest sequence's
  * number of keys; it decides how the work is split and nothing else.  q:
  * [T_q, q_heads, head_dim]; k, v: [T_k, kv_heads, head_dim]; out: contiguous

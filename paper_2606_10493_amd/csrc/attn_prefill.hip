@@ -59,8 +59,17 @@ constexpr int kWaveRows = 32;
 struct RowTile {
   int local, n_tiles;      // place, and the sequence's number of tiles
   int q0, lq, k0, lk;
-  bool cut;                // the offsets leave the tensors
 };
+
+// Reports offsets that leave the tensors or decrease, of sequences without rows too.
+__device__ __forceinline__ void report_offsets(const PrefillArgs& a) {
+  bool bad = false;
+  for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+    const int q_lo = a.cu_q[b], q_hi = a.cu_q[b + 1], k_lo = a.cu_k[b], k_hi = a.cu_k[b + 1];
+    bad |= q_lo < 0 || q_hi > a.T_q || q_lo > q_hi || k_lo < 0 || k_hi > a.T_k || k_lo > k_hi;
+  }
+  if (__any(bad) && (threadIdx.x & 63) == 0) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
+}
 
 // Row tile `tile`, counted over the sequences in order; false behind the last.
 // Every lane of a wave calls it.  32 bits hold the counts: the launch checks
@@ -74,7 +83,6 @@ __device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile_rows, i
     const int q0 = min(max(q_lo, 0), a.T_q), k0 = min(max(k_lo, 0), a.T_k);
     const int lq = base + lane < a.B ? max(min(max(q_hi, 0), a.T_q) - q0, 0) : 0;
     const int lk = max(min(max(k_hi, 0), a.T_k) - k0, 0);
-    const bool cut = q0 != q_lo || q0 + lq != q_hi || k0 != k_lo || k0 + lk != k_hi;
     const int n = (int)(((uint32_t)lq * a.group + tile_rows - 1) / tile_rows);
     const int incl = wave_scan(n);
     const uint64_t past = __ballot(before + incl > tile);
@@ -86,7 +94,6 @@ __device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile_rows, i
       r.lq = __builtin_amdgcn_readlane(lq, w);
       r.k0 = __builtin_amdgcn_readlane(k0, w);
       r.lk = __builtin_amdgcn_readlane(lk, w);
-      r.cut = __builtin_amdgcn_readlane(cut, w);
       return true;
     }
     before += __builtin_amdgcn_readlane(incl, 63);
@@ -150,12 +157,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRing][kTileBytes];  // keys, values
   __shared__ __attribute__((aligned(1024))) uint8_t late_q[kHalf * kWaveRows * D * 2];
 
+  // With a status word the grid has one workgroup more, which looks at the offsets (a sequence that is cut to nothing has
+  // no tile, and the tiles' workgroups need not look behind theirs).
+  if (a.status && blockIdx.x == gridDim.x - 1) {
+    report_offsets(a);
+    return;
+  }
   const uint32_t item = blockIdx.x / (uint32_t)a.kv_heads;
   const int kvh = blockIdx.x - item * a.kv_heads, tile = item / (uint32_t)a.parts, part = item - tile * a.parts;
   RowTile rt;
   if (!find_tile(a, kTileRows, tile, rt)) return;
   const int q0 = rt.q0, lq = rt.lq, k0 = rt.k0, lk = rt.lk;
-  if (rt.cut && a.status && kvh == 0 && part == 0 && threadIdx.x == 0) atomicOr(a.status, MOE_DEV_BAD_LENGTH);
 
   const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -617,12 +629,13 @@ moe_status_t launch_prefill(const PrefillArgs& a, const PrefillPlan& p, hipStrea
   // 8, and all heads' longest rows come first.
   const int64_t items = p.tiles * a.parts * a.kv_heads, rows = (int64_t)a.T_q * a.kv_heads * a.group;
   constexpr int kJoinRows = 256 / (D / 4);
-  if (items * kWaves * 64 >= (int64_t)1 << 32 || (rows / kJoinRows + 1) * 256 >= (int64_t)1 << 32)
+  if ((items + 1) * kWaves * 64 >= (int64_t)1 << 32 || (rows / kJoinRows + 1) * 256 >= (int64_t)1 << 32)
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_prefill: %lld row tiles", (long long)items);
+  const dim3 grid((unsigned)items + (a.status ? 1 : 0));
   if (p.split)
-    MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves, true>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
+    MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves, true>), grid, dim3(64 * kWaves), 0, stream, a);
   else
-    MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves, false>), dim3((unsigned)items), dim3(64 * kWaves), 0, stream, a);
+    MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves, false>), grid, dim3(64 * kWaves), 0, stream, a);
   if (a.parts > 1)
     MOE_LAUNCH("attn_prefill_join", attn_prefill_join_kernel<D>, dim3((unsigned)((rows + kJoinRows - 1) / kJoinRows)),
                dim3(256), 0, stream, a, rows);
