@@ -558,7 +558,9 @@ moe_status_t moe_rope_cache(moe_attn_dims_t dims, int32_t T, const uint16_t* q, 
  * Reads cached sequences back: rows cu[b] .. cu[b+1] - 1 of k_out and v_out =
  * bf16(code * scale) of the first cu[b+1] - cu[b] tokens that row b of the page
  * table holds.  page_table: device int32 [B, table_width], rows contiguous.
- * cu: device int32 [B + 1], not decreasing, 0..T.  k_out, v_out:
+ * cu: device int32 [B + 1], not decreasing; rows outside 0..T - 1 are left out.
+ * Offsets that leave 0..T, or decrease, set MOE_DEV_BAD_LENGTH (a call with B or T
+ * 0 launches nothing and looks at nothing).  k_out, v_out:
  * device bf16 [T, kv_heads, head_dim], contiguous; rows outside all sequences
  * are not written.  A page id outside the cache or a sequence longer than its
  * table row sets MOE_DEV_BAD_PAGE / MOE_DEV_BAD_LENGTH and its rows get zeros.

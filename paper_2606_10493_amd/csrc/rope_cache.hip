@@ -222,7 +222,9 @@ __device__ __forceinline__ int sequence_of(const int32_t* __restrict__ cu, int B
   return min(lo, B - 1);
 }
 
-// A group of D / 8 lanes takes one token's keys and values of `per` heads.  What
+// A group of D / 8 lanes takes one token's keys and values of `per` heads.  With a
+// status word the grid has one column of workgroups more, the first of which looks
+// at the offsets: those of a sequence that the cut leaves nothing, too.  What
 // is written is read by another launch, if at all from a cache that holds all of
 // it: the stores are non-temporal (104k tokens of 8 heads of 128: 132 -> 123 us).
 template <int D>
@@ -233,6 +235,13 @@ __global__ __launch_bounds__(256) void cache_read_kernel(moe_kv_cache_t cache, i
                                                          int32_t* status) {
   constexpr int kLanes = D / 8, kTokens = 256 / kLanes;
   const int sub = threadIdx.x % kLanes;
+  if (status && blockIdx.x == gridDim.x - 1) {
+    if (blockIdx.y > 0) return;
+    bool cut = false;
+    for (int64_t i = threadIdx.x; i < B; i += 256) cut |= cu[i] < 0 || cu[i + 1] > T || cu[i] > cu[i + 1];
+    if (__any(cut) && threadIdx.x % 64 == 0) atomicOr(status, MOE_DEV_BAD_LENGTH);
+    return;
+  }
   const int64_t t = (int64_t)blockIdx.x * kTokens + threadIdx.x / kLanes;
   if (t >= T || t < cu[0] || t >= cu[B]) return;  // whole groups leave together
   const int b = sequence_of<kLanes>(cu, B, t, sub);
@@ -359,7 +368,7 @@ extern "C" moe_status_t moe_cache_read(moe_attn_dims_t d, moe_kv_cache_t cache, 
   if (T > kSpanTokens) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_cache_read: T=%d is over %lld", T, (long long)kSpanTokens);
   const unsigned gx = (unsigned)((T + per - 1) / per);
   const int heads = gx < 1024 ? 1 : d.kv_heads;  // few tokens: more workgroups rather than longer ones
-  const dim3 grid(gx, (d.kv_heads + heads - 1) / heads);
+  const dim3 grid(gx + (dev_status ? 1 : 0), (d.kv_heads + heads - 1) / heads);
   if (d.head_dim == 64)
     MOE_LAUNCH("cache_read", cache_read_kernel<64>, grid, dim3(256), 0, stream, cache, shift, d.kv_heads, heads,
                page_table, B,
