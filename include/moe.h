@@ -591,6 +591,8 @@ moe_status_t moe_cache_read(moe_attn_dims_t dims, moe_kv_cache_t cache, const in
  * [T_q, q_heads, head_dim]; k, v: [T_k, kv_heads, head_dim]; out: contiguous
  * [T_q, q_heads, head_dim], no overlap with the inputs.  scale > 0.
  * ws: moe_attn_prefill_workspace(dims, B, T_q, max_k) bytes, 256-byte aligned.
+ * No smaller B, T_q or max_k needs more: what the largest call needs serves all
+ * (32 heads of 128, any number of tokens and sequences, up to 8701 keys: 205 MB).
  */
 size_t moe_attn_prefill_workspace(moe_attn_dims_t dims, int32_t B, int32_t T_q, int32_t max_k);
 moe_status_t moe_attn_prefill(moe_attn_dims_t dims, int32_t B, int32_t T_q, int32_t T_k, int32_t max_k,

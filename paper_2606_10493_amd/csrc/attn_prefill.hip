@@ -587,25 +587,45 @@ struct PrefillPlan {
 // 157 and 208 (twice the keys go through LDS).  509 tokens of 32 heads over 8
 // behind 8192 keys are 64 workgroups of 136 tiles: 184 us whole, 72 us in four
 // parts and 8 us to join them.
+//
+// What the chosen number of parts needs goes up and down with the sizes, and a
+// caller has one workspace for calls of many sizes.  So the plan keeps to
+// `most_sums`, which only grows, and a call that cuts its keys asks for all of that.
+constexpr double kStart[2] = {5.0, 6.3};  // us of a workgroup, whole rows and shared ones
+double step_us(int32_t head_dim, int split) { return head_dim == 128 ? (split ? 1.8 : 1.45) : (split ? 1.25 : 1.1); }
+constexpr int kMostParts = 16;
+
+// Bytes of the parts' sums that a call of these sizes or smaller ones may use.  More parts than key tiles are never
+// faster; and the sums' way to memory and back, 8 bytes an element at 4 TB/s, takes less than what parts can save, which
+// is one round of workgroups (kStart + step_us for each key tile): bytes < 2e6 of the us of a round.  Half of that has
+// been enough for every plan of 14 head layouts, 1 to 300 sequences, up to 60000 tokens and 10^6 keys (0.43 at the most).
+size_t most_sums(const moe_attn_dims_t& d, int32_t T_q, int32_t max_k) {
+  const int key_tiles = max_k / kKeys + 1;
+  if (key_tiles == 1) return 0;
+  const size_t each = (size_t)T_q * d.q_heads * d.head_dim * sizeof(float) * std::min(kMostParts, key_tiles);
+  return std::min(each, (size_t)(1e6 * (kStart[0] + step_us(d.head_dim, 0) * key_tiles)));
+}
+
 PrefillPlan plan_prefill(const moe_attn_dims_t& d, int32_t B, int32_t T_q, int32_t max_k) {
   PrefillPlan p{};
   const int group = d.q_heads / d.kv_heads;
   const int64_t rows = (int64_t)T_q * d.q_heads;
   const int key_tiles = max_k / kKeys + 1;
-  const double start[2] = {5.0, 6.3};
-  const double step[2] = {d.head_dim == 128 ? 1.45 : 1.1, d.head_dim == 128 ? 1.8 : 1.25};
+  const size_t most = most_sums(d, T_q, max_k);
   // a causal prompt's rows see the keys before them: their mean over the longest's
   const double mean = 1.0 - std::min((double)T_q / B, (double)max_k) / (2.0 * std::max(max_k, 1)), even = 2.0 * mean - 1.0;
   double best = 0.0;
   for (int split = 0; split < 2; ++split) {
     const int64_t tiles = (int64_t)T_q * group / (kWaves * kWaveRows >> split) + B;  // sequences may each add a part of one
-    for (int parts = 1; parts <= 16; ++parts) {
+    for (int parts = 1; parts <= std::min(kMostParts, key_tiles); ++parts) {
+      if (parts > 1 && (size_t)rows * parts * d.head_dim * sizeof(float) > most) break;
       const int part_tiles = (key_tiles + parts - 1) / parts;
       const double steps = (part_tiles + split) >> split;
       // workgroups a CU: the more alike they are, the more a last round of few costs a whole one
       const double load = (double)(tiles * d.kv_heads * parts) / 256;
       const double rounds = load + (std::max(1.0, ceil(load)) - load) * even * even;
-      double us = std::max(start[split] + step[split] * steps, rounds * (start[split] + step[split] * steps * mean));
+      const double start = kStart[split], step = step_us(d.head_dim, split);
+      double us = std::max(start + step * steps, rounds * (start + step * steps * mean));
       if (parts > 1) us += 4.5 + (double)rows * parts * d.head_dim * 8 / 4e6;
       if (p.parts == 0 || us < best) {
         best = us;
@@ -621,6 +641,12 @@ PrefillPlan plan_prefill(const moe_attn_dims_t& d, int32_t B, int32_t T_q, int32
     p.ml_bytes = ((size_t)rows * p.parts * 2 * sizeof(float) + 255) & ~(size_t)255;
   }
   return p;
+}
+
+// A call's workspace where its plan has parts: sums, and a maximum and a sum for every head_dim of them.
+size_t prefill_workspace(const moe_attn_dims_t& d, int32_t T_q, int32_t max_k) {
+  const size_t sums = most_sums(d, T_q, max_k), pairs = sums / d.head_dim * 2;
+  return ((sums + 255) & ~(size_t)255) + ((pairs + 255) & ~(size_t)255);
 }
 
 template <int D>
@@ -650,8 +676,7 @@ using namespace moe;
 
 extern "C" size_t moe_attn_prefill_workspace(moe_attn_dims_t d, int32_t B, int32_t T_q, int32_t max_k) {
   if (check_attn_dims(d, "moe_attn_prefill_workspace") != MOE_OK || B < 1 || T_q < 1 || max_k < 0) return 0;
-  const PrefillPlan p = plan_prefill(d, B, T_q, max_k);
-  return p.o_bytes + p.ml_bytes;
+  return prefill_workspace(d, T_q, max_k);
 }
 
 extern "C" moe_status_t moe_attn_prefill(moe_attn_dims_t d, int32_t B, int32_t T_q, int32_t T_k, int32_t max_k,
@@ -672,7 +697,7 @@ extern "C" moe_status_t moe_attn_prefill(moe_attn_dims_t d, int32_t B, int32_t T
   if (!cu_q || !cu_k || !out) return fail(MOE_ERR_INVALID_ARG, "moe_attn_prefill: null pointer");
   if (!aligned(out, 16)) return fail(MOE_ERR_INVALID_ARG, "moe_attn_prefill: out must be 16-byte aligned");
   const PrefillPlan p = plan_prefill(d, B, T_q, max_k);
-  const size_t need = p.o_bytes + p.ml_bytes;
+  const size_t need = p.parts > 1 ? prefill_workspace(d, T_q, max_k) : 0;
   if (need && (!ws || ws_bytes < need || !aligned(ws, 256)))
     return fail(MOE_ERR_WORKSPACE, "moe_attn_prefill: workspace %zu bytes, needs %zu, 256-byte aligned", ws_bytes, need);
   uint8_t* base = static_cast<uint8_t*>(ws);
