@@ -618,7 +618,8 @@ moe_status_t moe_attn_prefill(moe_attn_dims_t dims, int32_t B, int32_t T_q, int3
  * unspecified.  max_len: the longest of lens; it decides how the work is split
  * and nothing else.  q: [B, q_heads, head_dim]; out contiguous, no overlap.
  * ws: moe_attn_decode_workspace(dims, B, max_len, prefix_len) bytes, 256-byte
- * aligned; what the longest max_len needs is enough for every shorter one.
+ * aligned.  No smaller B, max_len or prefix_len (0 too) needs more: what the
+ * largest call needs serves all.
  */
 size_t moe_attn_decode_workspace(moe_attn_dims_t dims, int32_t B, int32_t max_len, int32_t prefix_len);
 moe_status_t moe_attn_decode(moe_attn_dims_t dims, int32_t B, const uint16_t* q, int64_t q_stride, moe_kv_cache_t cache,

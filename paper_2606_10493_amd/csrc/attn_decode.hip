@@ -642,10 +642,11 @@ struct DecodePlan {
   int own_blocks, prefix_blocks, pieces;
   int64_t workgroups;
   size_t o_bytes, ml_bytes, start_bytes;
+  size_t bytes() const { return o_bytes + ml_bytes + start_bytes; }
 };
 
-// Whether one launch, in which a workgroup walks all keys of a sequence and head,
-// the prefix's for each sequence anew, is faster than equal pieces and a join.
+// What one launch, in which a workgroup walks all keys of a sequence and head, the
+// prefix's for each sequence anew, saves against equal pieces and a join.
 // Estimates in us, of D = 128 (D = 64 is quicker on both sides).  One launch: 0.9 a
 // step, more when more than 256 workgroups share the card (a sequence's own steps,
 // most of them fewer than the longest's, when more than 384).  Two: 5 us more to
@@ -654,15 +655,16 @@ struct DecodePlan {
 // against two: 1 sequence of 512 keys 6.8 against 8.2, of 1024 10.6 against 8.4; 32
 // of up to 1024 11.9 against 14.6, of up to 2048 19.3 against 18.6; 48 of up to 500
 // behind 120 shared ones 11.5 against 16.4, of up to 250 behind 1500 23 against 19.
-bool whole_is_faster(const DecodePlan& p, const moe_attn_dims_t& d, int32_t B, int32_t own_steps, int32_t prefix_steps) {
-  const double groups = (double)p.workgroups;
+double whole_gains(const DecodePlan& p, const moe_attn_dims_t& d, int32_t B, int32_t own_steps, int32_t prefix_steps) {
+  const double groups = (double)p.own_blocks * B * d.kv_heads;
   const double line = 2.0 * p.prefix_blocks * prefix_steps + (double)p.own_blocks * B * own_steps;
   const double one = 3.2 + 0.9 * (own_steps * std::max(1.0, groups / 384) + prefix_steps * std::max(1.0, groups / 256));
   const double two = (prefix_steps > 0 ? 9.5 : 8.2) + 3.2 * groups / 512 + 0.9 * line * d.kv_heads / 512;
-  return one <= two;
+  return two - one;
 }
 
-DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int32_t prefix_len) {
+// The columns' blocks: all that the choice between one launch and two looks at.
+DecodePlan plan_blocks(const moe_attn_dims_t& d, int32_t B, int32_t prefix_len) {
   DecodePlan p{};
   const int group = d.q_heads / d.kv_heads;
   const int64_t all = (int64_t)B * group;
@@ -672,25 +674,47 @@ DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int
   p.front = prefix_len > 0 && all > 16 ? 2 : p.own;
   p.own_blocks = (group + 16 * p.own - 1) / (16 * p.own);
   p.prefix_blocks = prefix_len > 0 ? (int)((all + 16 * p.front - 1) / (16 * p.front)) : 0;
-  const int64_t own_pairs = (int64_t)p.own_blocks * B;
-  p.workgroups = own_pairs * d.kv_heads;
-  p.whole = whole_is_faster(p, d, B, steps_of(max_len), steps_of(prefix_len));
-  if (!p.whole) {
-    const int64_t steps = own_pairs * steps_of(max_len) + (int64_t)p.prefix_blocks * steps_of(prefix_len);
-    // Two workgroups a CU (64 ragged contexts: 77 us with 512 workgroups, 81 with 768, 84 with 1536; one context of 65536:
-    // 27, 29 and 31 us, and a longer join).
-    // Fewer where a row would have many segments of few steps: steps / pieces in the first launch and pieces / runs of keys
-    // in the second cost about as much at this number (16 heads over 1, one context of 65536, 80 pieces 11.6 + 5.3 us, 512
-    // 8.1 + 24.4; 28 over 4, two of up to 16583, 80 pieces 8.6 + 6.4, 128 9.1 + 8.2).
-    const int64_t few = (int64_t)ceil(3.5 * sqrt((double)steps * (double)(p.prefix_blocks + own_pairs)));
-    p.pieces = (int)std::max<int64_t>(1, std::min(std::min<int64_t>(512 / d.kv_heads, few), steps));
-    p.workgroups = (int64_t)p.pieces * d.kv_heads;
-    const size_t places = (size_t)d.kv_heads * (p.pieces + p.prefix_blocks + own_pairs) * 16 * std::max(p.front, p.own);
-    p.o_bytes = (places * d.head_dim * sizeof(float) + 255) & ~(size_t)255;
-    p.ml_bytes = (places * sizeof(float2) + 255) & ~(size_t)255;
-    p.start_bytes = ((size_t)(B + 1) * sizeof(uint32_t) + 255) & ~(size_t)255;
-  }
   return p;
+}
+
+// Equal pieces and a join.  Everything here only grows with B, max_len and prefix_len.
+DecodePlan plan_pieces(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int32_t prefix_len) {
+  DecodePlan p = plan_blocks(d, B, prefix_len);
+  const int64_t own_pairs = (int64_t)p.own_blocks * B;
+  const int64_t steps = own_pairs * steps_of(max_len) + (int64_t)p.prefix_blocks * steps_of(prefix_len);
+  // Two workgroups a CU (64 ragged contexts: 77 us with 512 workgroups, 81 with 768, 84 with 1536; one context of 65536:
+  // 27, 29 and 31 us, and a longer join).
+  // Fewer where a row would have many segments of few steps: steps / pieces in the first launch and pieces / runs of keys
+  // in the second cost about as much at this number (16 heads over 1, one context of 65536, 80 pieces 11.6 + 5.3 us, 512
+  // 8.1 + 24.4; 28 over 4, two of up to 16583, 80 pieces 8.6 + 6.4, 128 9.1 + 8.2).
+  const int64_t few = (int64_t)ceil(3.5 * sqrt((double)steps * (double)(p.prefix_blocks + own_pairs)));
+  p.pieces = (int)std::max<int64_t>(1, std::min(std::min<int64_t>(512 / d.kv_heads, few), steps));
+  p.workgroups = (int64_t)p.pieces * d.kv_heads;
+  const size_t places = (size_t)d.kv_heads * (p.pieces + p.prefix_blocks + own_pairs) * 16 * std::max(p.front, p.own);
+  p.o_bytes = (places * d.head_dim * sizeof(float) + 255) & ~(size_t)255;
+  p.ml_bytes = (places * sizeof(float2) + 255) & ~(size_t)255;
+  p.start_bytes = ((size_t)(B + 1) * sizeof(uint32_t) + 255) & ~(size_t)255;
+  return p;
+}
+
+DecodePlan plan_decode(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int32_t prefix_len) {
+  DecodePlan p = plan_blocks(d, B, prefix_len);
+  p.whole = whole_gains(p, d, B, steps_of(max_len), steps_of(prefix_len)) >= 0.0;
+  if (!p.whole) return plan_pieces(d, B, max_len, prefix_len);
+  p.workgroups = (int64_t)p.own_blocks * B * d.kv_heads;
+  return p;
+}
+
+// What a call of these sizes or smaller ones may need.  A longer context or prefix never makes one launch the faster
+// form, but for a prefix at all (the join costs more with one); a larger batch can, since its workgroups share the card.
+// So the largest batch that would take two launches, with the prefix or without, decides.
+size_t decode_workspace(const moe_attn_dims_t& d, int32_t B, int32_t max_len, int32_t prefix_len) {
+  constexpr double kRounding = 1e-9;  // us: of estimates that are equal but for the order of their sums
+  for (int32_t b = B; b > 0; --b)
+    for (const int32_t prefix : {prefix_len, 0})
+      if (whole_gains(plan_blocks(d, b, prefix), d, b, steps_of(max_len), steps_of(prefix)) < kRounding)
+        return plan_pieces(d, b, max_len, prefix_len).bytes();
+  return 0;
 }
 
 template <int D, int NCP, int NCO>
@@ -730,8 +754,7 @@ extern "C" size_t moe_attn_decode_workspace(moe_attn_dims_t d, int32_t B, int32_
   if (check_attn_dims(d, "moe_attn_decode_workspace") != MOE_OK || B < 1 || B > 65535 || max_len < 0 || prefix_len < 0 ||
       max_len > kMostKeys || prefix_len > kMostKeys)
     return 0;
-  const DecodePlan p = plan_decode(d, B, max_len, prefix_len);
-  return p.o_bytes + p.ml_bytes + p.start_bytes;
+  return decode_workspace(d, B, max_len, prefix_len);
 }
 
 extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint16_t* q, int64_t q_stride,
@@ -758,7 +781,7 @@ extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint
   if ((int64_t)p.prefix_blocks * steps_of(prefix_len) + (int64_t)p.own_blocks * B * steps_of((int)row_keys) > 0x7fffffff)
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_decode: %d sequences of %lld keys and a prefix of %d: over 2^31 steps", B,
                 (long long)row_keys, prefix_len);
-  const size_t need = p.o_bytes + p.ml_bytes + p.start_bytes;
+  const size_t need = p.bytes();
   if (need && (!ws || ws_bytes < need || !aligned(ws, 256)))
     return fail(MOE_ERR_WORKSPACE, "moe_attn_decode: workspace %zu bytes, needs %zu, 256-byte aligned", ws_bytes, need);
   uint8_t* base = static_cast<uint8_t*>(ws);

@@ -31,3 +31,23 @@ def test_a_larger_prompt_call_never_needs_less(dims):
         a = [log_uniform(rng, m) for m in (300, 60000, 1000000)]
         b = [x + rng.choice((0, 0, 1, log_uniform(rng, m))) for x, m in zip(a, (300, 60000, 1000000))]
         assert need(*a) <= need(*b), (a, b)
+
+
+@pytest.mark.parametrize("dims", HEADS)
+def test_a_larger_batch_or_prefix_never_needs_less(dims):
+    d, rng = moe.MoeAttnDims(*dims), random.Random(62)
+
+    def need(batch, longest, prefix):
+        return moe.moe_attn_decode_workspace(d, batch, longest, prefix)
+    for longest in (0, 100, 500, 768, 1024, 1500, 2048, 4000, 9000):
+        for prefix in (0, 120, 1500, 8191):
+            sizes = [need(b, longest, prefix) for b in [*range(1, 129), 200, 384, 500, 1000, 5000]]
+            assert sizes == sorted(sizes), (longest, prefix)
+        for batch in (1, 8, 48):
+            sizes = [need(batch, longest, p) for p in range(0, 3000, 43)]
+            assert sizes == sorted(sizes), (longest, batch)
+    for _ in range(3000):
+        a = [log_uniform(rng, m) for m in (300, 20000, 20000)]
+        b = [x + rng.choice((0, 0, 1, log_uniform(rng, m))) for x, m in zip(a, (300, 20000, 20000))]
+        assert need(*a) <= need(*b), (a, b)
+        assert need(a[0], a[1], 0) <= need(*a)
