@@ -11,7 +11,7 @@ Python.
 """
 from __future__ import annotations
 
-import os
+import importlib
 
 import torch
 
@@ -19,10 +19,21 @@ from . import _dev, _stream  # defined before the package imports this module
 from ._lib import MoeAttnDims, MoeKvCache, MoeRopeCfg, MOE_ROPE_HALF, MOE_ROPE_PLAIN, check as _check, lib
 
 
-if not os.path.exists(os.path.join(os.path.dirname(os.path.abspath(__file__)), "_binding.so")):
-    raise ImportError("_binding.so is not built; run `python paper_2606_10493_amd/build.py`")
+class _NoBinding:
+    """Stands for a binding that is not there: the rest of the package works, every attention call says why it does not."""
 
-from . import _binding  # noqa: E402  (links libmoe.so, which is loaded by now)
+    def __init__(self, why: str):
+        self.why = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"_binding.so, which the attention calls need, cannot be loaded ({self.why}); build it with "
+                          "`python paper_2606_10493_amd/build.py`")
+
+
+try:
+    _binding = importlib.import_module("._binding", __package__)  # links libmoe.so, which is loaded by now
+except ImportError as e:
+    _binding = _NoBinding(str(e))
 
 
 class KVCache:

@@ -8,7 +8,9 @@ _binding.so, the attention calls' native Python binding.
 Every .hip file under csrc/ is compiled with hipcc in parallel and linked
 into paper_2606_10493_amd/libmoe.so.  It compiles on a machine without a
 GPU (hipcc cross-compiles for gfx950).  csrc/binding.cpp is compiled with g++
-against the Python and torch headers and linked with libmoe.so.
+against the Python and torch headers and linked with libmoe.so; where one of
+these is missing the library is built all the same, and the attention calls
+are left without their Python binding.
 """
 from __future__ import annotations
 
@@ -30,6 +32,8 @@ BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
+CXX = os.environ.get("CXX", "g++")
+PYTHON_INCLUDE = sysconfig.get_paths()["include"]
 
 CFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
@@ -52,21 +56,36 @@ def _compile(src: str) -> str:
     return obj
 
 
-def _build_binding() -> None:
-    import torch  # its headers and its ABI flag
+def build_binding() -> bool:
+    """_binding.so, if there is what it needs; otherwise none, since an earlier one might not fit the library."""
+    if os.path.exists(BINDING):
+        os.remove(BINDING)
+    missing = None
+    if not (CXX and shutil.which(CXX)):
+        missing = f"C++ compiler {CXX}"
+    elif not os.path.exists(os.path.join(PYTHON_INCLUDE, "Python.h")):
+        missing = f"{PYTHON_INCLUDE}/Python.h"
+    try:
+        import torch  # its headers and its ABI flag
+    except ImportError:
+        missing = "torch"
+    if missing:
+        print(f"_binding.so is not built, the attention calls have no Python binding: {missing} is missing", file=sys.stderr)
+        return False
     lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
     include = os.path.join(os.path.dirname(torch.__file__), "include")
     tmp = BINDING + ".tmp"
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+    cmd = [CXX, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE, "-isystem", include,
            "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
-           "-isystem", sysconfig.get_paths()["include"], "-isystem", "/opt/rocm/include",
+           "-isystem", PYTHON_INCLUDE, "-isystem", "/opt/rocm/include",
            os.path.join(CSRC, "binding.cpp"), "-o", tmp,
            "-L", PKG, "-lmoe", "-L", lib_dir, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError(f"building binding.cpp failed:\n{res.stdout}\n{res.stderr}")
     os.replace(tmp, BINDING)
+    return True
 
 
 def build(verbose: bool = False) -> str:
@@ -80,9 +99,9 @@ def build(verbose: bool = False) -> str:
     if res.returncode != 0:
         raise RuntimeError(f"link failed:\n{res.stdout}\n{res.stderr}")
     os.replace(tmp, LIB)
-    _build_binding()
+    bound = build_binding()
     if verbose:
-        print(f"built {LIB} from {len(srcs)} sources, and {BINDING}")
+        print(f"built {LIB} from {len(srcs)} sources" + (f", and {BINDING}" if bound else ""))
     return LIB
 
 
