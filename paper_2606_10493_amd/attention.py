@@ -44,6 +44,12 @@ class KVCache:
         if k.dim() != 4 or v.shape != k.shape or k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
             raise ValueError("KVCache: codes are [n_pages, kv_heads, page_size, head_dim], scales [n_pages, kv_heads, "
                              "page_size]")
+        for t, name in ((k, "k"), (v, "v")):
+            if t.dtype not in (torch.uint8, torch.int8, torch.float8_e4m3fn):
+                raise ValueError(f"{name} must be e4m3 codes (uint8, int8 or float8_e4m3fn)")
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype != torch.float32:
+                raise ValueError(f"{name} must be fp32")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.kv_heads, self.page_size, self.head_dim = k.shape[1:]
         self.n_pages = k.shape[0]
@@ -71,6 +77,8 @@ def moe_rope_table(table, base: float = 10000.0, scaling: int = MOE_ROPE_PLAIN, 
                    stream=None):
     """Fills table fp32 [n_pos, rot_dim]: cosines, then sines of every position (see include/moe.h)."""
     n_pos, rot = table.shape
+    if table.dtype != torch.float32:
+        raise ValueError("table must be fp32")
     cfg = MoeRopeCfg(rot, scaling, base, factor, original_len, slow_turns, fast_turns, magnitude)
     _check(lib.moe_rope_table(cfg, n_pos, _dev(table, 4, "table"), _stream(stream)))
 

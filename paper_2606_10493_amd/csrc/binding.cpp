@@ -10,6 +10,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <type_traits>
 
 #include "moe.h"
 
@@ -32,23 +33,26 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
   return t;
 }
 
-// The address of a contiguous device tensor with elements of `bytes` bytes; NULL for None.
+// The address of a contiguous device tensor, NULL for None.  Integers and fp32 numbers have that type; bytes
+// (workspaces) and 16-bit words, whose type bf16_rows looks at, have that size.
 template <typename T>
-T* address(PyObject* o, size_t bytes, const char* name, int64_t* count = nullptr) {
+T* address(PyObject* o, const char* name, int64_t* count = nullptr) {
   if (o == Py_None) {
     if (count) *count = 0;
     return nullptr;
   }
   const at::Tensor& t = tensor(o, name);
   if (!t.is_contiguous()) bad_value("%s must be contiguous", name);
-  if ((size_t)t.element_size() != bytes) bad_value("%s has elements of another size", name);
+  if (std::is_same_v<T, int32_t> && t.scalar_type() != at::kInt) bad_value("%s must be int32", name);
+  if (std::is_same_v<T, float> && t.scalar_type() != at::kFloat) bad_value("%s must be fp32", name);
+  if ((size_t)t.element_size() != sizeof(T)) bad_value("%s has elements of another size", name);
   if (count) *count = t.numel();
   return static_cast<T*>(t.data_ptr());
 }
 
 template <typename T>
 T* matrix(PyObject* o, const char* name, int64_t& rows, int64_t& cols) {
-  T* p = address<T>(o, 4, name);
+  T* p = address<T>(o, name);
   if (!p && o == Py_None) bad_value("%s must not be None", name);
   const at::Tensor& t = THPVariable_Unpack(o);
   if (t.dim() != 2) bad_value("%s must have two dimensions", name);
@@ -84,7 +88,7 @@ struct Rows {
 };
 
 uint16_t* out_rows(PyObject* o, int64_t tokens, int64_t heads, int64_t dim, const char* name) {
-  uint16_t* p = address<uint16_t>(o, 2, name);
+  uint16_t* p = address<uint16_t>(o, name);
   if (o == Py_None) bad_value("%s must not be None", name);
   const at::Tensor& t = THPVariable_Unpack(o);
   bf16_rows(t, heads, dim, name);
@@ -143,7 +147,7 @@ hipStream_t stream_of(PyObject* o) {
   return reinterpret_cast<hipStream_t>(v);
 }
 
-int32_t* status_of(PyObject* o) { return address<int32_t>(o, 4, "dev_status"); }
+int32_t* status_of(PyObject* o) { return address<int32_t>(o, "dev_status"); }
 
 // The functions proper, and their entries for Python: the number of arguments is
 // checked, and no C++ exception passes.
@@ -168,7 +172,7 @@ PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n) {
 moe_status_t rope(PyObject* const* a) {
   const auto d = structure<moe_attn_dims_t>(a[0], "dims");
   int64_t n, n_pos, rot;
-  const int32_t* positions = address<int32_t>(a[3], 4, "positions", &n);
+  const int32_t* positions = address<int32_t>(a[3], "positions", &n);
   const float* table = matrix<float>(a[4], "table", n_pos, rot);
   Rows q, k;
   uint16_t *qo = nullptr, *ko = nullptr;
@@ -191,7 +195,7 @@ moe_status_t rope(PyObject* const* a) {
 moe_status_t rope_cache(PyObject* const* a) {
   const auto d = structure<moe_attn_dims_t>(a[0], "dims");
   int64_t n, n_slots, n_pos, rot;
-  const int32_t *positions = address<int32_t>(a[4], 4, "positions", &n), *slots = address<int32_t>(a[7], 4, "slots", &n_slots);
+  const int32_t *positions = address<int32_t>(a[4], "positions", &n), *slots = address<int32_t>(a[7], "slots", &n_slots);
   const float* table = matrix<float>(a[5], "table", n_pos, rot);
   const Rows q(a[1], d.q_heads, d.head_dim, "q"), k(a[2], d.kv_heads, d.head_dim, "k"), v(a[3], d.kv_heads, d.head_dim, "v");
   same(q.n, n, "q");
@@ -210,7 +214,7 @@ moe_status_t cache_read(PyObject* const* a) {
   const auto d = structure<moe_attn_dims_t>(a[0], "dims");
   int64_t batch, width, n;
   const int32_t* pages = matrix<int32_t>(a[2], "page_table", batch, width);
-  const int32_t* cu = address<int32_t>(a[3], 4, "cu", &n);
+  const int32_t* cu = address<int32_t>(a[3], "cu", &n);
   same(n, batch + 1, "cu");
   const at::Tensor& k = tensor(a[4], "k_out");
   const int64_t tokens = k.dim() == 3 ? k.size(0) : -1;
@@ -226,9 +230,9 @@ moe_status_t attn_prefill(PyObject* const* a) {
   const Rows q(a[1], d.q_heads, d.head_dim, "q"), k(a[2], d.kv_heads, d.head_dim, "k"), v(a[3], d.kv_heads, d.head_dim, "v");
   same(v.n, k.n, "v");
   int64_t n, m, ws_bytes;
-  const int32_t *cu_q = address<int32_t>(a[4], 4, "cu_q", &n), *cu_k = address<int32_t>(a[5], 4, "cu_k", &m);
+  const int32_t *cu_q = address<int32_t>(a[4], "cu_q", &n), *cu_k = address<int32_t>(a[5], "cu_k", &m);
   same(m, n, "cu_k");
-  uint8_t* ws = address<uint8_t>(a[9], 1, "ws", &ws_bytes);
+  uint8_t* ws = address<uint8_t>(a[9], "ws", &ws_bytes);
   return moe_attn_prefill(d, to_int32(n, "cu_q") - 1, to_int32(q.n, "q"), to_int32(k.n, "k"), integer32(a[6], "max_k"), q.p,
                           q.stride, k.p, k.stride, v.p, v.stride, cu_q, cu_k, real(a[7]), PyObject_IsTrue(a[10]) == 1,
                           out_rows(a[8], q.n, d.q_heads, d.head_dim, "out"), status_of(a[11]), ws, (size_t)ws_bytes,
@@ -243,12 +247,12 @@ moe_status_t attn_decode(PyObject* const* a) {
   const int32_t* pages = matrix<int32_t>(a[3], "page_table", batch, width);
   const Rows q(a[1], d.q_heads, d.head_dim, "q");
   same(q.n, batch, "q");
-  const int32_t* lens = address<int32_t>(a[4], 4, "lens", &n);
+  const int32_t* lens = address<int32_t>(a[4], "lens", &n);
   same(n, batch, "lens");
-  const int32_t* prefix = address<int32_t>(a[9], 4, "prefix_pages", &n_prefix);
+  const int32_t* prefix = address<int32_t>(a[9], "prefix_pages", &n_prefix);
   const int32_t prefix_len = integer32(a[10], "prefix_len");
   if (prefix_len > 0 && n_prefix * c.page_size < prefix_len) bad_value("%s must hold the prefix's tokens", "prefix_pages");
-  uint8_t* ws = address<uint8_t>(a[8], 1, "ws", &ws_bytes);
+  uint8_t* ws = address<uint8_t>(a[8], "ws", &ws_bytes);
   return moe_attn_decode(d, to_int32(batch, "page_table"), q.p, q.stride, c, pages, to_int32(width, "page_table"), lens,
                          integer32(a[5], "max_len"), prefix, prefix_len, real(a[6]),
                          out_rows(a[7], batch, d.q_heads, d.head_dim, "out"), status_of(a[11]), ws, (size_t)ws_bytes,
