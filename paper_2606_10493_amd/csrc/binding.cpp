@@ -176,16 +176,17 @@ moe_status_t rope(PyObject* const* a) {
   const float* table = matrix<float>(a[4], "table", n_pos, rot);
   Rows q, k;
   uint16_t *qo = nullptr, *ko = nullptr;
+  // an output without its input is passed on, for the call to refuse
   if (a[1] != Py_None) {
     q = Rows(a[1], d.q_heads, d.head_dim, "q");
     same(q.n, n, "q");
-    qo = out_rows(a[6], n, d.q_heads, d.head_dim, "q_out");
   }
+  if (a[1] != Py_None || a[6] != Py_None) qo = out_rows(a[6], n, d.q_heads, d.head_dim, "q_out");
   if (a[2] != Py_None) {
     k = Rows(a[2], d.kv_heads, d.head_dim, "k");
     same(k.n, n, "k");
-    ko = out_rows(a[7], n, d.kv_heads, d.head_dim, "k_out");
   }
+  if (a[2] != Py_None || a[7] != Py_None) ko = out_rows(a[7], n, d.kv_heads, d.head_dim, "k_out");
   return moe_rope(d, to_int32(n, "positions"), q.p, q.stride, k.p, k.stride, positions, table, to_int32(n_pos, "table"),
                   to_int32(rot, "table"), (moe_rope_layout_t)integer32(a[5], "layout"), qo, ko, status_of(a[8]),
                   stream_of(a[9]));

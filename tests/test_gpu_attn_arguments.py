@@ -46,3 +46,13 @@ def test_types_of_the_cache_and_the_table(moe):
             moe.KVCache(codes, codes.view(other), scales, scales)
     with pytest.raises(ValueError, match="table"):
         moe.moe_rope_table(torch.zeros((8, 64), dtype=torch.int32, device="cuda"))
+
+
+def test_an_output_without_its_input(call, moe):
+    """As the C call: queries and their output, and keys and theirs, are given together."""
+    for changed in (dict(q=None), dict(k=None), dict(q=None, k=None)):
+        with pytest.raises(moe.MoEError) as e:
+            call("moe_rope", **changed)
+        assert e.value.status == moe.MOE_ERR_INVALID_ARG
+    call("moe_rope", q=None, q_out=None)
+    call("moe_rope", k=None, k_out=None)
