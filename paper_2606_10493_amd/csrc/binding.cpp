@@ -136,6 +136,12 @@ float real(PyObject* o) {
   return (float)v;
 }
 
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Bad{};
+  return v != 0;
+}
+
 // The caller's torch stream, or the current device's current one.
 hipStream_t stream_of(PyObject* o) {
   if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
@@ -235,7 +241,7 @@ moe_status_t attn_prefill(PyObject* const* a) {
   same(m, n, "cu_k");
   uint8_t* ws = address<uint8_t>(a[9], "ws", &ws_bytes);
   return moe_attn_prefill(d, to_int32(n, "cu_q") - 1, to_int32(q.n, "q"), to_int32(k.n, "k"), integer32(a[6], "max_k"), q.p,
-                          q.stride, k.p, k.stride, v.p, v.stride, cu_q, cu_k, real(a[7]), PyObject_IsTrue(a[10]) == 1,
+                          q.stride, k.p, k.stride, v.p, v.stride, cu_q, cu_k, real(a[7]), truth(a[10]),
                           out_rows(a[8], q.n, d.q_heads, d.head_dim, "out"), status_of(a[11]), ws, (size_t)ws_bytes,
                           stream_of(a[12]));
 }

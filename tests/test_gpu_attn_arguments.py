@@ -1,4 +1,5 @@
 """GPU: arguments that the attention calls' binding has to refuse, or to take."""
+import numpy as np
 import pytest
 import torch
 
@@ -56,3 +57,13 @@ def test_an_output_without_its_input(call, moe):
         assert e.value.status == moe.MOE_ERR_INVALID_ARG
     call("moe_rope", q=None, q_out=None)
     call("moe_rope", k=None, k_out=None)
+
+
+def test_a_flag_that_has_no_truth_value(call):
+    class Vague:
+        def __bool__(self):
+            raise RuntimeError("neither")
+    with pytest.raises(RuntimeError, match="neither"):
+        call("moe_attn_prefill", causal=Vague())
+    call("moe_attn_prefill", causal=0)
+    call("moe_attn_prefill", causal=np.True_)
