@@ -11,6 +11,7 @@ Python.
 """
 from __future__ import annotations
 
+import ctypes
 import importlib
 
 import torch
@@ -36,6 +37,11 @@ except ImportError as e:
     _binding = _NoBinding(str(e))
 
 
+class _DeviceCache(ctypes.Structure):
+    """What the binding takes: the C ABI's structure and its tensors' device."""
+    _fields_ = [("cache", MoeKvCache), ("device", ctypes.c_int64)]
+
+
 class KVCache:
     """A layer's paged key/value cache: e4m3 codes [n_pages, kv_heads, page_size, head_dim] (uint8) and
     fp32 scales [n_pages, kv_heads, page_size] of keys and values."""
@@ -50,11 +56,14 @@ class KVCache:
         for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
             if t.dtype != torch.float32:
                 raise ValueError(f"{name} must be fp32")
+        if len({t.device for t in (k, v, k_scale, v_scale)}) != 1:
+            raise ValueError("KVCache: the tensors are on different devices")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.kv_heads, self.page_size, self.head_dim = k.shape[1:]
         self.n_pages = k.shape[0]
         self.c = MoeKvCache(_dev(k, 1, "k"), _dev(v, 1, "v"), _dev(k_scale, 4, "k_scale"), _dev(v_scale, 4, "v_scale"),
                             k.shape[0], k.shape[2])
+        self.on_device = _DeviceCache(self.c, k.device.index)
 
     @classmethod
     def empty(cls, n_pages: int, kv_heads: int, page_size: int, head_dim: int, device="cuda"):
@@ -69,7 +78,7 @@ class KVCache:
         if self.kv_heads != dims.kv_heads or self.head_dim != dims.head_dim:
             raise ValueError(f"the cache has {self.kv_heads} heads of {self.head_dim}, the call {dims.kv_heads} of "
                              f"{dims.head_dim}")
-        return self.c
+        return self.on_device
 
 
 def moe_rope_table(table, base: float = 10000.0, scaling: int = MOE_ROPE_PLAIN, factor: float = 1.0,
@@ -79,6 +88,8 @@ def moe_rope_table(table, base: float = 10000.0, scaling: int = MOE_ROPE_PLAIN, 
     n_pos, rot = table.shape
     if table.dtype != torch.float32:
         raise ValueError("table must be fp32")
+    if table.is_cuda and table.device.index != (torch.cuda.current_device() if stream is None else stream.device_index):
+        raise ValueError("table is on another device than the call's stream")
     cfg = MoeRopeCfg(rot, scaling, base, factor, original_len, slow_turns, fast_turns, magnitude)
     _check(lib.moe_rope_table(cfg, n_pos, _dev(table, 4, "table"), _stream(stream)))
 

@@ -4,8 +4,8 @@
 // them the launch, and 9 with the same checks in Python and ctypes.
 //
 // Every function takes what its namesake in attention.py passes, in order, and
-// returns the status of the C call.  Tensors are read through torch's C++ objects;
-// nothing of a call is kept.
+// returns the status of the C call; the stream is always the last.  Tensors are read
+// through torch's C++ objects; nothing of a call is kept.
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -23,6 +23,52 @@ struct Bad {};  // a Python error is set
   throw Bad{};
 }
 
+int64_t integer(PyObject* o) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw Bad{};
+  return v;
+}
+
+int64_t attribute(PyObject* o, const char* name) {
+  PyObject* value = PyObject_GetAttrString(o, name);
+  if (!value) throw Bad{};
+  const long long v = PyLong_AsLongLong(value);
+  Py_DECREF(value);
+  if (v == -1 && PyErr_Occurred()) throw Bad{};
+  return v;
+}
+
+// The stream of the call that runs (the interpreter's lock is held) and its device: the caller's torch stream, or the
+// current device's current one.  Taken once, by the first tensor.
+struct Stream {
+  PyObject* given = nullptr;
+  hipStream_t handle = nullptr;
+  int64_t device = -1;
+  void take() {
+    if (device >= 0) return;
+    if (given == Py_None) {
+      const auto current = c10::hip::getCurrentHIPStream();
+      handle = current.stream();
+      device = current.device_index();
+    } else {
+      handle = reinterpret_cast<hipStream_t>(attribute(given, "cuda_stream"));
+      // an object that has a handle alone stands for a stream of the current device
+      device = PyObject_HasAttrString(given, "device_index") ? attribute(given, "device_index")
+                                                             : c10::hip::getCurrentHIPStream().device_index();
+    }
+  }
+} call_stream;
+
+void on_call_device(int64_t index, const char* name) {
+  call_stream.take();
+  if (index != call_stream.device) bad_value("%s is on another device than the call's stream", name);
+}
+
+hipStream_t stream() {
+  call_stream.take();
+  return call_stream.handle;
+}
+
 const at::Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) {
     PyErr_Format(PyExc_TypeError, "%s must be a tensor", name);
@@ -30,6 +76,7 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
   }
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.is_cuda()) bad_value("%s must be a device tensor", name);
+  on_call_device(t.device().index(), name);
   return t;
 }
 
@@ -118,10 +165,16 @@ T structure(PyObject* o, const char* name) {
   return r;
 }
 
-int64_t integer(PyObject* o) {
-  const long long v = PyLong_AsLongLong(o);
-  if (v == -1 && PyErr_Occurred()) throw Bad{};
-  return v;
+// A cache as KVCache gives it, its tensors' device behind it.
+struct DeviceCache {
+  moe_kv_cache_t cache;
+  int64_t device;
+};
+
+moe_kv_cache_t kv_cache(PyObject* o) {
+  const auto c = structure<DeviceCache>(o, "cache");
+  on_call_device(c.device, "cache");
+  return c.cache;
 }
 
 int32_t integer32(PyObject* o, const char* name) {
@@ -142,17 +195,6 @@ bool truth(PyObject* o) {
   return v != 0;
 }
 
-// The caller's torch stream, or the current device's current one.
-hipStream_t stream_of(PyObject* o) {
-  if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
-  PyObject* handle = PyObject_GetAttrString(o, "cuda_stream");
-  if (!handle) throw Bad{};
-  const int64_t v = PyLong_AsLongLong(handle);
-  Py_DECREF(handle);
-  if (v == -1 && PyErr_Occurred()) throw Bad{};
-  return reinterpret_cast<hipStream_t>(v);
-}
-
 int32_t* status_of(PyObject* o) { return address<int32_t>(o, "dev_status"); }
 
 // The functions proper, and their entries for Python: the number of arguments is
@@ -163,6 +205,7 @@ PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n) {
     PyErr_Format(PyExc_TypeError, "%d arguments expected, %zd given", kArgs, n);
     return nullptr;
   }
+  call_stream = Stream{a[kArgs - 1]};
   try {
     return PyLong_FromLong(kCall(a));
   } catch (const Bad&) {
@@ -195,7 +238,7 @@ moe_status_t rope(PyObject* const* a) {
   if (a[2] != Py_None || a[7] != Py_None) ko = out_rows(a[7], n, d.kv_heads, d.head_dim, "k_out");
   return moe_rope(d, to_int32(n, "positions"), q.p, q.stride, k.p, k.stride, positions, table, to_int32(n_pos, "table"),
                   to_int32(rot, "table"), (moe_rope_layout_t)integer32(a[5], "layout"), qo, ko, status_of(a[8]),
-                  stream_of(a[9]));
+                  stream());
 }
 
 // dims, q, k, v, positions, table, layout, slots, cache, q_out, k_out, dev_status, stream
@@ -213,7 +256,7 @@ moe_status_t rope_cache(PyObject* const* a) {
   uint16_t* ko = a[10] == Py_None ? nullptr : out_rows(a[10], n, d.kv_heads, d.head_dim, "k_out");
   return moe_rope_cache(d, to_int32(n, "positions"), q.p, q.stride, k.p, k.stride, v.p, v.stride, positions, table,
                         to_int32(n_pos, "table"), to_int32(rot, "table"), (moe_rope_layout_t)integer32(a[6], "layout"), slots,
-                        structure<moe_kv_cache_t>(a[8], "cache"), qo, ko, status_of(a[11]), stream_of(a[12]));
+                        kv_cache(a[8]), qo, ko, status_of(a[11]), stream());
 }
 
 // dims, cache, page_table, cu, k_out, v_out, dev_status, stream
@@ -227,8 +270,8 @@ moe_status_t cache_read(PyObject* const* a) {
   const int64_t tokens = k.dim() == 3 ? k.size(0) : -1;
   uint16_t* ko = out_rows(a[4], tokens, d.kv_heads, d.head_dim, "k_out");
   uint16_t* vo = out_rows(a[5], tokens, d.kv_heads, d.head_dim, "v_out");
-  return moe_cache_read(d, structure<moe_kv_cache_t>(a[1], "cache"), pages, to_int32(batch, "page_table"),
-                        to_int32(width, "page_table"), cu, to_int32(tokens, "k_out"), ko, vo, status_of(a[6]), stream_of(a[7]));
+  return moe_cache_read(d, kv_cache(a[1]), pages, to_int32(batch, "page_table"),
+                        to_int32(width, "page_table"), cu, to_int32(tokens, "k_out"), ko, vo, status_of(a[6]), stream());
 }
 
 // dims, q, k, v, cu_q, cu_k, max_k, scale, out, ws, causal, dev_status, stream
@@ -243,13 +286,13 @@ moe_status_t attn_prefill(PyObject* const* a) {
   return moe_attn_prefill(d, to_int32(n, "cu_q") - 1, to_int32(q.n, "q"), to_int32(k.n, "k"), integer32(a[6], "max_k"), q.p,
                           q.stride, k.p, k.stride, v.p, v.stride, cu_q, cu_k, real(a[7]), truth(a[10]),
                           out_rows(a[8], q.n, d.q_heads, d.head_dim, "out"), status_of(a[11]), ws, (size_t)ws_bytes,
-                          stream_of(a[12]));
+                          stream());
 }
 
 // dims, q, cache, page_table, lens, max_len, scale, out, ws, prefix_pages, prefix_len, dev_status, stream
 moe_status_t attn_decode(PyObject* const* a) {
   const auto d = structure<moe_attn_dims_t>(a[0], "dims");
-  const auto c = structure<moe_kv_cache_t>(a[2], "cache");
+  const auto c = kv_cache(a[2]);
   int64_t batch, width, n, n_prefix, ws_bytes;
   const int32_t* pages = matrix<int32_t>(a[3], "page_table", batch, width);
   const Rows q(a[1], d.q_heads, d.head_dim, "q");
@@ -263,7 +306,7 @@ moe_status_t attn_decode(PyObject* const* a) {
   return moe_attn_decode(d, to_int32(batch, "page_table"), q.p, q.stride, c, pages, to_int32(width, "page_table"), lens,
                          integer32(a[5], "max_len"), prefix, prefix_len, real(a[6]),
                          out_rows(a[7], batch, d.q_heads, d.head_dim, "out"), status_of(a[11]), ws, (size_t)ws_bytes,
-                         stream_of(a[12]));
+                         stream());
 }
 
 template <moe_status_t (*kCall)(PyObject* const*), int kArgs>

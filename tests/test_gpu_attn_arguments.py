@@ -67,3 +67,50 @@ def test_a_flag_that_has_no_truth_value(call):
         call("moe_attn_prefill", causal=Vague())
     call("moe_attn_prefill", causal=0)
     call("moe_attn_prefill", causal=np.True_)
+
+
+class Elsewhere(torch.Tensor):
+    @classmethod
+    def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+        raise NotImplementedError(func)
+
+
+def elsewhere(t):
+    """A tensor like t that says it is on another device (and has no memory)."""
+    return torch.Tensor._make_wrapper_subclass(Elsewhere, t.shape, strides=t.stride(), dtype=t.dtype,
+                                               device=torch.device("cuda:1"))
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_tensors_of_another_device(call, name):
+    """A call runs on its stream's device, the current one's if none is given."""
+    assert torch.cuda.current_device() == 0
+    streams = (None, torch.cuda.current_stream())
+    for stream in streams:
+        for key, value in call.args[name].items():
+            if isinstance(value, torch.Tensor):
+                with pytest.raises(ValueError, match=f"{key} is on another device"):
+                    call(name, **{key: elsewhere(value)}, stream=stream)
+        call(name, stream=stream)
+
+    class Handle:
+        cuda_stream = torch.cuda.current_stream().cuda_stream
+    call(name, stream=Handle())
+
+
+def test_caches_and_tables_of_another_device(call, moe):
+    codes, scales = torch.zeros((3, 2, 16, 64), dtype=torch.uint8, device="cuda"), torch.zeros((3, 2, 16), device="cuda")
+    for i in range(4):
+        parts = [codes, codes, scales, scales]
+        parts[i] = elsewhere(parts[i])
+        with pytest.raises(ValueError, match="different devices"):
+            moe.KVCache(*parts)
+    cache = moe.KVCache(codes, codes, scales, scales)
+    cache.on_device.device = 1
+    for name in ("moe_rope_cache", "moe_cache_read", "moe_attn_decode"):
+        with pytest.raises(ValueError, match="cache is on another device"):
+            call(name, cache=cache)
+    with pytest.raises(ValueError, match="table is on another device"):
+        moe.moe_rope_table(elsewhere(torch.zeros((8, 64), device="cuda")))
+    with pytest.raises(ValueError, match="table is on another device"):
+        moe.moe_rope_table(elsewhere(torch.zeros((8, 64), device="cuda")), stream=torch.cuda.current_stream())
