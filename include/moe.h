@@ -576,7 +576,9 @@ moe_status_t moe_cache_read(moe_attn_dims_t dims, moe_kv_cache_t cache, const in
  * over the keys j of i's own sequence; with causal != 0 over those up to i's
  * place, sequences' ends aligned: query i of lq sees keys 0 .. i + lk - lq (a
  * chunk of queries behind keys that are cached already).  A query that sees no
- * key gets zeros, and keys and values that a query does not see may hold
+ * key gets zeros, as does one whose scores are all -inf (a score of -inf weighs
+ * nothing); any other whose product with log2(e) fp32 holds is weighed.  Keys and
+ * values that a query does not see may hold
  * anything, NaN too.  Scores, the running maximum and sum and the accumulation are
  * fp32; the softmax's numerators are rounded to bf16 for the product with v (and
  * their sum is that of the rounded ones).

@@ -12,10 +12,10 @@ typedef float v2f __attribute__((ext_vector_type(2)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef int v2i __attribute__((ext_vector_type(2)));
 
-// The running maximum of scores before the first key: finite, so that
-// exp2(kNoScore - m) is 0 and masked scores (-inf) give exp2(-inf) = 0 against
-// it, never exp2(-inf + inf).
-constexpr float kNoScore = -1e30f;
+// The running maximum of scores before the first key: the lowest finite value, so
+// that no score lies below it but -inf, a masked key's, and exp2(-inf - m) is 0
+// against it, never exp2(-inf + inf).
+constexpr float kNoScore = -3.402823466e+38f;
 constexpr float kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
