@@ -48,6 +48,7 @@ struct PrefillArgs {
   uint32_t group_inverse;  // ceil(2^21 / group): n / group = n * group_inverse >> 21 for n < 1280, group <= 1024
   int parts, part_tiles;   // key tiles are cut into parts of this many, the last takes what is left
   float c;  // scale * log2(e): the softmax runs on powers of 2
+  uint32_t looks;  // the workgroup that looks at the offsets
 };
 
 constexpr int kKeys = 64;  // keys per tile
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
 
   // With a status word the grid has one workgroup more, which looks at the offsets (a sequence that is cut to nothing has
   // no tile, and the tiles' workgroups need not look behind theirs).
-  if (a.status && blockIdx.x == gridDim.x - 1) {
+  if (blockIdx.x == a.looks) {
     report_offsets(a);
     return;
   }
@@ -650,7 +651,7 @@ size_t prefill_workspace(const moe_attn_dims_t& d, int32_t T_q, int32_t max_k) {
 }
 
 template <int D>
-moe_status_t launch_prefill(const PrefillArgs& a, const PrefillPlan& p, hipStream_t stream) {
+moe_status_t launch_prefill(PrefillArgs a, const PrefillPlan& p, hipStream_t stream) {
   // Heads fastest: workgroups that share keys have numbers equal mod 8 (one XCD's L2) where kv_heads is a multiple of
   // 8, and all heads' longest rows come first.
   const int64_t items = p.tiles * a.parts * a.kv_heads, rows = (int64_t)a.T_q * a.kv_heads * a.group;
@@ -658,6 +659,7 @@ moe_status_t launch_prefill(const PrefillArgs& a, const PrefillPlan& p, hipStrea
   if ((items + 1) * kWaves * 64 >= (int64_t)1 << 32 || (rows / kJoinRows + 1) * 256 >= (int64_t)1 << 32)
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_attn_prefill: %lld row tiles", (long long)items);
   const dim3 grid((unsigned)items + (a.status ? 1 : 0));
+  a.looks = a.status ? (uint32_t)items : ~0u;
   if (p.split)
     MOE_LAUNCH("attn_prefill", (attn_prefill_kernel<D, kWaves, true>), grid, dim3(64 * kWaves), 0, stream, a);
   else
@@ -706,6 +708,6 @@ extern "C" moe_status_t moe_attn_prefill(moe_attn_dims_t d, int32_t B, int32_t T
                       p.parts > 1 ? reinterpret_cast<float*>(base + p.o_bytes) : nullptr, dev_status,
                       B, T_q, T_k, d.kv_heads, d.q_heads / d.kv_heads, causal != 0,
                       (uint32_t)(((1 << 21) + d.q_heads / d.kv_heads - 1) / (d.q_heads / d.kv_heads)), p.parts, p.part_tiles,
-                      scale * kLog2e};
+                      scale * kLog2e, ~0u};
   return d.head_dim == 64 ? launch_prefill<64>(a, p, stream) : launch_prefill<128>(a, p, stream);
 }

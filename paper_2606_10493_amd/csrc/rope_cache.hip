@@ -232,10 +232,10 @@ __global__ __launch_bounds__(256) void cache_read_kernel(moe_kv_cache_t cache, i
                                                          const int32_t* __restrict__ pages, int B, int width,
                                                          const int32_t* __restrict__ cu, int T,
                                                          uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out,
-                                                         int32_t* status) {
+                                                         int32_t* status, uint32_t looks) {
   constexpr int kLanes = D / 8, kTokens = 256 / kLanes;
   const int sub = threadIdx.x % kLanes;
-  if (status && blockIdx.x == gridDim.x - 1) {
+  if (blockIdx.x == looks) {
     if (blockIdx.y > 0) return;
     bool cut = false;
     for (int64_t i = threadIdx.x; i < B; i += 256) cut |= cu[i] < 0 || cu[i + 1] > T || cu[i] > cu[i + 1];
@@ -368,14 +368,15 @@ extern "C" moe_status_t moe_cache_read(moe_attn_dims_t d, moe_kv_cache_t cache, 
   if (T > kSpanTokens) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_cache_read: T=%d is over %lld", T, (long long)kSpanTokens);
   const unsigned gx = (unsigned)((T + per - 1) / per);
   const int heads = gx < 1024 ? 1 : d.kv_heads;  // few tokens: more workgroups rather than longer ones
+  const uint32_t looks = dev_status ? gx : ~0u;  // the column that looks at the offsets
   const dim3 grid(gx + (dev_status ? 1 : 0), (d.kv_heads + heads - 1) / heads);
   if (d.head_dim == 64)
     MOE_LAUNCH("cache_read", cache_read_kernel<64>, grid, dim3(256), 0, stream, cache, shift, d.kv_heads, heads,
                page_table, B,
-               table_width, cu, T, k_out, v_out, dev_status);
+               table_width, cu, T, k_out, v_out, dev_status, looks);
   else
     MOE_LAUNCH("cache_read", cache_read_kernel<128>, grid, dim3(256), 0, stream, cache, shift, d.kv_heads, heads,
                page_table, B,
-               table_width, cu, T, k_out, v_out, dev_status);
+               table_width, cu, T, k_out, v_out, dev_status, looks);
   return check_launch("moe_cache_read");
 }
