@@ -557,7 +557,8 @@ moe_status_t moe_rope_cache(moe_attn_dims_t dims, int32_t T, const uint16_t* q, 
 /*
  * Reads cached sequences back: rows cu[b] .. cu[b+1] - 1 of k_out and v_out =
  * bf16(code * scale) of the first cu[b+1] - cu[b] tokens that row b of the page
- * table holds.  page_table: device int32 [B, table_width], rows contiguous.
+ * table holds.  page_table: device int32 [B, table_width], rows contiguous; may be
+ * NULL with table_width 0.
  * cu: device int32 [B + 1], not decreasing; rows outside 0..T - 1 are left out.
  * Offsets that leave 0..T, or decrease, set MOE_DEV_BAD_LENGTH (a call with B or T
  * 0 launches nothing and looks at nothing).  k_out, v_out:
@@ -612,8 +613,8 @@ moe_status_t moe_attn_prefill(moe_attn_dims_t dims, int32_t B, int32_t T_q, int3
  * all sequences share (a prompt's prefix written once); NULL with prefix_len
  * 0.  A long prefix is read once for the whole batch, every sequence's queries
  * being rows of one product (a short one by each sequence for itself, which
- * costs less).  page_table: device int32 [B, table_width], entries behind a
- * sequence's last page are not used.  lens: device int32 [B], 0 for
+ * costs less).  page_table: device int32 [B, table_width] (NULL with table_width 0:
+ * no sequence has keys of its own), entries behind a sequence's last page are not used.  lens: device int32 [B], 0 for
  * an idle slot (with no prefix either its output is zeros).  A length below 0
  * or beyond table_width pages (or 2^30) is cut and sets MOE_DEV_BAD_LENGTH; a page id
  * outside the cache sets MOE_DEV_BAD_PAGE and leaves the outputs that need it

@@ -773,7 +773,7 @@ extern "C" moe_status_t moe_attn_decode(moe_attn_dims_t d, int32_t B, const uint
   if (!(scale > 0.0f) || !isfinite(scale * kLog2e)) return fail(MOE_ERR_INVALID_ARG, "moe_attn_decode: scale=%g", scale);
   if (B == 0) return MOE_OK;
   if ((st = check_rows(q, q_stride, d.q_heads, d.head_dim, "moe_attn_decode", "q")) != MOE_OK) return st;
-  if (!page_table || !lens || !out || (prefix_len > 0 && !prefix_pages))
+  if ((!page_table && table_width > 0) || !lens || !out || (prefix_len > 0 && !prefix_pages))
     return fail(MOE_ERR_INVALID_ARG, "moe_attn_decode: null pointer");
   if (!aligned(out, 16)) return fail(MOE_ERR_INVALID_ARG, "moe_attn_decode: out must be 16-byte aligned");
   const DecodePlan p = plan_decode(d, B, max_len, prefix_len);

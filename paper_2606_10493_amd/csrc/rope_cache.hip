@@ -361,7 +361,7 @@ extern "C" moe_status_t moe_cache_read(moe_attn_dims_t d, moe_kv_cache_t cache, 
   if (B < 0 || T < 0 || table_width < 0)
     return fail(MOE_ERR_INVALID_ARG, "moe_cache_read: B=%d T=%d table_width=%d", B, T, table_width);
   if (B == 0 || T == 0) return MOE_OK;
-  if (!page_table || !cu || !k_out || !v_out) return fail(MOE_ERR_INVALID_ARG, "moe_cache_read: null pointer");
+  if ((!page_table && table_width > 0) || !cu || !k_out || !v_out) return fail(MOE_ERR_INVALID_ARG, "moe_cache_read: null pointer");
   if (!aligned(k_out, 16) || !aligned(v_out, 16))
     return fail(MOE_ERR_INVALID_ARG, "moe_cache_read: outputs must be 16-byte aligned");
   const int shift = log2_of(cache.page_size), per = 256 / (d.head_dim / 8);

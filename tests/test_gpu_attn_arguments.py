@@ -3,7 +3,9 @@ import numpy as np
 import pytest
 import torch
 
+from attention_cases import Cache, bf16
 from gpu_cases import require_gpu
+from oracle import attention_oracle as ao
 from test_gpu_attn_binding import NAMES, Call
 
 pytestmark = pytest.mark.gpu
@@ -114,3 +116,30 @@ def test_caches_and_tables_of_another_device(call, moe):
         moe.moe_rope_table(elsewhere(torch.zeros((8, 64), device="cuda")))
     with pytest.raises(ValueError, match="table is on another device"):
         moe.moe_rope_table(elsewhere(torch.zeros((8, 64), device="cuda")), stream=torch.cuda.current_stream())
+
+
+@pytest.mark.parametrize("prefix", [40, 2000])
+def test_tables_without_columns(moe, prefix):
+    """Sequences that have nothing of their own yet: a table of no pages, which has no address."""
+    rng = np.random.default_rng(71)
+    cache = Cache(moe, rng, [prefix], 2, 64, 16)
+    q, qv = bf16(rng.standard_normal((3, 4, 64)))
+    d = moe.MoeAttnDims(4, 2, 64)
+    none = torch.empty((3, 0), dtype=torch.int32, device="cuda")
+    zero = torch.zeros(3, dtype=torch.int32, device="cuda")
+    out, status = torch.empty_like(q), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(256, moe.moe_attn_decode_workspace(d, 3, 0, prefix)), dtype=torch.uint8, device="cuda")
+    moe.moe_attn_decode(d, q, cache.dev, none, zero, 0, 0.1, out, ws, prefix_pages=torch.from_numpy(cache.table[0]).cuda(),
+                        prefix_len=prefix, dev_status=status)
+    for h in range(4):
+        ref, bound = ao.attention(qv[:, h], cache.values["k"][0][h // 2], cache.values["v"][0][h // 2], 0.1)
+        assert np.all(np.abs(out[:, h].double().cpu().numpy() - ref) <= bound)
+    assert int(status.item()) == 0
+    moe.moe_attn_decode(d, q, cache.dev, none, zero, 0, 0.1, out, ws)
+    assert not out.any()
+    rows = [torch.full((5, 2, 64), 9.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    moe.moe_cache_read(d, cache.dev, none, torch.zeros(4, dtype=torch.int32, device="cuda"), *rows, status)
+    assert int(status.item()) == 0 and all(bool((r == 9).all()) for r in rows)
+    moe.moe_cache_read(d, cache.dev, none, torch.tensor([0, 0, 2, 2], dtype=torch.int32, device="cuda"), *rows, status)
+    assert int(status.item()) == moe.MOE_DEV_BAD_LENGTH
+    assert all(not r[:2].any() and bool((r[2:] == 9).all()) for r in rows)
