@@ -411,7 +411,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     wait_async_and_barrier<0>();  // no fetch is on its way to LDS, and no wave reads from it any more
 
     // A product multiplies a hidden key's value by 0, which an infinite or NaN value does not survive.  If a sum is not
-    // finite, the wave takes its sums again, key by key, from what each row sees; maxima and denominators stand.
+    // finite, the wave takes its sums again; maxima and denominators stand.  Tiles that all its rows see whole are products
+    // as before, their operands straight from memory; in the others every key is weighed for the rows that see it alone.
+    // 16384 tokens of 32 heads of 128 with an infinite value that all rows see: 9.6 ms (164 key by key), 2.2 without.
     float finite = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
@@ -420,26 +422,64 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_kernel(PrefillArgs
     if (__any(finite != 0.0f)) {
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) o[i] = v16f{};
-      for (int tile = first; tile < kt1; tile += kSplit ? 2 : 1)
-        for (int j = tile * kKeys; j <= min(tile * kKeys + kKeys - 1, tile_last); ++j) {
-          float score = 0.0f;
+      int tile = first;
+#pragma unroll 1
+      for (; tile < n_free; tile += kSplit ? 2 : 1) {
+        s[0] = s[1] = v16f{};
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            const v8bf key = *reinterpret_cast<const v8bf*>(kbase + j * a.k_stride + 16 * i + 8 * h);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) score = fmaf((float)qf[i][e], (float)key[e], score);
-          }
-          score += __shfl_xor(score, 32, 64);
-          const float w = (float)(__bf16)__builtin_amdgcn_exp2f(fmaf(score, a.c, -m));
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            const uint2 x = *reinterpret_cast<const uint2*>(vbase + j * a.v_stride + 8 * i + 4 * h);
-            const float v[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
-                                __uint_as_float(x.y & 0xffff0000u)};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[i / 4][4 * (i % 4) + e] += j <= limit ? w * v[e] : 0.0f;
-          }
+        for (int f = 0; f < kK; ++f) {
+          const int64_t key = tile * kKeys + 32 * (f & 1) + col;
+          const v8bf x = *reinterpret_cast<const v8bf*>(kbase + key * a.k_stride + 16 * (f >> 1) + 8 * h);
+          s[f & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[f >> 1], s[f & 1], 0, 0, 0);
         }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2)
+            p.x[8 * u + i / 2] = pack_bf16(__builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.c, -m)),
+                                           __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i + 1], a.c, -m)));
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt) {
+            union {
+              v8bf v;
+              uint16_t x[8];
+            } y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int64_t key = tile * kKeys + 16 * w + 8 * (e / 4) + 4 * h + (e & 3);
+              y.x[e] = vbase[key * a.v_stride + 32 * dt + col];
+            }
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y.v, p.v[w], o[dt], 0, 0, 0);
+          }
+      }
+#pragma unroll 1
+      for (; tile < kt1; tile += kSplit ? 2 : 1)
+#pragma unroll 1
+        for (int j0 = tile * kKeys; j0 <= min(tile * kKeys + kKeys - 1, tile_last); j0 += 4)  // four on their way at once
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int64_t j = min(j0 + x, tile_last);  // (limit <= tile_last)
+            const bool sees = j0 + x <= limit;
+            float score = 0.0f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+              const v8bf key = *reinterpret_cast<const v8bf*>(kbase + j * a.k_stride + 16 * i + 8 * h);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) score = fmaf((float)qf[i][e], (float)key[e], score);
+            }
+            score += __shfl_xor(score, 32, 64);
+            const float w = (float)(__bf16)__builtin_amdgcn_exp2f(fmaf(score, a.c, -m));
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {
+              const uint2 y = *reinterpret_cast<const uint2*>(vbase + j * a.v_stride + 8 * i + 4 * h);
+              const float v[4] = {__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xffff0000u), __uint_as_float(y.y << 16),
+                                  __uint_as_float(y.y & 0xffff0000u)};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i / 4][4 * (i % 4) + e] += sees ? w * v[e] : 0.0f;
+            }
+          }
     }
   }
 
