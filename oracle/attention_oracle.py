@@ -12,6 +12,7 @@ import numpy as np
 from .moe_oracle import E4M3_MAX, bf16_to_f32, e4m3_decode, e4m3_encode
 
 BF16_ROUNDOFF = 2.0 ** -8  # half the spacing of bf16 above 1: 7 stored bits of mantissa
+TWO_BF16_ROUNDOFF = 2.0 ** -16  # a number as a rounded bf16 and the rounded rest, which is at most 2^-8 of it
 
 
 def rope_frequencies(rot_dim, base, scaling="plain", factor=1.0, original_len=1.0, slow_turns=1.0, fast_turns=32.0):
@@ -61,14 +62,15 @@ def cached_rows(codes, scales):
     return e4m3_decode(codes).astype(np.float32) * scales[..., None].astype(np.float32)
 
 
-def attention(q, k, v, scale, visible=None):
+def attention(q, k, v, scale, visible=None, numerators=BF16_ROUNDOFF):
     """fp64 attention of rows q [n, dim] over k, v [t, dim] and a bound on a kernel's error.
 
     visible: bool [n, t] (None: all).  Returns (out [n, dim], bound [n, dim]).
 
     The bound follows from the roundings of the definition: the softmax's
     numerators are rounded to bf16 for the product with v (unit roundoff 2^-8, 8
-    significant bits, of every term), the result to bf16 (2^-8 of it); scores are sums of dim products
+    significant bits, of every term; `numerators`: TWO_BF16_ROUNDOFF where they are
+    two bf16 each), the result to bf16 (2^-8 of it); scores are sums of dim products
     in fp32, so a score is off by at most (dim + 8) 2^-24 of the sum of its terms'
     magnitudes, which moves its numerator by that much relatively and the
     denominator no more; 2^-18 covers the exponential, the sums' fp32 roundings
@@ -91,7 +93,7 @@ def attention(q, k, v, scale, visible=None):
     out, terms = p @ v, p @ np.abs(v)
     seen = np.where(p > 2.0 ** -40, size, 0.0).max(1, keepdims=True)
     moved = 2.0 * (dim + 8) * 2.0 ** -24 * seen + 2.0 ** -18
-    return out, (BF16_ROUNDOFF + moved) * terms + BF16_ROUNDOFF * np.abs(out) + 1e-30
+    return out, (numerators + moved) * terms + BF16_ROUNDOFF * np.abs(out) + 1e-30
 
 
 def packed_attention(q, k, v, cu_q, cu_k, scale, causal, want=None):
