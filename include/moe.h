@@ -582,7 +582,9 @@ moe_status_t moe_cache_read(moe_attn_dims_t dims, moe_kv_cache_t cache, const in
  * values that a query does not see may hold
  * anything, NaN too.  Scores, the running maximum and sum and the accumulation are
  * fp32; the softmax's numerators are rounded to bf16 for the product with v (and
- * their sum is that of the rounded ones).
+ * their sum is that of the rounded ones).  The division comes last: values of
+ * 2^120 / (keys of the query) and more may overflow.  An infinite or NaN value that a
+ * query sees costs time: a call may take ten times as long.
  *
  * Sequence b: queries cu_q[b] .. cu_q[b+1] - 1 of T_q, keys cu_k[b] ..
  * cu_k[b+1] - 1 of T_k (device int32 [B + 1], not decreasing); offsets that

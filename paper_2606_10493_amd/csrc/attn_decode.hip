@@ -19,10 +19,12 @@
 //
 // Bound by memory: head_dim + 4 bytes per key, value and head against 4 * G *
 // head_dim flops.  64 sequences of up to 8192 keys: 77 us, 5.2 TB/s (a kernel that
-// only loads the same takes as long); one of 65536: 25 us, 5.5 TB/s.  On a prefix,
-// where a key serves 16 NCP columns, bound by the vector instructions of a step:
-// 48 sequences behind 8191 shared keys 26 us, of which 15 are eight steps of about
-// 330 instructions beside 48 MFMAs, two waves to a SIMD.
+// only loads the same takes as long), and 81 with the join; one of 65536: 25 us, 5.5
+// TB/s, and 34 until the join has ended.  On a prefix, where a key serves 16 NCP
+// columns, by latencies: 48 sequences behind 8191 shared keys 26 us, of which 15 are
+// eight steps of about 330 instructions beside 48 MFMAs, two waves to a SIMD, and the
+// rest is finding the piece, the first loads and joining the waves' sums (vector
+// instructions take 26 % of the SIMDs' cycles, the matrix cores 13 %).
 //
 // A head's work is a line of steps of 128 keys (32 for each wave of a
 // workgroup): the prefix's for every block of columns, then the sequences' one
@@ -655,6 +657,9 @@ struct DecodePlan {
 // against two: 1 sequence of 512 keys 6.8 against 8.2, of 1024 10.6 against 8.4; 32
 // of up to 1024 11.9 against 14.6, of up to 2048 19.3 against 18.6; 48 of up to 500
 // behind 120 shared ones 11.5 against 16.4, of up to 250 behind 1500 23 against 19.
+// The estimates know neither the memory's rate nor how the lengths differ: 48 of 4000
+// keys each 75 us in one launch (which they choose) and 76 in two, of up to 4000 40
+// and 34.
 double whole_gains(const DecodePlan& p, const moe_attn_dims_t& d, int32_t B, int32_t own_steps, int32_t prefix_steps) {
   const double groups = (double)p.own_blocks * B * d.kv_heads;
   const double line = 2.0 * p.prefix_blocks * prefix_steps + (double)p.own_blocks * B * own_steps;

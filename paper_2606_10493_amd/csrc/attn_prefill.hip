@@ -19,12 +19,15 @@
 //
 // Bound by the matrix cores, 4 * head_dim flops per row and key, and by the power
 // that they draw when all are busy (the clock falls to 1.6 - 2.0 GHz).  16384
-// causal tokens of 32 heads of 128: 1.86 ms, 1180 TFLOP/s, where the largest
-// library products reach 1340.  Eight prompts of 357 to 2048 tokens: 143 us, 860
-// TFLOP/s; their 1248 workgroups of unequal length end unevenly.  Where there are
-// fewer workgroups than CUs, a call takes 5 us and 1.4 us for each key tile of the
-// longest rows: rows are then shared by two halves of a workgroup's waves, and keys
-// cut into parts.
+// causal tokens of 32 heads of 128: 1.86 to 1.94 ms from card to card, 1140 to 1180
+// TFLOP/s, where the largest library products reach 1340.  Eight prompts of 357 to
+// 2048 tokens: 147 to 152 us, 810 to 830 TFLOP/s, the matrix cores busy for 41 % of
+// the cycles; their 1248 workgroups of unequal length end unevenly, each with a
+// beginning and an end that nothing covers.  Where there are fewer workgroups than
+// CUs, a call takes 5 us and 1.4 us for each key tile of the longest rows: rows are
+// then shared by two halves of a workgroup's waves, and keys cut into parts.  Heads
+// of 64 are bound by the vector phase and by their longest rows (403 and 2995 tokens
+// of 24 heads over 8: 60 us for 28 GFLOP).
 #include <math.h>
 
 #include <algorithm>
@@ -621,7 +624,8 @@ struct PrefillPlan {
 // The height of the row tiles and the number of parts that the keys are cut into:
 // those whose estimated time is the least.  A CU runs one workgroup at a time; one
 // takes about 5 us and a step for each of its key tiles, or 6.3 us and a longer
-// step for each two of them.  Joining parts costs a launch, 4.5 us, and their sums go
+// step for each two of them (a step takes a third longer than assumed where all CUs
+// are busy: the 34 tiles of a part below 72 us, not 54).  Joining parts costs a launch, 4.5 us, and their sums go
 // to memory and back at about 4 TB/s.  Whole rows against halves: 1040 tokens of 16
 // heads of 64 23.7 and 17.1 us, 206 tokens of 40 heads over 8 of 128 behind 320
 // keys 18.5 and 15.5; where the card is full, eight prompts of up to 2048 tokens,
