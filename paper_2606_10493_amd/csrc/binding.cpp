@@ -38,8 +38,9 @@ int64_t attribute(PyObject* o, const char* name) {
   return v;
 }
 
-// The stream of the call that runs (the interpreter's lock is held) and its device: the caller's torch stream, or the
-// current device's current one.  Taken once, by the first tensor.
+// The stream of the call that runs and its device: the caller's torch stream, or the current device's current one.
+// Taken once, by the first tensor.  An argument may be an object whose attributes are Python code, which may make calls
+// of its own and let other threads run: each thread has its own, and a call puts back what it found.
 struct Stream {
   PyObject* given = nullptr;
   hipStream_t handle = nullptr;
@@ -57,7 +58,15 @@ struct Stream {
                                                              : c10::hip::getCurrentHIPStream().device_index();
     }
   }
-} call_stream;
+};
+
+thread_local Stream call_stream;
+
+struct OwnStream {
+  const Stream before = call_stream;
+  explicit OwnStream(PyObject* given) { call_stream = Stream{given}; }
+  ~OwnStream() { call_stream = before; }
+};
 
 void on_call_device(int64_t index, const char* name) {
   call_stream.take();
@@ -205,7 +214,7 @@ PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n) {
     PyErr_Format(PyExc_TypeError, "%d arguments expected, %zd given", kArgs, n);
     return nullptr;
   }
-  call_stream = Stream{a[kArgs - 1]};
+  const OwnStream own(a[kArgs - 1]);
   try {
     return PyLong_FromLong(kCall(a));
   } catch (const Bad&) {

@@ -143,3 +143,22 @@ def test_tables_without_columns(moe, prefix):
     moe.moe_cache_read(d, cache.dev, none, torch.tensor([0, 0, 2, 2], dtype=torch.int32, device="cuda"), *rows, status)
     assert int(status.item()) == moe.MOE_DEV_BAD_LENGTH
     assert all(not r[:2].any() and bool((r[2:] == 9).all()) for r in rows)
+
+
+def test_a_call_within_a_call(call, moe):
+    """A stream whose handle comes from Python code, which makes calls of its own on another: each call has its own stream."""
+    class Far:
+        cuda_stream, device_index = 0, 1
+
+    class Nested:
+        device_index = 0
+
+        @property
+        def cuda_stream(self):
+            with pytest.raises(ValueError, match="another device"):
+                call("moe_attn_decode", stream=Far())
+            return torch.cuda.current_stream().cuda_stream
+    for name in NAMES:
+        call(name, stream=Nested())
+        with pytest.raises(ValueError, match="another device"):
+            call(name, stream=Far())
