@@ -61,9 +61,10 @@ class KVCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.kv_heads, self.page_size, self.head_dim = k.shape[1:]
         self.n_pages = k.shape[0]
-        self.c = MoeKvCache(_dev(k, 1, "k"), _dev(v, 1, "v"), _dev(k_scale, 4, "k_scale"), _dev(v_scale, 4, "v_scale"),
-                            k.shape[0], k.shape[2])
-        self.on_device = _DeviceCache(self.c, k.device.index)
+        c = MoeKvCache(_dev(k, 1, "k"), _dev(v, 1, "v"), _dev(k_scale, 4, "k_scale"), _dev(v_scale, 4, "v_scale"),
+                       k.shape[0], k.shape[2])
+        self.on_device = _DeviceCache(c, k.device.index)
+        self.c = self.on_device.cache
 
     @classmethod
     def empty(cls, n_pages: int, kv_heads: int, page_size: int, head_dim: int, device="cuda"):

@@ -32,7 +32,7 @@ BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
-CXX = os.environ.get("CXX", "g++")
+CXX = "g++"
 PYTHON_INCLUDE = sysconfig.get_paths()["include"]
 
 CFLAGS = [

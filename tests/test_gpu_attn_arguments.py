@@ -162,3 +162,10 @@ def test_a_call_within_a_call(call, moe):
         call(name, stream=Nested())
         with pytest.raises(ValueError, match="another device"):
             call(name, stream=Far())
+
+
+def test_the_cache_and_its_structure_are_one(moe):
+    cache = moe.KVCache.empty(3, 2, 16, 64)
+    assert bytes(cache.c) == bytes(cache.on_device)[:len(bytes(cache.c))]
+    cache.c.n_pages = 2
+    assert cache.on_device.cache.n_pages == 2
