@@ -19,7 +19,7 @@
 //
 // Bound by the matrix cores, 4 * head_dim flops per row and key, and by the power
 // that they draw when all are busy (the clock falls to 1.6 - 2.0 GHz).  16384
-// causal tokens of 32 heads of 128: 1.86 to 1.94 ms from card to card, 1140 to 1180
+// causal tokens of 32 heads of 128: 1.86 to 1.95 ms from card to card, 1130 to 1180
 // TFLOP/s, where the largest library products reach 1340.  Eight prompts of 357 to
 // 2048 tokens: 147 to 152 us, 810 to 830 TFLOP/s, the matrix cores busy for 41 % of
 // the cycles; their 1248 workgroups of unequal length end unevenly, each with a
