@@ -24,6 +24,13 @@
  *   moe_attn_decode  attention of one token per sequence over the cache,
  *                   a prefix that all sequences share computed once
  *
+ * and what stands between and beside the two halves:
+ *
+ *   moe_add_norm    residual addition and root-mean-square norm, its result in
+ *                   bf16, in e4m3 codes with their scales, or in both
+ *   moe_linear_w4   products with a matrix of 4-bit weights (projections)
+ *   moe_expert_ffn_w4, moe_ffn_layer_w4  routed experts with 4-bit weights
+ *
  * Conventions (all entry points):
  *   - Every pointer is owned by the caller.  "device" pointers are HIP device
  *     memory of the current device; "pinned host" pointers come from
@@ -70,6 +77,8 @@ typedef enum {
 #define MOE_DEV_BAD_SLOT 8       /* a cache slot beyond the last page */
 #define MOE_DEV_BAD_PAGE 16      /* a page id outside [0, n_pages) */
 #define MOE_DEV_BAD_LENGTH 32    /* lengths or offsets that leave their tensors or page tables */
+/* Bit OR-ed in by moe_pack_weight_w4. */
+#define MOE_DEV_BAD_SCALE 64     /* a scale byte above 252 */
 
 /* Kernel family used by moe_expert_ffn.  AUTO picks DECODE for
  * tokens <= MOE_DECODE_MAX_TOKENS, else PREFILL; both compute the same
@@ -631,6 +640,139 @@ moe_status_t moe_attn_decode(moe_attn_dims_t dims, int32_t B, const uint16_t* q,
                              const int32_t* page_table, int32_t table_width, const int32_t* lens, int32_t max_len,
                              const int32_t* prefix_pages, int32_t prefix_len, float scale, uint16_t* out,
                              int32_t* dev_status, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Norm between the layer's halves.
+ * ---------------------------------------------------------------------------
+ */
+typedef enum {
+  MOE_BF16 = 0,
+  MOE_F32 = 1
+} moe_float_t;
+
+typedef struct {
+  float eps;             /* added to the mean square: at least 1e-12 */
+  float weight_offset;   /* added to every weight (1 for weights stored less one) */
+  int32_t heads;         /* rows of a token that are normalised each by itself (1: the whole token) */
+  int32_t x_type;        /* moe_float_t of x */
+  int32_t stream_type;   /* moe_float_t of residual and sum */
+} moe_norm_cfg_t;
+
+/*
+ * Residual addition and root-mean-square norm of rows of H values:
+ *   z = x + residual
+ *   y = z / sqrt(mean(z^2) + eps) * (weight + weight_offset)
+ * in fp32; sum = z and out = y rounded once, q and s the e4m3 codes and scales
+ * of the unrounded y by the rule of moe_quant_act (what moe_expert_ffn reads).
+ *
+ * T tokens of `heads` rows each: row (t, h) of x begins t * x_stride + h * H
+ * elements into it, of residual, sum and out likewise with theirs; q is
+ * [T * heads, H] and s [T * heads, H / 128], contiguous.  So x may be the query
+ * heads of a packed projection.  residual (no addition), weight (ones), sum,
+ * out, q and s may be NULL; q and s come together, and one of out and q is
+ * there.  sum may be residual, and out or sum may be x, where type and stride are the
+ * same; any other overlap of an output is an error of the caller.
+ * H a multiple of 8, and of 128 with q, 8..32768; else
+ * MOE_ERR_UNSUPPORTED_SHAPE.  Strides are multiples of 8 and at least heads * H;
+ * pointers are 16-byte aligned (q 8, s 4).  z has to fit fp32; its squares need
+ * not.  weight: device bf16 [H].
+ */
+moe_status_t moe_add_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                          const uint16_t* weight_bf16, int32_t T, int32_t H, moe_norm_cfg_t cfg, void* sum,
+                          int64_t sum_stride, uint16_t* out_bf16, int64_t out_stride, uint8_t* q, float* s,
+                          hipStream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * 4-bit weights.
+ *
+ * A [rows, cols] matrix is stored as e2m1 codes (sign, two bits of exponent, one
+ * of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6), two to a byte with the even column in
+ * the low nibble, and one scale byte b for 32 consecutive columns of a row:
+ * value = e2m1 * 2^(b - 127).  Scale bytes go up to 252 (6 * 2^125 is the largest
+ * that bf16 holds); weights below 2^-126 may count as zero in products.
+ * The products take bf16 activations, every weight being exact in bf16, and add
+ * up in fp32.
+ * ---------------------------------------------------------------------------
+ */
+#define MOE_W4_GROUP 32
+
+/*
+ * Weight quantization, w: device fp32 [n_mats, rows, cols] -> q: device
+ * [n_mats, rows, cols / 2], s: device [n_mats, rows, cols / 32].  Per group: the
+ * smallest scale 2^e, -120 <= e <= 120, that leaves no magnitude above 7 * 2^e
+ * (so that none is off by more than half a step of the codes there), code = nearest e2m1 of w / 2^e,
+ * ties to the even code, above 6 the 6; a value that rounds to zero keeps its
+ * sign.  rows >= 1, cols a multiple of 32; w and q 16-byte aligned.  Offline, like
+ * moe_quant_weight.
+ */
+moe_status_t moe_quant_weight_w4(const float* w, int32_t n_mats, int32_t rows, int32_t cols, uint8_t* q, uint8_t* s,
+                                 hipStream_t stream);
+
+/*
+ * The layout that the products read.  Codes: tiles of 16 rows x 128 columns of
+ * 1024 bytes, tile (g, b) at (g * cols/128 + b) * 1024 of the matrix; its 4 bytes
+ * at 256 kq + 16 r + 4 j hold row 16g + r, columns 128b + 32j + 8kq + [0, 8)
+ * (kq, j in [0, 4), r in [0, 16)), in the order of q: a wave reads a tile as one
+ * contiguous 1 KB load, lane 16 kq + r its operands of four matrix instructions
+ * of 32 columns, one scale group each.  Scales: 256 bytes for 16 rows x 512
+ * columns at (g * ceil(cols/512) + c) * 256, row r's 16 bytes at 16 r; those past
+ * the last column are 127.
+ *
+ * q, s: device, row-major as from moe_quant_weight_w4 or a checkpoint.  packed:
+ * device, n_mats * rows * cols / 2 bytes; packed_s: device,
+ * moe_w4_scale_bytes(n_mats, rows, cols) bytes; neither overlaps q or s.  rows a
+ * multiple of 16, cols of 128; q, packed and packed_s 16-byte, s 4-byte aligned.  A scale byte
+ * above 252 sets MOE_DEV_BAD_SCALE in *dev_status (may be NULL) and products with
+ * its group are unspecified.  Offline, like moe_pack_weight.
+ */
+size_t moe_w4_scale_bytes(int32_t n_mats, int32_t rows, int32_t cols);
+moe_status_t moe_pack_weight_w4(const uint8_t* q, const uint8_t* s, int32_t n_mats, int32_t rows, int32_t cols,
+                                uint8_t* packed, uint8_t* packed_s, int32_t* dev_status, hipStream_t stream);
+
+/*
+ * out[t, n] = sum_k x[t, k] W[n, k] (+ bias[n]), added up in fp32 and rounded
+ * once to out_type.  T >= 0 tokens; K a multiple of 128, N of 16.
+ * x: device bf16, rows x_stride elements apart (a multiple of 8, at least K);
+ * w, w_s: packed as above, one matrix [N, K]; bias: device bf16 [N] or NULL; out:
+ * device bf16 or fp32, rows out_stride elements apart (a multiple of 8, at least
+ * N); rows and columns outside [T, N] are not written.  All pointers 16-byte
+ * aligned (bias 8); out overlaps nothing.  ws: moe_linear_w4_workspace(T, K, N) bytes,
+ * 256-byte aligned; no smaller T needs more.
+ */
+size_t moe_linear_w4_workspace(int32_t T, int32_t K, int32_t N);
+moe_status_t moe_linear_w4(const uint16_t* x_bf16, int64_t x_stride, int32_t T, int32_t K, const uint8_t* w,
+                           const uint8_t* w_s, int32_t N, const uint16_t* bias_bf16, void* out, int64_t out_stride,
+                           moe_float_t out_type, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Expert FFN with 4-bit weights and bf16 activations, any number of tokens, over
+ * the expert-sorted rows (see moe_expert_ffn for their definition):
+ *   h = bf16_rne(G * sigmoid(G) * U), G = x W_gate^T, U = x W_up^T
+ *   y_rows = h W_down^T
+ * sums in fp32.  x_bf16: device [T, H], 16-byte aligned.  Weight stacks [E, I, H],
+ * [E, I, H] and [E, H, I], packed by moe_pack_weight_w4 with n_mats = E.
+ * y_rows: device fp32 [T*k, H].  ws: moe_expert_ffn_w4_workspace(dims, T) bytes,
+ * 256-byte aligned.  Rows with a bad entry of sorted_src get unspecified
+ * values, rows outside expert_offsets none.
+ */
+size_t moe_expert_ffn_w4_workspace(moe_dims_t dims, int32_t T);
+moe_status_t moe_expert_ffn_w4(moe_dims_t dims, int32_t T, const uint16_t* x_bf16, const int32_t* expert_offsets,
+                               const int32_t* sorted_src, const uint8_t* w_gate, const uint8_t* s_gate,
+                               const uint8_t* w_up, const uint8_t* s_up, const uint8_t* w_down, const uint8_t* s_down,
+                               float* y_rows, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * The whole layer with such experts in one call: the sort of moe_permute,
+ * moe_expert_ffn_w4 and the sum of moe_combine.  Arguments as in moe_ffn_layer, weight stacks as
+ * above.  ws: moe_ffn_layer_w4_workspace(dims, T) bytes, 256-byte aligned.
+ */
+size_t moe_ffn_layer_w4_workspace(moe_dims_t dims, int32_t T);
+moe_status_t moe_ffn_layer_w4(moe_dims_t dims, int32_t T, const uint16_t* x_bf16, const int32_t* topk_ids,
+                              const float* topk_w, const uint8_t* w_gate, const uint8_t* s_gate, const uint8_t* w_up,
+                              const uint8_t* s_up, const uint8_t* w_down, const uint8_t* s_down, uint16_t* out_bf16,
+                              int32_t* dev_status, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
  * Diagnostics: per-launch kernel timing.  After moe_profile_begin(n), every

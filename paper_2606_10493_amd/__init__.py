@@ -1,4 +1,4 @@
-"""MI355X (gfx950) routed-expert FP8 MoE FFN, and the attention half of its decoder layer.
+"""MI355X (gfx950) routed-expert FP8 MoE FFN, the attention half of its decoder layer, and products with 4-bit weights.
 
 Thin Python binding of libmoe.so (the C ABI in include/moe.h).  Functions
 carry the C names and only marshal arguments: every step of the layer runs
@@ -18,7 +18,7 @@ from ._lib import (  # noqa: F401
     MoeRouterCfg, MoeStreamOp, MOE_SOP_WAIT_OFF, MOE_SOP_COPY, MOE_SOP_RECORD_ON, MOE_SOP_WAIT_ON, MOE_SOP_LAUNCH,
     MOE_SOP_RECORD_OFF, MoeAttnDims, MoeKvCache, MoeRopeCfg, MOE_DEV_BAD_POSITION, MOE_DEV_BAD_SLOT,
     MOE_DEV_BAD_PAGE, MOE_DEV_BAD_LENGTH, MOE_ROPE_HALF, MOE_ROPE_INTERLEAVED, MOE_ROPE_PLAIN, MOE_ROPE_LINEAR,
-    MOE_ROPE_BY_PARTS,
+    MOE_ROPE_BY_PARTS, MOE_DEV_BAD_SCALE, MOE_BF16, MOE_F32, MOE_W4_GROUP, MoeNormCfg,
     EXPORTED_SYMBOLS,
 )
 from ._lib import check as _check
@@ -289,4 +289,7 @@ def moe_profile_end():
 from .attention import (  # noqa: E402,F401
     AttentionBuffers, KVCache, moe_attn_decode, moe_attn_decode_workspace, moe_attn_prefill,
     moe_attn_prefill_workspace, moe_cache_read, moe_rope, moe_rope_cache, moe_rope_table, run_attention)
+from .w4 import (  # noqa: E402,F401
+    moe_add_norm, moe_expert_ffn_w4, moe_expert_ffn_w4_workspace, moe_ffn_layer_w4, moe_ffn_layer_w4_workspace,
+    moe_linear_w4, moe_linear_w4_workspace, moe_pack_weight_w4, moe_quant_weight_w4, moe_w4_scale_bytes)
 from .layer import MoELayerBuffers, run_layer  # noqa: E402,F401

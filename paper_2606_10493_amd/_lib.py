@@ -25,6 +25,12 @@ MOE_DEV_BAD_POSITION = 4
 MOE_DEV_BAD_SLOT = 8
 MOE_DEV_BAD_PAGE = 16
 MOE_DEV_BAD_LENGTH = 32
+MOE_DEV_BAD_SCALE = 64
+
+MOE_BF16 = 0
+MOE_F32 = 1
+
+MOE_W4_GROUP = 32
 
 MOE_ROPE_HALF = 0
 MOE_ROPE_INTERLEAVED = 1
@@ -68,6 +74,11 @@ class MoeRopeCfg(ctypes.Structure):
     _fields_ = [("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
                 ("factor", ctypes.c_double), ("original_len", ctypes.c_double), ("slow_turns", ctypes.c_double),
                 ("fast_turns", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class MoeNormCfg(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float), ("weight_offset", ctypes.c_float), ("heads", ctypes.c_int32),
+                ("x_type", ctypes.c_int32), ("stream_type", ctypes.c_int32)]
 
 
 class MoEError(RuntimeError):
@@ -132,6 +143,16 @@ _SIGS = {
                                _P]),
     "moe_attn_decode_workspace": (_S, [MoeAttnDims, _I, _I, _I]),
     "moe_attn_decode": (_ST, [MoeAttnDims, _I, _P, _L, MoeKvCache, _P, _I, _P, _I, _P, _I, _F, _P, _P, _P, _S, _P]),
+    "moe_add_norm": (_ST, [_P, _L, _P, _L, _P, _I, _I, MoeNormCfg, _P, _L, _P, _L, _P, _P, _P]),
+    "moe_quant_weight_w4": (_ST, [_P, _I, _I, _I, _P, _P, _P]),
+    "moe_w4_scale_bytes": (_S, [_I, _I, _I]),
+    "moe_pack_weight_w4": (_ST, [_P, _P, _I, _I, _I, _P, _P, _P, _P]),
+    "moe_linear_w4_workspace": (_S, [_I, _I, _I]),
+    "moe_linear_w4": (_ST, [_P, _L, _I, _I, _P, _P, _I, _P, _P, _L, _ST, _P, _S, _P]),
+    "moe_expert_ffn_w4_workspace": (_S, [MoeDims, _I]),
+    "moe_expert_ffn_w4": (_ST, [MoeDims, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _S, _P]),
+    "moe_ffn_layer_w4_workspace": (_S, [MoeDims, _I]),
+    "moe_ffn_layer_w4": (_ST, [MoeDims, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _S, _P]),
     "moe_profile_begin": (_ST, [_I]),
     "moe_profile_end": (_I, []),
     "moe_profile_get": (_ST, [_I, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_char_p)]),

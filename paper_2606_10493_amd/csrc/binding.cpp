@@ -1,9 +1,9 @@
-// The attention calls' Python binding: checks of the tensors and the call of the
-// C ABI in one native function each.  A decode step makes these calls for every
+// The Python binding of the attention calls, the norm and the calls with 4-bit
+// weights: checks of the tensors and the call of the C ABI in one native function each.  A decode step makes these calls for every
 // layer and is bound by the host: moe_rope_cache takes 3 us of it here, most of
 // them the launch, and 9 with the same checks in Python and ctypes.
 //
-// Every function takes what its namesake in attention.py passes, in order, and
+// Every function takes what its namesake in attention.py or w4.py passes, in order, and
 // returns the status of the C call; the stream is always the last.  Tensors are read
 // through torch's C++ objects; nothing of a call is kept.
 #include <c10/hip/HIPStream.h>
@@ -117,9 +117,13 @@ T* matrix(PyObject* o, const char* name, int64_t& rows, int64_t& cols) {
   return p;
 }
 
-void bf16_rows(const at::Tensor& t, int64_t heads, int64_t dim, const char* name) {
+bool is_bf16(const at::Tensor& t) {
   const at::ScalarType type = t.scalar_type();
-  if (type != at::kBFloat16 && type != at::kShort && type != at::kUInt16) bad_value("%s must be bf16 or its bits", name);
+  return type == at::kBFloat16 || type == at::kShort || type == at::kUInt16;
+}
+
+void bf16_rows(const at::Tensor& t, int64_t heads, int64_t dim, const char* name) {
+  if (!is_bf16(t)) bad_value("%s must be bf16 or its bits", name);
   if (t.dim() != 3 || t.size(1) != heads || t.size(2) != dim) {
     PyErr_Format(PyExc_ValueError, "%s must be [tokens, %lld, %lld]", name, (long long)heads, (long long)dim);
     throw Bad{};
@@ -318,6 +322,154 @@ moe_status_t attn_decode(PyObject* const* a) {
                          stream());
 }
 
+// bf16 or fp32 rows [tokens, width] or [tokens, heads, width], a token's values contiguous.
+struct Matrix {
+  void* p = nullptr;
+  int64_t tokens = 0, heads = 1, width = 0, stride = 0;
+  int32_t type = MOE_BF16;
+  Matrix(PyObject* o, bool has_heads, const char* name) {
+    const at::Tensor& t = tensor(o, name);
+    if (is_bf16(t)) type = MOE_BF16;
+    else if (t.scalar_type() == at::kFloat) type = MOE_F32;
+    else bad_value("%s must be bf16, its bits or fp32", name);
+    if (t.dim() != 2 && !(has_heads && t.dim() == 3))
+      bad_value(has_heads ? "%s must be [tokens, width] or [tokens, heads, width]" : "%s must be [tokens, width]", name);
+    p = t.data_ptr();
+    tokens = t.size(0);
+    if (t.dim() == 3) heads = t.size(1);
+    width = t.size(t.dim() - 1);
+    stride = heads * width;  // that of a single token is arbitrary
+    if (tokens == 0 || stride == 0) return;
+    if ((t.stride(t.dim() - 1) != 1 && width != 1) || (t.dim() == 3 && heads != 1 && t.stride(1) != width))
+      bad_value("%s: a token's values must be contiguous", name);
+    if (tokens > 1) stride = t.stride(0);
+  }
+  Matrix() = default;
+  void like(const Matrix& o, const char* name) const {
+    if (tokens != o.tokens || heads != o.heads || width != o.width) bad_value("%s has another shape than x", name);
+  }
+};
+
+const uint16_t* bf16_vector(PyObject* o, int64_t count, const char* name) {
+  int64_t n;
+  const uint16_t* p = address<uint16_t>(o, name, &n);
+  if (o == Py_None) return nullptr;
+  if (!is_bf16(THPVariable_Unpack(o))) bad_value("%s must be bf16 or its bits", name);
+  same(n, count, name);
+  return p;
+}
+
+// x, weight, out, q, s, residual, sum_out, eps, weight_offset, stream
+moe_status_t add_norm(PyObject* const* a) {
+  const Matrix x(a[0], true, "x");
+  Matrix out, residual, sum;
+  moe_norm_cfg_t cfg{real(a[7]), real(a[8]), to_int32(x.heads, "x"), x.type, MOE_BF16};
+  if (a[2] != Py_None) {
+    out = Matrix(a[2], true, "out");
+    out.like(x, "out");
+    if (out.type != MOE_BF16) bad_value("%s must be bf16 or its bits", "out");
+  }
+  if (a[5] != Py_None) {
+    residual = Matrix(a[5], true, "residual");
+    residual.like(x, "residual");
+    cfg.stream_type = residual.type;
+  }
+  if (a[6] != Py_None) {
+    sum = Matrix(a[6], true, "sum_out");
+    sum.like(x, "sum_out");
+    if (residual.p && sum.type != residual.type) bad_value("%s must have the residual's type", "sum_out");
+    cfg.stream_type = sum.type;
+  }
+  const uint16_t* weight = bf16_vector(a[1], x.width, "weight");
+  int64_t n_q, n_s;
+  uint8_t* q = address<uint8_t>(a[3], "q", &n_q);
+  float* s = address<float>(a[4], "s", &n_s);
+  const int64_t n = x.tokens * x.heads * x.width;
+  if (a[3] != Py_None) same(n_q, n, "q");
+  if (a[4] != Py_None) same(n_s, x.tokens * x.heads * (x.width / MOE_BLOCK), "s");
+  return moe_add_norm(x.p, x.stride, residual.p, residual.stride, weight, to_int32(x.tokens, "x"), to_int32(x.width, "x"), cfg,
+                      sum.p, sum.stride, static_cast<uint16_t*>(out.p), out.stride, q, s, stream());
+}
+
+// Packed codes and scales of n_mats matrices [rows, cols].
+struct Packed {
+  const uint8_t *w, *s;
+  Packed(PyObject* codes, PyObject* scales, int64_t n_mats, int64_t rows, int64_t cols, const char* name, const char* s_name) {
+    int64_t n_w, n_s;
+    w = address<uint8_t>(codes, name, &n_w);
+    s = address<uint8_t>(scales, s_name, &n_s);
+    // shapes that are no matrix of 4-bit weights are passed on, for the call to refuse
+    if (n_mats <= 0 || rows <= 0 || cols <= 0 || rows % 16 || cols % MOE_BLOCK) return;
+    if (codes != Py_None) same(n_w, n_mats * rows * (cols / 2), name);
+    if (scales != Py_None) same(n_s, (int64_t)moe_w4_scale_bytes((int32_t)n_mats, (int32_t)rows, (int32_t)cols), s_name);
+  }
+};
+
+// x, w, w_s, out, bias, ws, stream
+moe_status_t linear_w4(PyObject* const* a) {
+  const Matrix x(a[0], false, "x"), out(a[3], false, "out");
+  if (x.type != MOE_BF16) bad_value("%s must be bf16 or its bits", "x");
+  same(out.tokens, x.tokens, "out");
+  const int32_t T = to_int32(x.tokens, "x"), K = to_int32(x.width, "x"), N = to_int32(out.width, "out");
+  const Packed w(a[1], a[2], 1, N, K, "w", "w_s");
+  int64_t ws_bytes;
+  uint8_t* ws = address<uint8_t>(a[5], "ws", &ws_bytes);
+  return moe_linear_w4(static_cast<const uint16_t*>(x.p), x.stride, T, K, w.w, w.s, N, bf16_vector(a[4], out.width, "bias"),
+                       out.p, out.stride, (moe_float_t)out.type, ws, (size_t)ws_bytes, stream());
+}
+
+// Contiguous rows of the layer calls.
+void* full_rows(PyObject* o, int64_t rows, int64_t width, int32_t type, const char* name) {
+  const Matrix m(o, false, name);
+  if (m.type != type) bad_value(type == MOE_BF16 ? "%s must be bf16 or its bits" : "%s must be fp32", name);
+  if (m.tokens != rows || m.width != width || m.stride != width) bad_value("%s has another shape, or is not contiguous", name);
+  return m.p;
+}
+
+struct Experts {
+  Packed gate, up, down;
+  Experts(const moe_dims_t& d, PyObject* const* a)
+      : gate(a[0], a[1], d.n_experts, d.inter, d.hidden, "w_gate", "s_gate"),
+        up(a[2], a[3], d.n_experts, d.inter, d.hidden, "w_up", "s_up"),
+        down(a[4], a[5], d.n_experts, d.hidden, d.inter, "w_down", "s_down") {}
+};
+
+// dims, T, x, expert_offsets, sorted_src, six weights, y_rows, ws, stream
+moe_status_t expert_ffn_w4(PyObject* const* a) {
+  const auto d = structure<moe_dims_t>(a[0], "dims");
+  const int32_t T = integer32(a[1], "T");
+  const int64_t rows = (int64_t)T * d.topk;
+  const Experts w(d, a + 5);
+  int64_t n_off, n_src, ws_bytes;
+  const int32_t* offsets = address<int32_t>(a[3], "expert_offsets", &n_off);
+  const int32_t* src = address<int32_t>(a[4], "sorted_src", &n_src);
+  same(n_off, (int64_t)d.n_experts + 1, "expert_offsets");
+  same(n_src, rows, "sorted_src");
+  uint8_t* ws = address<uint8_t>(a[12], "ws", &ws_bytes);
+  return moe_expert_ffn_w4(d, T, static_cast<const uint16_t*>(full_rows(a[2], T, d.hidden, MOE_BF16, "x")), offsets, src,
+                           w.gate.w, w.gate.s, w.up.w, w.up.s, w.down.w, w.down.s,
+                           static_cast<float*>(full_rows(a[11], rows, d.hidden, MOE_F32, "y_rows")), ws, (size_t)ws_bytes,
+                           stream());
+}
+
+// dims, T, x, topk_ids, topk_w, six weights, out, dev_status, ws, stream
+moe_status_t ffn_layer_w4(PyObject* const* a) {
+  const auto d = structure<moe_dims_t>(a[0], "dims");
+  const int32_t T = integer32(a[1], "T");
+  const int64_t rows = (int64_t)T * d.topk;
+  const Experts w(d, a + 5);
+  int64_t n_ids, n_p, ws_bytes;
+  const int32_t* ids = address<int32_t>(a[3], "topk_ids", &n_ids);
+  const float* p = address<float>(a[4], "topk_w", &n_p);
+  same(n_ids, rows, "topk_ids");
+  same(n_p, rows, "topk_w");
+  uint8_t* ws = address<uint8_t>(a[13], "ws", &ws_bytes);
+  return moe_ffn_layer_w4(d, T, static_cast<const uint16_t*>(full_rows(a[2], T, d.hidden, MOE_BF16, "x")), ids, p, w.gate.w,
+                          w.gate.s, w.up.w, w.up.s, w.down.w, w.down.s,
+                          static_cast<uint16_t*>(full_rows(a[11], T, d.hidden, MOE_BF16, "out")), status_of(a[12]), ws,
+                          (size_t)ws_bytes, stream());
+}
+
 template <moe_status_t (*kCall)(PyObject* const*), int kArgs>
 constexpr PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<kCall, kArgs>)), METH_FASTCALL, nullptr};
@@ -328,9 +480,13 @@ PyMethodDef kMethods[] = {method<rope, 10>("rope"),
                           method<cache_read, 8>("cache_read"),
                           method<attn_prefill, 13>("attn_prefill"),
                           method<attn_decode, 13>("attn_decode"),
+                          method<add_norm, 10>("add_norm"),
+                          method<linear_w4, 7>("linear_w4"),
+                          method<expert_ffn_w4, 14>("expert_ffn_w4"),
+                          method<ffn_layer_w4, 15>("ffn_layer_w4"),
                           {nullptr, nullptr, 0, nullptr}};
 
-PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", "The attention calls of libmoe.so on torch tensors.", -1, kMethods};
+PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", "The attention calls, the norm and the calls with 4-bit weights of libmoe.so on torch tensors.", -1, kMethods};
 
 }  // namespace
 

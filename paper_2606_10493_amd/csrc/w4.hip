@@ -1,0 +1,175 @@
+// The calls with 4-bit weights: checks, workspaces, and which kernel runs.
+#include "w4.h"
+
+namespace moe {
+
+moe_status_t run_w4_gemv(const W4Args& a, bool gateup, int32_t T, int64_t rows, hipStream_t stream);
+moe_status_t run_w4_gemm(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
+
+namespace {
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+moe_status_t run_w4(const W4Args& a, bool gateup, int32_t T, int64_t rows, hipStream_t stream) {
+  if (T <= MOE_DECODE_MAX_TOKENS) return run_w4_gemv(a, gateup, T, rows, stream);
+  return run_w4_gemm(a, gateup, rows, stream);
+}
+
+moe_status_t check_w4_dims(const moe_dims_t& d, int32_t T, const char* who) {
+  if (d.hidden <= 0 || d.inter <= 0 || d.n_experts < 1 || d.n_experts > 1024 || d.topk < 1 || d.topk > 32 ||
+      d.topk > d.n_experts || T < 0)
+    return fail(MOE_ERR_INVALID_ARG, "%s: dims H=%d I=%d E=%d k=%d, T=%d", who, d.hidden, d.inter, d.n_experts, d.topk, T);
+  if (d.hidden % kBlock || d.inter % kBlock)
+    return fail(MOE_ERR_UNSUPPORTED_SHAPE, "%s: H=%d, I=%d must be multiples of 128", who, d.hidden, d.inter);
+  if ((int64_t)T * d.topk > 0x7fffffff) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "%s: T*k overflows", who);
+  return MOE_OK;
+}
+
+moe_status_t check_w4_stacks(const void* x, const uint8_t* const (&w)[6], const void* out, const char* who) {
+  for (const uint8_t* m : w)
+    if (!m) return fail(MOE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (!x || !out) return fail(MOE_ERR_INVALID_ARG, "%s: null pointer", who);
+  for (const uint8_t* m : w)
+    if (!aligned(m, 16)) return fail(MOE_ERR_INVALID_ARG, "%s: misaligned weights (16 bytes needed)", who);
+  if (!aligned(x, 16) || !aligned(out, 16)) return fail(MOE_ERR_INVALID_ARG, "%s: misaligned pointer (16 bytes needed)", who);
+  return MOE_OK;
+}
+
+moe_status_t check_workspace(const void* ws, size_t have, size_t need, const char* who) {
+  if (need && (!ws || have < need)) return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu", who, have, need);
+  if (!aligned(ws, 256)) return fail(MOE_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
+  return MOE_OK;
+}
+
+moe_status_t expert_ffn_w4(const moe_dims_t& d, int32_t T, const uint16_t* x, const int32_t* offsets, const int32_t* src,
+                           const uint8_t* const (&w)[6], uint16_t* h, float* y, hipStream_t stream) {
+  const int64_t rows = (int64_t)T * d.topk;
+  W4Args g{};
+  g.x = x; g.x_stride = d.hidden; g.x_rows = T; g.sorted_src = src; g.topk = d.topk;
+  g.offsets = offsets; g.E = d.n_experts;
+  g.w0 = w[0]; g.s0 = w[1]; g.w1 = w[2]; g.s1 = w[3];
+  g.N = d.inter; g.K = d.hidden; g.out16 = h; g.out_stride = d.inter;
+  const moe_status_t st = run_w4(g, true, T, rows, stream);
+  if (st != MOE_OK) return st;
+  W4Args dn{};
+  dn.x = h; dn.x_stride = d.inter; dn.x_rows = rows;
+  dn.offsets = offsets; dn.E = d.n_experts;
+  dn.w0 = w[4]; dn.s0 = w[5];
+  dn.N = d.hidden; dn.K = d.inter; dn.out32 = y; dn.out_stride = d.hidden;
+  return run_w4(dn, false, T, rows, stream);
+}
+
+struct W4LayerLayout {
+  size_t offsets, src, dest, y, perm, h, total;
+};
+
+W4LayerLayout w4_layer_layout(const moe_dims_t& d, int32_t T) {
+  W4LayerLayout L{};
+  const size_t R = (size_t)T * d.topk;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += align256(bytes);
+    return here;
+  };
+  L.offsets = take((size_t)(d.n_experts + 1) * sizeof(int32_t));
+  L.src = take(R * sizeof(int32_t));
+  L.dest = take(R * sizeof(int32_t));
+  L.y = take(R * d.hidden * sizeof(float));
+  L.perm = take(moe_permute_workspace(T, d.topk, d.n_experts));
+  L.h = take(moe_expert_ffn_w4_workspace(d, T));
+  L.total = at;
+  return L;
+}
+
+}  // namespace
+
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" size_t moe_linear_w4_workspace(int32_t T, int32_t K, int32_t N) {
+  (void)T;
+  (void)K;
+  (void)N;
+  return 0;
+}
+
+extern "C" moe_status_t moe_linear_w4(const uint16_t* x, int64_t x_stride, int32_t T, int32_t K, const uint8_t* w,
+                                      const uint8_t* w_s, int32_t N, const uint16_t* bias, void* out, int64_t out_stride,
+                                      moe_float_t out_type, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (T < 0 || K <= 0 || N <= 0) return fail(MOE_ERR_INVALID_ARG, "moe_linear_w4: T=%d K=%d N=%d", T, K, N);
+  if (out_type != MOE_BF16 && out_type != MOE_F32) return fail(MOE_ERR_INVALID_ARG, "moe_linear_w4: out_type=%d", (int)out_type);
+  if (K % kBlock || N % 16)
+    return fail(MOE_ERR_UNSUPPORTED_SHAPE, "moe_linear_w4: K=%d (a multiple of 128), N=%d (of 16)", K, N);
+  if (T == 0) return MOE_OK;
+  if (!x || !w || !w_s || !out) return fail(MOE_ERR_INVALID_ARG, "moe_linear_w4: null pointer");
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(w_s, 16) || !aligned(out, 16) || !aligned(bias, 8))
+    return fail(MOE_ERR_INVALID_ARG, "moe_linear_w4: misaligned pointer");
+  if (x_stride < K || x_stride % 8 || out_stride < N || out_stride % 8)
+    return fail(MOE_ERR_INVALID_ARG, "moe_linear_w4: strides %lld of x, %lld of out must be multiples of 8, at least %d and %d",
+                (long long)x_stride, (long long)out_stride, K, N);
+  const moe_status_t st = check_workspace(ws, ws_bytes, moe_linear_w4_workspace(T, K, N), "moe_linear_w4");
+  if (st != MOE_OK) return st;
+  W4Args a{};
+  a.x = x; a.x_stride = x_stride; a.x_rows = T;
+  a.w0 = w; a.s0 = w_s; a.bias = bias; a.N = N; a.K = K;
+  a.out32 = out_type == MOE_F32 ? static_cast<float*>(out) : nullptr;
+  a.out16 = out_type == MOE_F32 ? nullptr : static_cast<uint16_t*>(out);
+  a.out_stride = out_stride;
+  return run_w4(a, false, T, T, stream);
+}
+
+extern "C" size_t moe_expert_ffn_w4_workspace(moe_dims_t d, int32_t T) {
+  if (T < 0 || d.inter <= 0 || d.topk <= 0) return 0;
+  return align256((size_t)T * d.topk * d.inter * sizeof(uint16_t));
+}
+
+extern "C" moe_status_t moe_expert_ffn_w4(moe_dims_t d, int32_t T, const uint16_t* x, const int32_t* expert_offsets,
+                                          const int32_t* sorted_src, const uint8_t* w_gate, const uint8_t* s_gate,
+                                          const uint8_t* w_up, const uint8_t* s_up, const uint8_t* w_down,
+                                          const uint8_t* s_down, float* y_rows, void* ws, size_t ws_bytes,
+                                          hipStream_t stream) {
+  moe_status_t st = check_w4_dims(d, T, "moe_expert_ffn_w4");
+  if (st != MOE_OK) return st;
+  if (T == 0) return MOE_OK;
+  const uint8_t* const w[6] = {w_gate, s_gate, w_up, s_up, w_down, s_down};
+  st = check_w4_stacks(x, w, y_rows, "moe_expert_ffn_w4");
+  if (st != MOE_OK) return st;
+  if (!expert_offsets || !sorted_src) return fail(MOE_ERR_INVALID_ARG, "moe_expert_ffn_w4: null pointer");
+  st = check_workspace(ws, ws_bytes, moe_expert_ffn_w4_workspace(d, T), "moe_expert_ffn_w4");
+  if (st != MOE_OK) return st;
+  return expert_ffn_w4(d, T, x, expert_offsets, sorted_src, w, static_cast<uint16_t*>(ws), y_rows, stream);
+}
+
+extern "C" size_t moe_ffn_layer_w4_workspace(moe_dims_t d, int32_t T) {
+  if (check_w4_dims(d, T, "moe_ffn_layer_w4_workspace") != MOE_OK) return 0;
+  return w4_layer_layout(d, T).total;
+}
+
+extern "C" moe_status_t moe_ffn_layer_w4(moe_dims_t d, int32_t T, const uint16_t* x, const int32_t* topk_ids,
+                                         const float* topk_w, const uint8_t* w_gate, const uint8_t* s_gate,
+                                         const uint8_t* w_up, const uint8_t* s_up, const uint8_t* w_down,
+                                         const uint8_t* s_down, uint16_t* out, int32_t* dev_status, void* ws,
+                                         size_t ws_bytes, hipStream_t stream) {
+  moe_status_t st = check_w4_dims(d, T, "moe_ffn_layer_w4");
+  if (st != MOE_OK) return st;
+  if (T == 0) return MOE_OK;
+  const uint8_t* const w[6] = {w_gate, s_gate, w_up, s_up, w_down, s_down};
+  st = check_w4_stacks(x, w, out, "moe_ffn_layer_w4");
+  if (st != MOE_OK) return st;
+  if (!topk_ids || !topk_w) return fail(MOE_ERR_INVALID_ARG, "moe_ffn_layer_w4: null pointer");
+  const W4LayerLayout L = w4_layer_layout(d, T);
+  st = check_workspace(ws, ws_bytes, L.total, "moe_ffn_layer_w4");
+  if (st != MOE_OK) return st;
+  uint8_t* b = static_cast<uint8_t*>(ws);
+  int32_t* offsets = reinterpret_cast<int32_t*>(b + L.offsets);
+  int32_t* src = reinterpret_cast<int32_t*>(b + L.src);
+  int32_t* dest = reinterpret_cast<int32_t*>(b + L.dest);
+  float* y = reinterpret_cast<float*>(b + L.y);
+  st = moe_permute(topk_ids, T, d.topk, d.n_experts, offsets, src, dest, dev_status, b + L.perm, L.h - L.perm, stream);
+  if (st != MOE_OK) return st;
+  st = expert_ffn_w4(d, T, x, offsets, src, w, reinterpret_cast<uint16_t*>(b + L.h), y, stream);
+  if (st != MOE_OK) return st;
+  return moe_combine(y, dest, topk_w, T, d.topk, d.hidden, out, stream);
+}
