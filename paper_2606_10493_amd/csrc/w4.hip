@@ -3,7 +3,9 @@
 
 namespace moe {
 
-moe_status_t run_w4_gemv(const W4Args& a, bool gateup, int32_t T, int64_t rows, hipStream_t stream);
+moe_status_t run_w4_gemv(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
+bool w4_few_fits(int32_t K);
+moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
 moe_status_t run_w4_gemm(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
 
 namespace {
@@ -11,7 +13,8 @@ namespace {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 moe_status_t run_w4(const W4Args& a, bool gateup, int32_t T, int64_t rows, hipStream_t stream) {
-  if (T <= MOE_DECODE_MAX_TOKENS) return run_w4_gemv(a, gateup, T, rows, stream);
+  if (T <= MOE_DECODE_MAX_TOKENS && (a.offsets || T <= 16) && w4_few_fits(a.K)) return run_w4_few(a, gateup, rows, stream);
+  if (T <= MOE_DECODE_MAX_TOKENS) return run_w4_gemv(a, gateup, rows, stream);
   return run_w4_gemm(a, gateup, rows, stream);
 }
 

@@ -1,0 +1,227 @@
+// Products of up to 16 rows a matrix with 4-bit weights: every weight is read once
+// and the kernel is bound by that stream.
+//
+// An item is R tiles of 16 weight rows (with GATEUP half of them W_gate's and half
+// the same rows of W_up) against a tile of up to 16 activation rows.  A workgroup
+// takes a run of neighbouring items, so neighbouring weights and mostly the same
+// activations: wave w keeps the activations' K blocks of 128 from NBW w to
+// NBW w + NBW - 1 in registers from one item to the next and streams those blocks
+// of the weights; the waves' sums are added through LDS in wave order.  So the loop
+// over items loads weights and scales alone.  D items are in flight: a register is
+// loaded again, for the item D further on, as soon as it has been used.
+//
+// The matrix instruction is 16x16x32 bf16 with the weights as its first operand:
+// 32 columns are one scale group, expanded to bf16 with the scale in it, and a
+// result register holds four neighbouring outputs of one activation row.
+#include <algorithm>
+
+#include "w4.h"
+#include "w4_rows.h"
+
+namespace moe {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Waves of a workgroup (a CU's), so that NBW blocks of activations fit their registers.
+constexpr int few_waves(int nbw) { return nbw <= 2 ? 16 : 12; }
+constexpr int kFewMaxBlocks = 60;  // 12 waves of 5
+
+template <int NBW, int R, int D, bool GATEUP>
+__global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_few_kernel(W4Args p, int64_t rows) {
+  constexpr int kTiles = GATEUP ? R / 2 : R;  // tiles of outputs
+  extern __shared__ __attribute__((aligned(16))) uint8_t red_bytes[];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = blockDim.x >> 6;
+  v4f* red = reinterpret_cast<v4f*>(red_bytes);  // [2][waves][R][64]
+  const int r = lane & 15, kq = lane >> 4;
+  const int nb = p.K / kBlock;
+  const int groups = p.N / 16;
+  const int items_n = (groups + kTiles - 1) / kTiles;
+  const int kb0 = wave * NBW;
+  const int64_t chunks = (nb + 3) / 4;
+
+  const int64_t m_tiles = p.offsets ? all_tiles(p.offsets, p.E, 16, (int)rows) : (rows + 15) / 16;
+  const int64_t items = m_tiles * items_n;
+  const int64_t first = items * blockIdx.x / gridDim.x, end = items * (blockIdx.x + 1) / gridDim.x;
+  if (first >= end) return;
+
+  struct Tile {
+    int64_t a, p0;
+    int e, m;
+  };
+  auto find = [&](int64_t a) {
+    if (!p.offsets) return Tile{a, a * 16, 0, (int)min((int64_t)16, rows - a * 16)};
+    const ExpertRows t = find_row_tile(p.offsets, p.E, (int)a, 16, (int)rows);
+    return Tile{a, t.p0, t.e, t.m};
+  };
+
+  // What is loaded next: item lg of row tile lk.
+  Tile lk = find(first / items_n);
+  int lg = (int)(first - lk.a * items_n);
+  int64_t left = end - first;  // items that are not loaded yet
+  const uint8_t *w_base[GATEUP ? 2 : 1], *s_base[GATEUP ? 2 : 1];
+  auto point = [&]() {
+    const int64_t g = (int64_t)lk.e * groups;
+    w_base[0] = p.w0 + g * nb * kW4TileBytes;
+    s_base[0] = p.s0 + g * chunks * kW4ScaleTile;
+    if constexpr (GATEUP) {
+      w_base[1] = p.w1 + g * nb * kW4TileBytes;
+      s_base[1] = p.s1 + g * chunks * kW4ScaleTile;
+    }
+  };
+  point();
+  struct Codes {
+    u32x4 w[R][NBW];
+    uint32_t s[R][NBW];
+  };
+  auto load = [&](Codes& q, int t) {  // tile t of the item
+    const int mat = GATEUP && t >= kTiles ? 1 : 0;
+    const int64_t g = min(lg * kTiles + (GATEUP ? t % kTiles : t), groups - 1);
+    const uint8_t* w = w_base[mat] + g * nb * kW4TileBytes;
+#pragma unroll
+    for (int u = 0; u < NBW; ++u)  // blocks past the last are that one again, against zeros
+      q.w[t][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(w + min(kb0 + u, nb - 1) * kW4TileBytes + lane * 16));
+    const uint8_t* s = s_base[mat] + g * chunks * kW4ScaleTile + r * 16;
+    if constexpr (NBW == 5) {
+#pragma unroll
+      for (int u = 0; u < NBW; ++u) {
+        const int b = min(kb0 + u, nb - 1);
+        q.s[t][u] = *reinterpret_cast<const uint32_t*>(s + (b >> 2) * kW4ScaleTile + (b & 3) * 4);
+      }
+      return;
+    }
+    s += (kb0 >> 2) * kW4ScaleTile + (kb0 & 3) * 4;
+    if constexpr (NBW == 4) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(s);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) q.s[t][u] = v[u];
+    } else if constexpr (NBW == 2) {
+      const u32x2 v = *reinterpret_cast<const u32x2*>(s);
+      q.s[t][0] = v[0];
+      q.s[t][1] = v[1];
+    } else {
+      q.s[t][0] = *reinterpret_cast<const uint32_t*>(s);
+    }
+  };
+  auto next_item = [&]() {
+    if (--left <= 0) return;  // the last item is loaded again, and not used
+    if (++lg < items_n) return;
+    lg = 0;
+    lk = find(lk.a + 1);
+    point();
+  };
+
+  Codes q[D];
+  Tile ck = lk;
+  int cg = lg;
+  w4_bf16x8 x[NBW][4];
+  auto load_x = [&]() {
+    // Rows past the tile's last read that one again: what a lane has for an activation row reaches that row's sums
+    // alone, which are not stored.
+    int64_t row = ck.p0 + min(r, ck.m - 1);
+    if (p.sorted_src) {
+      row = p.sorted_src[row] / p.topk;
+      if (row < 0 || row >= p.x_rows) row = 0;
+    }
+    const uint16_t* xr = p.x + row * p.x_stride + 8 * kq;
+#pragma unroll
+    for (int u = 0; u < NBW; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint4 v = *reinterpret_cast<const uint4*>(xr + min(kb0 + u, nb - 1) * kBlock + 32 * j);
+        x[u][j] = __builtin_bit_cast(w4_bf16x8, kb0 + u < nb ? v : make_uint4(0, 0, 0, 0));
+      }
+  };
+#pragma unroll
+  for (int d = 0; d < D; ++d) {
+#pragma unroll
+    for (int t = 0; t < R; ++t) load(q[d], t);
+    next_item();
+  }
+  load_x();
+
+  int parity = 0;
+  int64_t todo = end - first;
+  auto item = [&](Codes& c) {
+    v4f* mine = red + (int64_t)parity * waves * R * 64;
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      v4f acc = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < NBW; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w4_expand(c.w[t][u][j], w4_scale(c.s[t][u], j)), x[u][j], acc, 0, 0, 0);
+      load(c, t);
+      mine[(wave * R + t) * 64 + lane] = acc;
+    }
+    next_item();
+    // A plain barrier: loads stay in flight across it.
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // The waves' sums, in wave order.  Other waves finish the next item's, and all go on meanwhile.
+    for (int t = (wave + waves - cg * kTiles % waves) % waves; t < kTiles; t += waves) {
+      v4f v = mine[t * 64 + lane];
+      for (int w = 1; w < waves; ++w) v += mine[(w * R + t) * 64 + lane];
+      if (GATEUP) {
+        v4f u = mine[(kTiles + t) * 64 + lane];
+        for (int w = 1; w < waves; ++w) u += mine[(w * R + kTiles + t) * 64 + lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = silu_mul(v[i], u[i]);
+      }
+      if (r < ck.m && cg * kTiles + t < groups) w4_store(p, ck.p0 + r, (cg * kTiles + t) * 16 + 4 * kq, v);
+    }
+    parity ^= 1;
+    --todo;
+    if (++cg == items_n && todo > 0) {
+      cg = 0;
+      ck = find(ck.a + 1);
+      load_x();
+    }
+  };
+  static_assert(D == 1 || D == 2 || D == 4, "the loop below is written out");
+  while (true) {
+    item(q[0]);
+    if (todo == 0) return;
+    if constexpr (D > 1) {
+      item(q[1]);
+      if (todo == 0) return;
+    }
+    if constexpr (D > 2) {
+      item(q[2]);
+      if (todo == 0) return;
+      item(q[3]);
+      if (todo == 0) return;
+    }
+  }
+}
+
+template <int NBW, int R, int D, bool GATEUP>
+moe_status_t launch_few(const W4Args& a, int64_t rows, hipStream_t stream) {
+  const char* name = GATEUP ? "w4_few_gateup" : "w4_few";
+  const int waves = (a.K / kBlock + NBW - 1) / NBW;
+  const int tiles = GATEUP ? R / 2 : R;
+  const int64_t items_n = (a.N / 16 + tiles - 1) / tiles;
+  // Row tiles of experts: each may leave its last one unfilled.
+  const int64_t m_tiles = a.offsets ? rows / 16 + (rows < a.E ? rows : (int64_t)a.E) : (rows + 15) / 16;
+  const int64_t blocks = std::min<int64_t>(items_n * m_tiles, 256 * (few_waves(NBW) / waves));
+  MOE_LAUNCH(name, (w4_few_kernel<NBW, R, D, GATEUP>), dim3((unsigned)blocks), dim3(64 * waves), 2 * waves * R * 1024, stream, a, rows);
+  return check_launch(name);
+}
+
+}  // namespace
+
+bool w4_few_fits(int32_t K) { return K / kBlock <= kFewMaxBlocks; }
+
+moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
+  const int nb = a.K / kBlock;
+  if (nb <= 8) return gateup ? launch_few<1, 2, 4, true>(a, rows, stream) : launch_few<1, 2, 4, false>(a, rows, stream);
+  if (nb <= 32) return gateup ? launch_few<2, 2, 2, true>(a, rows, stream) : launch_few<2, 2, 2, false>(a, rows, stream);
+  if (nb <= 48) return gateup ? launch_few<4, 2, 1, true>(a, rows, stream) : launch_few<4, 2, 1, false>(a, rows, stream);
+  return gateup ? launch_few<5, 2, 1, true>(a, rows, stream) : launch_few<5, 2, 1, false>(a, rows, stream);
+}
+
+}  // namespace moe

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int6
   int e = 0, mc;
   int64_t p0;
   if (p.offsets) {
-    const ExpertRows ref = find_row_tile(p.offsets, p.E, a, 16 * MT, (int)rows);
+    const ExpertRows ref = find_row_tile(p.offsets, p.E, (int)a, 16 * MT, (int)rows);
     if (ref.e < 0) return;  // the whole workgroup
     e = ref.e;
     p0 = ref.p0;

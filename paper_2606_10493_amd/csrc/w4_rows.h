@@ -10,65 +10,72 @@ struct ExpertRows {
   int e, p0, m;  // expert (-1: there is none), first row, rows
 };
 
-// Lane l's expert c0 + l: its first row and the row behind its last.
-__device__ __forceinline__ void expert_span(const int32_t* __restrict__ offsets, int E, int x, int rows, int& lo, int& hi) {
-  lo = min(max(offsets[min(x, E)], 0), rows);
-  hi = x < E ? min(max(offsets[min(x + 1, E)], lo), rows) : lo;
+// The row tiles of 256 experts, c0 + 64 c + lane being the lane's in part c: their
+// first rows, rows, and in `upto` the tiles of all 256 up to and with it.  The
+// offsets go out together, so that this costs one round trip.
+struct TileCounts {
+  int lo[4], n[4], upto[4], all;
+};
+
+__device__ __forceinline__ TileCounts count_tiles(const int32_t* __restrict__ offsets, int E, int c0, int tile, int rows) {
+  const int lane = threadIdx.x & 63;
+  TileCounts t;
+  int hi[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int x = c0 + 64 * c + lane;
+    t.lo[c] = offsets[min(x, E)];
+    hi[c] = offsets[min(x + 1, E)];
+  }
+  t.all = 0;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    t.lo[c] = min(max(t.lo[c], 0), rows);
+    t.n[c] = c0 + 64 * c + lane < E ? max(min(hi[c], rows) - t.lo[c], 0) : 0;
+    int x = (int)(((int64_t)t.n[c] + tile - 1) / tile);
+    // Inclusive sum over the lanes: neighbours, rows of 16 and halves by register moves.
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);   // row_shr:2
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);   // row_shr:4
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);   // row_shr:8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
+    t.upto[c] = t.all + x;
+    t.all += __builtin_amdgcn_readlane(x, 63);
+  }
+  return t;
 }
 
-// The a-th of the experts that have m_lo to m_hi rows.  The offsets of 256 experts
-// go out together, so that the search costs one round trip.
-__device__ __forceinline__ ExpertRows find_expert(const int32_t* __restrict__ offsets, int E, int a, int m_lo, int m_hi, int rows) {
-  const int lane = threadIdx.x & 63;
-  ExpertRows found{-1, 0, 0};
-  for (int c0 = 0; c0 < E && found.e < 0; c0 += 256) {
-    int lo[4], hi[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) expert_span(offsets, E, c0 + 64 * c + lane, rows, lo[c], hi[c]);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int n = hi[c] - lo[c];
-      unsigned long long on = __ballot(n >= m_lo && n <= m_hi && n > 0);
-      const int count = __popcll(on);
-      if (found.e < 0 && a < count) {
-        for (int i = 0; i < a; ++i) on &= on - 1ull;
-        const int at = __ffsll((long long)on) - 1;
-        found = ExpertRows{c0 + 64 * c + at, __shfl(lo[c], at), __shfl(n, at)};
-      }
-      a -= count;
-    }
-  }
-  return found;
+// All experts' row tiles.
+__device__ __forceinline__ int all_tiles(const int32_t* __restrict__ offsets, int E, int tile, int rows) {
+  int n = 0;
+  for (int c0 = 0; c0 < E; c0 += 256) n += count_tiles(offsets, E, c0, tile, rows).all;
+  return n;
 }
 
 // The a-th tile of `tile` rows over all experts in order (an expert's last tile may
 // hold fewer rows).
-__device__ __forceinline__ ExpertRows find_row_tile(const int32_t* __restrict__ offsets, int E, int64_t a, int tile, int rows) {
-  const int lane = threadIdx.x & 63;
-  ExpertRows found{-1, 0, 0};
-  for (int c0 = 0; c0 < E && found.e < 0; c0 += 256) {
-    int lo[4], hi[4];
+__device__ __forceinline__ ExpertRows find_row_tile(const int32_t* __restrict__ offsets, int E, int a, int tile, int rows) {
+  for (int c0 = 0; c0 < E; c0 += 256) {
+    const TileCounts t = count_tiles(offsets, E, c0, tile, rows);
+    if (a < t.all) {
+      ExpertRows found{-1, 0, 0};
 #pragma unroll
-    for (int c = 0; c < 4; ++c) expert_span(offsets, E, c0 + 64 * c + lane, rows, lo[c], hi[c]);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int own = (int)(((int64_t)hi[c] - lo[c] + tile - 1) / tile);
-      int n = own;  // becomes the tiles of the experts up to this lane's
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(n, d);
-        if (lane >= d) n += y;
+      for (int c = 0; c < 4; ++c) {
+        const unsigned long long holds = __ballot(a < t.upto[c]);
+        if (found.e < 0 && holds) {
+          const int at = __ffsll((long long)holds) - 1;
+          const int n = __builtin_amdgcn_readlane(t.n[c], at);
+          const int back = __builtin_amdgcn_readlane(t.upto[c], at) - a;  // tiles from this one to the expert's last
+          const int skip = (((n + tile - 1) / tile) - back) * tile;
+          found = ExpertRows{c0 + 64 * c + at, __builtin_amdgcn_readlane(t.lo[c], at) + skip, min(tile, n - skip)};
+        }
       }
-      const unsigned long long holds = __ballot(a < n);
-      if (found.e < 0 && holds) {
-        const int at = __ffsll((long long)holds) - 1;
-        const int first = __shfl(lo[c], at) + ((int)a - __shfl(n - own, at)) * tile;
-        found = ExpertRows{c0 + 64 * c + at, first, min(tile, __shfl(hi[c], at) - first)};
-      }
-      a -= __shfl(n, 63);
+      return found;
     }
+    a -= t.all;
   }
-  return found;
+  return ExpertRows{-1, 0, 0};
 }
 
 }  // namespace moe
