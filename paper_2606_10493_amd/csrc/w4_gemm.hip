@@ -1,14 +1,19 @@
 // Products of many rows with 4-bit weights: an LDS-tiled bf16 GEMM that expands
 // the weights in registers on their way from LDS to the matrix instruction.
 //
-// A workgroup of four waves takes 16 MT activation rows against 256 weight rows
-// (GATEUP: 128 of W_gate and the same 128 of W_up), a wave 64 of them (32 and
-// 32) against all activation rows: no weight is expanded twice in a workgroup.
-// Steps of 128 K.  Activations (256 bytes a row), codes (a wave's four 1 KB
-// tiles) and scales (one dword a row) go straight from global memory into three
-// LDS stages, two steps ahead, with one barrier a step; activation rows are
-// gathered on the way.  The 16-byte piece c of an activation row lies at position
-// c ^ row % 16, so that a quarter wave's reads fill all banks.
+// A workgroup takes a tile of up to 32 S activation rows against 256 weight rows
+// (GATEUP: 128 of W_gate and the same 128 of W_up).  Its eight waves, two to a SIMD,
+// are two halves of the activation rows by four quarters of the weight rows: a wave
+// expands 64 weight rows for up to 16 S activation rows, and the expansion of one
+// wave of a SIMD runs beside the products of the other.  How many 16-row parts of
+// activations a half has is known when the tile is, and each number has its own loop,
+// so that an expert's rows are cut into equal tiles whose size follows them.
+//
+// Steps of 128 K.  Activations (256 bytes a row), codes (1 KB a tile of 16 rows) and
+// scales (one dword a row) go straight from global memory into LDS stages, one or
+// two steps ahead, with one barrier a step; activation rows are gathered on the
+// way.  The 16-byte piece c of an activation row lies at position c ^ row % 16, so
+// that a quarter wave's reads fill all banks.
 #include "w4.h"
 #include "w4_rows.h"
 
@@ -16,11 +21,13 @@ namespace moe {
 
 namespace {
 
-constexpr int kGemmWaves = 4;
-constexpr int kGemmTiles = 4;  // 16-row weight tiles of a wave
-constexpr int kGemmStages = 3;
-constexpr int kGemmRows = kGemmWaves * kGemmTiles * 16;  // weight rows of a workgroup
-constexpr int kGemmWaveStage = kGemmTiles * kW4TileBytes + kGemmTiles * 64;  // codes, then scales
+constexpr int kGemmWaves = 8;
+constexpr int kGemmTiles = 4;                          // 16-row weight tiles of a wave
+constexpr int kGemmRows = 4 * kGemmTiles * 16;         // weight rows of a workgroup
+constexpr int kGemmCodes = kGemmRows / 16 * kW4TileBytes;  // of a stage
+constexpr int kGemmScales = kGemmWaves * kGemmTiles * 64;  // a copy for each half
+constexpr int gemm_stage(int s) { return 32 * s * 2 * kBlock + kGemmCodes + kGemmScales; }
+constexpr int gemm_stages(int s) { return 3 * gemm_stage(s) <= 160 * 1024 ? 3 : 2; }
 
 // async_load_1k's counterpart for 4 bytes a lane.
 __device__ __forceinline__ void async_load_256(const void* src, uint32_t lds) {
@@ -30,91 +37,32 @@ __device__ __forceinline__ void async_load_256(const void* src, uint32_t lds) {
                : "memory");
 }
 
-template <int MT, bool GATEUP>
-__global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int64_t rows, int n_tiles) {
-  constexpr int kXStage = 16 * MT * 2 * kBlock;
-  constexpr int kStage = kXStage + kGemmWaves * kGemmWaveStage;
-  constexpr int kLoads = MT + kGemmTiles + 1;  // a wave's a step
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[kGemmStages * kStage];
+// The loop over K and the outputs of a wave with CNT parts of 16 activation rows.
+// `load` issues the loads of a step into a stage; x_at and w_at are the wave's
+// first activation part and its weights in stage 0.
+template <int CNT, int STAGES, int STAGE_BYTES, int LOADS, typename Load, typename Store>
+__device__ __forceinline__ void w4_gemm_wave(const uint8_t* smem, int nb, int x_at, int w_at, int s_at, Load load, Store store) {
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, kq = lane >> 4;
-  const int nb = p.K / kBlock, groups = p.N / 16;
-  const int64_t a = blockIdx.x / n_tiles;
-  const int nt = (int)(blockIdx.x % n_tiles);
-
-  int e = 0, mc;
-  int64_t p0;
-  if (p.offsets) {
-    const ExpertRows ref = find_row_tile(p.offsets, p.E, (int)a, 16 * MT, (int)rows);
-    if (ref.e < 0) return;  // the whole workgroup
-    e = ref.e;
-    p0 = ref.p0;
-    mc = ref.m;
-  } else {
-    p0 = a * 16 * MT;
-    mc = (int)min((int64_t)16 * MT, rows - p0);
-  }
-
-  // Sources.  Load i of the activations takes rows 16 i + 4 wave + lane / 16.
-  const uint16_t* xs[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = 16 * i + 4 * wave + (lane >> 4);
-    int64_t row = p0 + min(m, mc - 1);  // rows past the tile's end read a valid one, and are not stored
-    if (p.sorted_src) {
-      row = p.sorted_src[row] / p.topk;
-      if (row < 0 || row >= p.x_rows) row = 0;
-    }
-    xs[i] = p.x + row * p.x_stride + (((lane & 15) ^ (m & 15)) * 8);
-  }
-  // Tile t of the wave: 16-row group `group(t)` of its matrix (groups past the last are that one again).
-  auto group = [&](int t) {
-    if (GATEUP) return nt * (kGemmRows / 32) + wave * 2 + (t & 1);
-    return nt * (kGemmRows / 16) + wave * kGemmTiles + t;
-  };
-  const uint8_t* ws[kGemmTiles];
-#pragma unroll
-  for (int t = 0; t < kGemmTiles; ++t)
-    ws[t] = (GATEUP && t >= 2 ? p.w1 : p.w0) + ((int64_t)e * groups + min(group(t), groups - 1)) * nb * kW4TileBytes + lane * 16;
-  const uint8_t* ss;  // lane 16 t + r: row r of tile t
-  {
-    const int t = lane >> 4;
-    ss = (GATEUP && t >= 2 ? p.s1 : p.s0) + ((int64_t)e * groups + min(group(t), groups - 1)) * ((nb + 3) / 4) * kW4ScaleTile + r * 16;
-  }
-  const uint32_t lds0 = lds_address(smem);
-  // Steps past the end load the last one again, so that every step issues the same loads.
-  auto load = [&](int step, int stage) {
-    const int b = min(step, nb - 1);
-    const uint32_t to = lds0 + stage * kStage;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) async_load_1k(xs[i] + (int64_t)b * kBlock, to + (i * kGemmWaves + wave) * 1024);
-    const uint32_t own = to + kXStage + wave * kGemmWaveStage;
-#pragma unroll
-    for (int t = 0; t < kGemmTiles; ++t) async_load_1k(ws[t] + (int64_t)b * kW4TileBytes, own + t * kW4TileBytes);
-    async_load_256(ss + (b >> 2) * kW4ScaleTile + (b & 3) * 4, own + kGemmTiles * kW4TileBytes);
-  };
-
-  v4f acc[kGemmTiles][MT];
+  v4f acc[kGemmTiles][CNT];
 #pragma unroll
   for (int t = 0; t < kGemmTiles; ++t)
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) acc[t][mt] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < CNT; ++c) acc[t][c] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int s = 0; s < kGemmStages - 1; ++s) load(s, s);
-  int stage = 0, fill = kGemmStages - 1;
+  for (int s = 0; s < STAGES - 1; ++s) load(s, s);
+  int stage = 0, fill = STAGES - 1;
   for (int b = 0; b < nb; ++b) {
     // Step b has landed for every wave, and every wave has read step b - 1, whose stage is loaded next.
-    wait_async_and_barrier<(kGemmStages - 2) * kLoads>();
-    load(b + kGemmStages - 1, fill);
-    const uint8_t* at = smem + stage * kStage;
-    const uint8_t* own = at + kXStage + wave * kGemmWaveStage;
+    wait_async_and_barrier<(STAGES - 2) * LOADS>();
+    load(b + STAGES - 1, fill);
+    const uint8_t* at = smem + stage * STAGE_BYTES;
     uint4 raw[kGemmTiles];
     uint32_t sc[kGemmTiles];
 #pragma unroll
     for (int t = 0; t < kGemmTiles; ++t) {
-      raw[t] = *reinterpret_cast<const uint4*>(own + t * kW4TileBytes + lane * 16);
-      sc[t] = *reinterpret_cast<const uint32_t*>(own + kGemmTiles * kW4TileBytes + 64 * t + 4 * r);
+      raw[t] = *reinterpret_cast<const uint4*>(at + w_at + t * kW4TileBytes + lane * 16);
+      sc[t] = *reinterpret_cast<const uint32_t*>(at + s_at + 64 * t + 4 * r);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -125,45 +73,132 @@ __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int6
         w[t] = w4_expand(codes, w4_scale(sc[t], j));
       }
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
+      for (int c = 0; c < CNT; ++c) {
         const w4_bf16x8 x = __builtin_bit_cast(
-            w4_bf16x8, *reinterpret_cast<const uint4*>(at + (mt * 16 + r) * (2 * kBlock) + (((4 * j + kq) ^ r) * 16)));
+            w4_bf16x8, *reinterpret_cast<const uint4*>(at + x_at + (c * 16 + r) * (2 * kBlock) + (((4 * j + kq) ^ r) * 16)));
 #pragma unroll
-        for (int t = 0; t < kGemmTiles; ++t) acc[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[t], x, acc[t][mt], 0, 0, 0);
+        for (int t = 0; t < kGemmTiles; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[t], x, acc[t][c], 0, 0, 0);
       }
     }
-    stage = stage + 1 == kGemmStages ? 0 : stage + 1;
-    fill = fill + 1 == kGemmStages ? 0 : fill + 1;
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    fill = fill + 1 == STAGES ? 0 : fill + 1;
   }
   // No load may reach LDS after the workgroup has ended.
   wait_async_and_barrier<0>();
-
-  // Lane 16 kq + r holds outputs 4 kq .. 4 kq + 3 of each tile for row r of each 16.
+  // Lane 16 kq + r holds outputs 4 kq .. 4 kq + 3 of each tile for row r of each part.
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const int m = mt * 16 + r;
-    if (m >= mc) continue;
+  for (int c = 0; c < CNT; ++c) {
+    v4f v[kGemmTiles];
 #pragma unroll
-    for (int t = 0; t < (GATEUP ? 2 : kGemmTiles); ++t) {
-      v4f v = acc[t][mt];
-      if (GATEUP) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = silu_mul_fast(v[c], acc[t + 2][mt][c]);
-      }
-      if (group(t) < groups) w4_store(p, p0 + m, group(t) * 16 + 4 * kq, v);
-    }
+    for (int t = 0; t < kGemmTiles; ++t) v[t] = acc[t][c];
+    store(c, v);
   }
 }
 
-template <int MT, bool GATEUP>
+// Rows of one expert, or of the one matrix, are cut into the fewest tiles of at most
+// 32 S rows, equal ones but for the rounding to parts of 16.
+template <int S, bool GATEUP>
+__global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int64_t rows, int n_tiles) {
+  constexpr int kXStage = 32 * S * 2 * kBlock;
+  constexpr int kStage = gemm_stage(S), kStages = gemm_stages(S);
+  constexpr int kXLoads = S;                      // a wave's a step: 8 S KB in all
+  constexpr int kWLoads = kGemmCodes / 1024 / kGemmWaves;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * kStage];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = wave >> 2, quarter = wave & 3;
+  const int r = lane & 15, kq = lane >> 4;
+  const int nb = p.K / kBlock, groups = p.N / 16;
+  const int nt = (int)(blockIdx.x % n_tiles);
+
+  int e = 0, mc;
+  int64_t p0;
+  if (p.offsets) {
+    const ExpertRows ref = find_even_tile(p.offsets, p.E, (int)(blockIdx.x / n_tiles), 32 * S, (int)rows);
+    if (ref.e < 0) return;  // the whole workgroup
+    e = ref.e;
+    p0 = ref.p0;
+    mc = ref.m;
+  } else {
+    const int64_t tiles = (rows + 32 * S - 1) / (32 * S), part = even_tile_rows(rows, tiles);
+    p0 = (int64_t)(blockIdx.x / n_tiles) * part;
+    if (p0 >= rows) return;
+    mc = (int)min(part, rows - p0);
+  }
+  const int parts = (mc + 15) / 16;
+  const int first = half ? (parts + 1) / 2 : 0, count = half ? parts / 2 : (parts + 1) / 2;
+
+  // Sources.  Load i of the activations takes rows 32 i + 4 wave + lane / 16.
+  const uint16_t* xs[kXLoads];
+#pragma unroll
+  for (int i = 0; i < kXLoads; ++i) {
+    const int m = 32 * i + 4 * wave + (lane >> 4);
+    int64_t row = p0 + min(m, mc - 1);  // rows past the tile's end read a valid one, and are not stored
+    if (p.sorted_src) {
+      row = p.sorted_src[row] / p.topk;
+      if (row < 0 || row >= p.x_rows) row = 0;
+    }
+    xs[i] = p.x + row * p.x_stride + (((lane & 15) ^ (m & 15)) * 8);
+  }
+  // Tile t of a quarter: 16-row group group(quarter, t) of its matrix (groups past the last are that one again).
+  auto group = [&](int q, int t) {
+    if (GATEUP) return nt * (kGemmRows / 32) + q * 2 + (t & 1);
+    return nt * (kGemmRows / 16) + q * kGemmTiles + t;
+  };
+  auto held = [&](int q, int t) { return (int64_t)e * groups + min(group(q, t), groups - 1); };
+  const uint8_t* ws[kWLoads];  // the half's tiles of its quarter
+#pragma unroll
+  for (int i = 0; i < kWLoads; ++i) {
+    const int t = half * kWLoads + i;
+    ws[i] = (GATEUP && t >= 2 ? p.w1 : p.w0) + held(quarter, t) * nb * kW4TileBytes + lane * 16;
+  }
+  const int st = lane >> 4;  // lane 16 t + r: row r of tile t
+  const uint8_t* ss = (GATEUP && st >= 2 ? p.s1 : p.s0) + held(quarter, st) * ((nb + 3) / 4) * kW4ScaleTile + r * 16;
+  const int w_at = kXStage + quarter * kGemmTiles * kW4TileBytes;
+  const int s_at = kXStage + kGemmCodes + wave * kGemmTiles * 64;
+  const uint32_t lds0 = lds_address(smem);
+  // Steps past the end load the last one again, so that every step issues the same loads.
+  auto load = [&](int step, int stage) {
+    const int b = min(step, nb - 1);
+    const uint32_t to = lds0 + stage * kStage;
+#pragma unroll
+    for (int i = 0; i < kXLoads; ++i) async_load_1k(xs[i] + (int64_t)b * kBlock, to + (i * kGemmWaves + wave) * 1024);
+#pragma unroll
+    for (int i = 0; i < kWLoads; ++i)
+      async_load_1k(ws[i] + (int64_t)b * kW4TileBytes, to + w_at + (half * kWLoads + i) * kW4TileBytes);
+    async_load_256(ss + (b >> 2) * kW4ScaleTile + (b & 3) * 4, to + s_at);
+  };
+  auto store = [&](int c, v4f (&v)[kGemmTiles]) {
+    const int m = (first + c) * 16 + r;
+    if (m >= mc) return;
+#pragma unroll
+    for (int t = 0; t < (GATEUP ? 2 : kGemmTiles); ++t) {
+      if (GATEUP) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[t][i] = silu_mul_fast(v[t][i], v[t + 2][i]);
+      }
+      if (group(quarter, t) < groups) w4_store(p, p0 + m, group(quarter, t) * 16 + 4 * kq, v[t]);
+    }
+  };
+  // A half without rows goes along with one part, of which it stores nothing.
+  const int x_at = first * 16 * 2 * kBlock;
+  constexpr int kL = kXLoads + kWLoads + 1;
+  if (S >= 5 && count == 5) w4_gemm_wave<5, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
+  else if (S >= 4 && count == 4) w4_gemm_wave<4, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
+  else if (S >= 3 && count == 3) w4_gemm_wave<3, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
+  else if (S >= 2 && count == 2) w4_gemm_wave<2, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
+  else w4_gemm_wave<1, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
+}
+
+template <int S, bool GATEUP>
 moe_status_t launch_gemm(const W4Args& a, int64_t rows, hipStream_t stream) {
   const char* name = GATEUP ? "w4_gemm_gateup" : "w4_gemm";
   const int cols = GATEUP ? kGemmRows / 2 : kGemmRows;
   const int n_tiles = (a.N + cols - 1) / cols;
-  const int64_t m_tiles = a.offsets ? rows / (16 * MT) + (rows < a.E ? rows : (int64_t)a.E) : (rows + 16 * MT - 1) / (16 * MT);
+  const int64_t m_tiles = a.offsets ? rows / (32 * S) + (rows < a.E ? rows : (int64_t)a.E) : (rows + 32 * S - 1) / (32 * S);
   if (m_tiles * n_tiles > w4_max_blocks(64 * kGemmWaves))
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "%s: too many rows and columns", name);
-  MOE_LAUNCH(name, (w4_gemm_kernel<MT, GATEUP>), dim3((unsigned)(m_tiles * n_tiles)), dim3(64 * kGemmWaves), 0, stream, a, rows,
+  MOE_LAUNCH(name, (w4_gemm_kernel<S, GATEUP>), dim3((unsigned)(m_tiles * n_tiles)), dim3(64 * kGemmWaves), 0, stream, a, rows,
              n_tiles);
   return check_launch(name);
 }
@@ -171,9 +206,10 @@ moe_status_t launch_gemm(const W4Args& a, int64_t rows, hipStream_t stream) {
 template <bool GATEUP>
 moe_status_t gemm_by_rows(const W4Args& a, int64_t rows, hipStream_t stream) {
   const int64_t mean = a.offsets ? rows / a.E : rows;  // rows a matrix
-  if (mean <= 32) return launch_gemm<2, GATEUP>(a, rows, stream);
-  if (mean <= 96) return launch_gemm<4, GATEUP>(a, rows, stream);
-  return launch_gemm<8, GATEUP>(a, rows, stream);
+  if (mean <= 24) return launch_gemm<1, GATEUP>(a, rows, stream);
+  if (mean <= 56) return launch_gemm<2, GATEUP>(a, rows, stream);
+  if (!a.offsets) return launch_gemm<4, GATEUP>(a, rows, stream);
+  return launch_gemm<5, GATEUP>(a, rows, stream);
 }
 
 }  // namespace

@@ -78,4 +78,37 @@ __device__ __forceinline__ ExpertRows find_row_tile(const int32_t* __restrict__ 
   return ExpertRows{-1, 0, 0};
 }
 
+// Rows of each of `tiles` tiles that share n rows evenly, in parts of 16 (the last
+// tile may hold fewer, or none).
+__host__ __device__ __forceinline__ int64_t even_tile_rows(int64_t n, int64_t tiles) {
+  return ((n + tiles - 1) / tiles + 15) / 16 * 16;
+}
+
+// The a-th of the tiles that share their expert's rows evenly, the fewest of at most
+// `tile` rows (a multiple of 16): as many as find_row_tile's.
+__device__ __forceinline__ ExpertRows find_even_tile(const int32_t* __restrict__ offsets, int E, int a, int tile, int rows) {
+  for (int c0 = 0; c0 < E; c0 += 256) {
+    const TileCounts t = count_tiles(offsets, E, c0, tile, rows);
+    if (a < t.all) {
+      ExpertRows found{-1, 0, 0};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const unsigned long long holds = __ballot(a < t.upto[c]);
+        if (found.e < 0 && holds) {
+          const int at = __ffsll((long long)holds) - 1;
+          const int n = __builtin_amdgcn_readlane(t.n[c], at);
+          const int tiles = (n + tile - 1) / tile;
+          const int part = (int)even_tile_rows(n, tiles);
+          const int skip = (tiles - (__builtin_amdgcn_readlane(t.upto[c], at) - a)) * part;
+          found = ExpertRows{skip < n ? c0 + 64 * c + at : -2, __builtin_amdgcn_readlane(t.lo[c], at) + skip, min(part, n - skip)};
+          if (found.e == -2) return ExpertRows{-1, 0, 0};
+        }
+      }
+      return found;
+    }
+    a -= t.all;
+  }
+  return ExpertRows{-1, 0, 0};
+}
+
 }  // namespace moe
