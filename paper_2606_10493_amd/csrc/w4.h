@@ -52,7 +52,23 @@ struct W4Args {
   float* out32;               // one of the two
   uint16_t* out16;
   int64_t out_stride;
+  int splits;                 // parts of K, each a workgroup's, that write their sums to partial [splits, x_rows, N]; 0, 1: none
+  float* partial;
 };
+
+// This workgroup's part of K, in blocks; a part of several writes its sums as they are.
+struct W4Range {
+  int b0, n;
+};
+__device__ __forceinline__ W4Range w4_part(W4Args& p, int part) {
+  const int nb = p.K / kBlock;
+  if (p.splits <= 1) return W4Range{0, nb};
+  const int b0 = (int)((int64_t)nb * part / p.splits), b1 = (int)((int64_t)nb * (part + 1) / p.splits);
+  p.out32 = p.partial + (int64_t)part * p.x_rows * p.N;
+  p.out_stride = p.N;
+  p.bias = nullptr;
+  return W4Range{b0, b1 - b0};
+}
 
 // Four neighbouring outputs of a row.
 __device__ __forceinline__ void w4_store(const W4Args& p, int64_t row, int n, v4f v) {

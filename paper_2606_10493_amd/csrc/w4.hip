@@ -1,21 +1,55 @@
 // The calls with 4-bit weights: checks, workspaces, and which kernel runs.
+#include <algorithm>
+
 #include "w4.h"
 
 namespace moe {
 
-moe_status_t run_w4_gemv(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
 bool w4_few_fits(int32_t K);
+int w4_few_splits(int32_t K);
 moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
+int w4_gemm_splits(int64_t rows, int32_t K, int32_t N);
 moe_status_t run_w4_gemm(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
 
 namespace {
 
+constexpr int kFewRows = 16;  // rows of one matrix that w4_few takes
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-moe_status_t run_w4(const W4Args& a, bool gateup, int32_t T, int64_t rows, hipStream_t stream) {
-  if (T <= MOE_DECODE_MAX_TOKENS && (a.offsets || T <= 16) && w4_few_fits(a.K)) return run_w4_few(a, gateup, rows, stream);
-  if (T <= MOE_DECODE_MAX_TOKENS) return run_w4_gemv(a, gateup, rows, stream);
+// Experts.  Up to MOE_DECODE_MAX_TOKENS tokens most experts have a few rows, and all are bound by their weights.
+moe_status_t run_experts(const W4Args& a, bool gateup, int32_t T, int64_t rows, hipStream_t stream) {
+  if (T <= MOE_DECODE_MAX_TOKENS && w4_few_fits(a.K)) return run_w4_few(a, gateup, rows, stream);
   return run_w4_gemm(a, gateup, rows, stream);
+}
+
+int linear_splits(int32_t T, int32_t K, int32_t N) { return T <= kFewRows ? w4_few_splits(K) : w4_gemm_splits(T, K, N); }
+
+size_t partial_bytes(int32_t T, int32_t K, int32_t N) {
+  const int splits = linear_splits(T, K, N);
+  return splits > 1 ? (size_t)splits * (size_t)T * (size_t)N * sizeof(float) : 0;
+}
+
+// out = the parts' sums in their order (+ bias), four neighbouring outputs a lane.
+__global__ __launch_bounds__(256) void w4_join_kernel(W4Args p) {
+  const int64_t quads = p.x_rows * (p.N / 4);
+  const int64_t step = p.x_rows * p.N;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < quads; i += (int64_t)gridDim.x * blockDim.x) {
+    const int64_t row = i / (p.N / 4);
+    const int n = (int)(i - row * (p.N / 4)) * 4;
+    const float* from = p.partial + i * 4;
+    v4f v = *reinterpret_cast<const v4f*>(from);
+    for (int s = 1; s < p.splits; ++s) v += *reinterpret_cast<const v4f*>(from + s * step);
+    w4_store(p, row, n, v);
+  }
+}
+
+moe_status_t run_linear(const W4Args& a, int32_t T, hipStream_t stream) {
+  const moe_status_t st = T <= kFewRows ? run_w4_few(a, false, T, stream) : run_w4_gemm(a, false, T, stream);
+  if (st != MOE_OK || a.splits <= 1) return st;
+  const int64_t blocks = ((int64_t)T * (a.N / 4) + 255) / 256;
+  MOE_LAUNCH("w4_join", w4_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream, a);
+  return check_launch("w4_join");
 }
 
 moe_status_t check_w4_dims(const moe_dims_t& d, int32_t T, const char* who) {
@@ -52,14 +86,14 @@ moe_status_t expert_ffn_w4(const moe_dims_t& d, int32_t T, const uint16_t* x, co
   g.offsets = offsets; g.E = d.n_experts;
   g.w0 = w[0]; g.s0 = w[1]; g.w1 = w[2]; g.s1 = w[3];
   g.N = d.inter; g.K = d.hidden; g.out16 = h; g.out_stride = d.inter;
-  const moe_status_t st = run_w4(g, true, T, rows, stream);
+  const moe_status_t st = run_experts(g, true, T, rows, stream);
   if (st != MOE_OK) return st;
   W4Args dn{};
   dn.x = h; dn.x_stride = d.inter; dn.x_rows = rows;
   dn.offsets = offsets; dn.E = d.n_experts;
   dn.w0 = w[4]; dn.s0 = w[5];
   dn.N = d.hidden; dn.K = d.inter; dn.out32 = y; dn.out_stride = d.hidden;
-  return run_w4(dn, false, T, rows, stream);
+  return run_experts(dn, false, T, rows, stream);
 }
 
 struct W4LayerLayout {
@@ -92,10 +126,14 @@ W4LayerLayout w4_layer_layout(const moe_dims_t& d, int32_t T) {
 using namespace moe;
 
 extern "C" size_t moe_linear_w4_workspace(int32_t T, int32_t K, int32_t N) {
-  (void)T;
-  (void)K;
-  (void)N;
-  return 0;
+  if (T <= 0 || K <= 0 || N <= 0 || K % kBlock || N % 16) return 0;
+  // No smaller T needs more: the most rows of every number of parts count.
+  size_t need = partial_bytes(T, K, N);
+  const int32_t ends[] = {kFewRows, 32, 64};
+  for (const int32_t t : ends)
+    if (t < T) need = std::max(need, partial_bytes(t, K, N));
+  for (int32_t t = 128; t < T && t <= 128 * 256; t += 128) need = std::max(need, partial_bytes(t, K, N));
+  return align256(need);
 }
 
 extern "C" moe_status_t moe_linear_w4(const uint16_t* x, int64_t x_stride, int32_t T, int32_t K, const uint8_t* w,
@@ -120,7 +158,9 @@ extern "C" moe_status_t moe_linear_w4(const uint16_t* x, int64_t x_stride, int32
   a.out32 = out_type == MOE_F32 ? static_cast<float*>(out) : nullptr;
   a.out16 = out_type == MOE_F32 ? nullptr : static_cast<uint16_t*>(out);
   a.out_stride = out_stride;
-  return run_w4(a, false, T, T, stream);
+  a.splits = linear_splits(T, K, N);
+  a.partial = static_cast<float*>(ws);
+  return run_linear(a, T, stream);
 }
 
 extern "C" size_t moe_expert_ffn_w4_workspace(moe_dims_t d, int32_t T) {

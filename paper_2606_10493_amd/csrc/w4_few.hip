@@ -41,7 +41,8 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
   const int nb = p.K / kBlock;
   const int groups = p.N / 16;
   const int items_n = (groups + kTiles - 1) / kTiles;
-  const int kb0 = wave * NBW;
+  const W4Range range = w4_part(p, blockIdx.y);
+  const int kb0 = range.b0 + wave * NBW, last = range.b0 + range.n - 1;
   const int64_t chunks = (nb + 3) / 4;
 
   const int64_t m_tiles = p.offsets ? all_tiles(p.offsets, p.E, 16, (int)rows) : (rows + 15) / 16;
@@ -84,12 +85,12 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
     const uint8_t* w = w_base[mat] + g * nb * kW4TileBytes;
 #pragma unroll
     for (int u = 0; u < NBW; ++u)  // blocks past the last are that one again, against zeros
-      q.w[t][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(w + min(kb0 + u, nb - 1) * kW4TileBytes + lane * 16));
+      q.w[t][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(w + min(kb0 + u, last) * kW4TileBytes + lane * 16));
     const uint8_t* s = s_base[mat] + g * chunks * kW4ScaleTile + r * 16;
-    if constexpr (NBW == 5) {
+    if (NBW == 5 || p.splits > 1) {  // blocks that begin anywhere
 #pragma unroll
       for (int u = 0; u < NBW; ++u) {
-        const int b = min(kb0 + u, nb - 1);
+        const int b = min(kb0 + u, last);
         q.s[t][u] = *reinterpret_cast<const uint32_t*>(s + (b >> 2) * kW4ScaleTile + (b & 3) * 4);
       }
       return;
@@ -132,8 +133,8 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
     for (int u = 0; u < NBW; ++u)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint4 v = *reinterpret_cast<const uint4*>(xr + min(kb0 + u, nb - 1) * kBlock + 32 * j);
-        x[u][j] = __builtin_bit_cast(w4_bf16x8, kb0 + u < nb ? v : make_uint4(0, 0, 0, 0));
+        const uint4 v = *reinterpret_cast<const uint4*>(xr + min(kb0 + u, last) * kBlock + 32 * j);
+        x[u][j] = __builtin_bit_cast(w4_bf16x8, kb0 + u <= last ? v : make_uint4(0, 0, 0, 0));
       }
   };
 #pragma unroll
@@ -202,13 +203,14 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
 template <int NBW, int R, int D, bool GATEUP>
 moe_status_t launch_few(const W4Args& a, int64_t rows, hipStream_t stream) {
   const char* name = GATEUP ? "w4_few_gateup" : "w4_few";
-  const int waves = (a.K / kBlock + NBW - 1) / NBW;
+  const int splits = std::max(1, a.splits);
+  const int waves = ((a.K / kBlock + splits - 1) / splits + NBW - 1) / NBW;
   const int tiles = GATEUP ? R / 2 : R;
   const int64_t items_n = (a.N / 16 + tiles - 1) / tiles;
   // Row tiles of experts: each may leave its last one unfilled.
   const int64_t m_tiles = a.offsets ? rows / 16 + (rows < a.E ? rows : (int64_t)a.E) : (rows + 15) / 16;
-  const int64_t blocks = std::min<int64_t>(items_n * m_tiles, 256 * (few_waves(NBW) / waves));
-  MOE_LAUNCH(name, (w4_few_kernel<NBW, R, D, GATEUP>), dim3((unsigned)blocks), dim3(64 * waves), 2 * waves * R * 1024, stream, a, rows);
+  const int64_t blocks = std::min<int64_t>(items_n * m_tiles, std::max(1, 256 * (few_waves(NBW) / waves) / splits));
+  MOE_LAUNCH(name, (w4_few_kernel<NBW, R, D, GATEUP>), dim3((unsigned)blocks, splits), dim3(64 * waves), 2 * waves * R * 1024, stream, a, rows);
   return check_launch(name);
 }
 
@@ -216,8 +218,11 @@ moe_status_t launch_few(const W4Args& a, int64_t rows, hipStream_t stream) {
 
 bool w4_few_fits(int32_t K) { return K / kBlock <= kFewMaxBlocks; }
 
+// Parts of K of one matrix whose rows are longer than a workgroup holds.
+int w4_few_splits(int32_t K) { return w4_few_fits(K) ? 1 : (K / kBlock + 31) / 32; }
+
 moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
-  const int nb = a.K / kBlock;
+  const int splits = std::max(1, a.splits), nb = (a.K / kBlock + splits - 1) / splits;
   if (nb <= 8) return gateup ? launch_few<1, 2, 4, true>(a, rows, stream) : launch_few<1, 2, 4, false>(a, rows, stream);
   if (nb <= 32) return gateup ? launch_few<2, 2, 2, true>(a, rows, stream) : launch_few<2, 2, 2, false>(a, rows, stream);
   if (nb <= 48) return gateup ? launch_few<4, 2, 1, true>(a, rows, stream) : launch_few<4, 2, 1, false>(a, rows, stream);

@@ -14,6 +14,8 @@
 // two steps ahead, with one barrier a step; activation rows are gathered on the
 // way.  The 16-byte piece c of an activation row lies at position c ^ row % 16, so
 // that a quarter wave's reads fill all banks.
+#include <algorithm>
+
 #include "w4.h"
 #include "w4_rows.h"
 
@@ -110,6 +112,7 @@ __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int6
   const int r = lane & 15, kq = lane >> 4;
   const int nb = p.K / kBlock, groups = p.N / 16;
   const int nt = (int)(blockIdx.x % n_tiles);
+  const W4Range range = w4_part(p, blockIdx.y);
 
   int e = 0, mc;
   int64_t p0;
@@ -159,7 +162,7 @@ __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int6
   const uint32_t lds0 = lds_address(smem);
   // Steps past the end load the last one again, so that every step issues the same loads.
   auto load = [&](int step, int stage) {
-    const int b = min(step, nb - 1);
+    const int b = range.b0 + min(step, range.n - 1);
     const uint32_t to = lds0 + stage * kStage;
 #pragma unroll
     for (int i = 0; i < kXLoads; ++i) async_load_1k(xs[i] + (int64_t)b * kBlock, to + (i * kGemmWaves + wave) * 1024);
@@ -183,11 +186,11 @@ __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int6
   // A half without rows goes along with one part, of which it stores nothing.
   const int x_at = first * 16 * 2 * kBlock;
   constexpr int kL = kXLoads + kWLoads + 1;
-  if (S >= 5 && count == 5) w4_gemm_wave<5, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
-  else if (S >= 4 && count == 4) w4_gemm_wave<4, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
-  else if (S >= 3 && count == 3) w4_gemm_wave<3, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
-  else if (S >= 2 && count == 2) w4_gemm_wave<2, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
-  else w4_gemm_wave<1, kStages, kStage, kL>(smem, nb, x_at, w_at, s_at, load, store);
+  if (S >= 5 && count == 5) w4_gemm_wave<5, kStages, kStage, kL>(smem, range.n, x_at, w_at, s_at, load, store);
+  else if (S >= 4 && count == 4) w4_gemm_wave<4, kStages, kStage, kL>(smem, range.n, x_at, w_at, s_at, load, store);
+  else if (S >= 3 && count == 3) w4_gemm_wave<3, kStages, kStage, kL>(smem, range.n, x_at, w_at, s_at, load, store);
+  else if (S >= 2 && count == 2) w4_gemm_wave<2, kStages, kStage, kL>(smem, range.n, x_at, w_at, s_at, load, store);
+  else w4_gemm_wave<1, kStages, kStage, kL>(smem, range.n, x_at, w_at, s_at, load, store);
 }
 
 template <int S, bool GATEUP>
@@ -196,26 +199,46 @@ moe_status_t launch_gemm(const W4Args& a, int64_t rows, hipStream_t stream) {
   const int cols = GATEUP ? kGemmRows / 2 : kGemmRows;
   const int n_tiles = (a.N + cols - 1) / cols;
   const int64_t m_tiles = a.offsets ? rows / (32 * S) + (rows < a.E ? rows : (int64_t)a.E) : (rows + 32 * S - 1) / (32 * S);
-  if (m_tiles * n_tiles > w4_max_blocks(64 * kGemmWaves))
+  if (m_tiles * n_tiles * std::max(1, a.splits) > w4_max_blocks(64 * kGemmWaves))
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "%s: too many rows and columns", name);
-  MOE_LAUNCH(name, (w4_gemm_kernel<S, GATEUP>), dim3((unsigned)(m_tiles * n_tiles)), dim3(64 * kGemmWaves), 0, stream, a, rows,
-             n_tiles);
+  MOE_LAUNCH(name, (w4_gemm_kernel<S, GATEUP>), dim3((unsigned)(m_tiles * n_tiles), std::max(1, a.splits)), dim3(64 * kGemmWaves), 0,
+             stream, a, rows, n_tiles);
   return check_launch(name);
 }
 
 template <bool GATEUP>
 moe_status_t gemm_by_rows(const W4Args& a, int64_t rows, hipStream_t stream) {
-  const int64_t mean = a.offsets ? rows / a.E : rows;  // rows a matrix
+  const int64_t mean = rows / a.E;  // rows a matrix
   if (mean <= 24) return launch_gemm<1, GATEUP>(a, rows, stream);
   if (mean <= 56) return launch_gemm<2, GATEUP>(a, rows, stream);
-  if (!a.offsets) return launch_gemm<4, GATEUP>(a, rows, stream);
   return launch_gemm<5, GATEUP>(a, rows, stream);
+}
+
+// Activation rows of a tile of one matrix, over 32.
+int dense_parts(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+
+int64_t dense_tiles(int64_t rows, int32_t N) {
+  const int tile = 32 * dense_parts(rows);
+  return (rows + tile - 1) / tile * ((N + kGemmRows - 1) / kGemmRows);
 }
 
 }  // namespace
 
+// Parts of K of one matrix: where the tiles leave most CUs without work, as many as fill
+// them once, of at least kSplitSteps steps.
+int w4_gemm_splits(int64_t rows, int32_t K, int32_t N) {
+  constexpr int kSplitSteps = 4;
+  const int64_t tiles = dense_tiles(rows, N);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, K / kBlock / kSplitSteps));
+}
+
 moe_status_t run_w4_gemm(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
-  return gateup ? gemm_by_rows<true>(a, rows, stream) : gemm_by_rows<false>(a, rows, stream);
+  if (a.offsets) return gateup ? gemm_by_rows<true>(a, rows, stream) : gemm_by_rows<false>(a, rows, stream);
+  switch (dense_parts(rows)) {
+    case 1: return launch_gemm<1, false>(a, rows, stream);
+    case 2: return launch_gemm<2, false>(a, rows, stream);
+    default: return launch_gemm<4, false>(a, rows, stream);
+  }
 }
 
 }  // namespace moe
