@@ -56,14 +56,17 @@ struct W4Args {
   float* partial;
 };
 
-// This workgroup's part of K, in blocks; a part of several writes its sums as they are.
+// This workgroup's part of K, in blocks (it begins with the scales of 512 columns); a
+// part of several writes its sums as they are.
 struct W4Range {
   int b0, n;
 };
 __device__ __forceinline__ W4Range w4_part(W4Args& p, int part) {
   const int nb = p.K / kBlock;
   if (p.splits <= 1) return W4Range{0, nb};
-  const int b0 = (int)((int64_t)nb * part / p.splits), b1 = (int)((int64_t)nb * (part + 1) / p.splits);
+  const uint32_t chunks = (nb + 3) / 4, each = chunks / p.splits, more = chunks - each * p.splits;
+  const int b0 = 4 * (part * each + min((uint32_t)part, more));
+  const int b1 = min(nb, b0 + 4 * (int)(each + ((uint32_t)part < more ? 1u : 0u)));
   p.out32 = p.partial + (int64_t)part * p.x_rows * p.N;
   p.out_stride = p.N;
   p.bias = nullptr;

@@ -25,18 +25,26 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// Waves of a workgroup (a CU's), so that NBW blocks of activations fit their registers.
+// Waves of a CU, so that NBW blocks of activations fit their registers; a workgroup
+// has up to 12, whose sums fit 64 KB of LDS beside the list of row tiles.
 constexpr int few_waves(int nbw) { return nbw <= 2 ? 16 : 12; }
-constexpr int kFewMaxBlocks = 60;  // 12 waves of 5
+constexpr int kFewMaxWaves = 12;
+constexpr int kFewMaxBlocks = 60;  // K blocks: 12 waves of 5
+// Row tiles of experts: at most one an expert, and one for 16 rows.
+constexpr int kFewMaxRows = MOE_DECODE_MAX_TOKENS * 32;
+constexpr int few_tiles(int rows, int E) { return (rows < E ? rows : E) + rows / 16; }
 
-template <int NBW, int R, int D, bool GATEUP>
-__global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_few_kernel(W4Args p, int64_t rows) {
+enum FewMode { kDense, kExperts, kExpertsGateUp };
+
+template <int NBW, int R, int D, FewMode MODE>
+__global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_kernel(W4Args p, int rows) {
+  constexpr bool GATEUP = MODE == kExpertsGateUp;
   constexpr int kTiles = GATEUP ? R / 2 : R;  // tiles of outputs
-  extern __shared__ __attribute__((aligned(16))) uint8_t red_bytes[];
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = blockDim.x >> 6;
-  v4f* red = reinterpret_cast<v4f*>(red_bytes);  // [2][waves][R][64]
+  v4f* red = reinterpret_cast<v4f*>(lds);  // [2][waves][R][64]
   const int r = lane & 15, kq = lane >> 4;
   const int nb = p.K / kBlock;
   const int groups = p.N / 16;
@@ -45,25 +53,38 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
   const int kb0 = range.b0 + wave * NBW, last = range.b0 + range.n - 1;
   const int64_t chunks = (nb + 3) / 4;
 
-  const int64_t m_tiles = p.offsets ? all_tiles(p.offsets, p.E, 16, (int)rows) : (rows + 15) / 16;
-  const int64_t items = m_tiles * items_n;
-  const int64_t first = items * blockIdx.x / gridDim.x, end = items * (blockIdx.x + 1) / gridDim.x;
-  if (first >= end) return;
+  // The row tiles, and this workgroup's items: neighbouring ones, of neighbouring weights.
+  int m_tiles = (rows + 15) / 16;
+  int2* list = reinterpret_cast<int2*>(lds + (size_t)2 * waves * R * 1024);
+  if constexpr (MODE != kDense) {
+    const int most = few_tiles(rows, p.E);
+    if (wave == 0) {
+      const int n = list_row_tiles(p.offsets, p.E, 16, rows, most, list);
+      if (lane == 0) list[most] = make_int2(n, 0);
+    }
+    __syncthreads();
+    m_tiles = __builtin_amdgcn_readfirstlane(list[most].x);
+  }
+  // (A division of 64 bits is a hundred instructions: the launch sees to it that the items fit 32.)
+  const uint32_t items = (uint32_t)(m_tiles * items_n);
+  const uint32_t each = items / gridDim.x, more = items - each * gridDim.x;  // the first `more` workgroups take one more
+  const uint32_t first = blockIdx.x * each + min(blockIdx.x, more);
+  int todo = (int)(each + (blockIdx.x < more ? 1u : 0u));
+  if (todo == 0) return;
 
   struct Tile {
-    int64_t a, p0;
-    int e, m;
+    int a, e, p0, m;
   };
-  auto find = [&](int64_t a) {
-    if (!p.offsets) return Tile{a, a * 16, 0, (int)min((int64_t)16, rows - a * 16)};
-    const ExpertRows t = find_row_tile(p.offsets, p.E, (int)a, 16, (int)rows);
-    return Tile{a, t.p0, t.e, t.m};
+  auto find = [&](int a) {
+    if constexpr (MODE == kDense) return Tile{a, 0, a * 16, min(16, rows - a * 16)};
+    const int p0 = __builtin_amdgcn_readfirstlane(list[a].x), em = __builtin_amdgcn_readfirstlane(list[a].y);
+    return Tile{a, em & 0xffff, p0, em >> 16};
   };
 
   // What is loaded next: item lg of row tile lk.
-  Tile lk = find(first / items_n);
-  int lg = (int)(first - lk.a * items_n);
-  int64_t left = end - first;  // items that are not loaded yet
+  Tile lk = find((int)(first / (uint32_t)items_n));
+  int lg = (int)(first - (uint32_t)lk.a * items_n);
+  int left = todo;  // items that are not loaded yet
   const uint8_t *w_base[GATEUP ? 2 : 1], *s_base[GATEUP ? 2 : 1];
   auto point = [&]() {
     const int64_t g = (int64_t)lk.e * groups;
@@ -87,7 +108,7 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
     for (int u = 0; u < NBW; ++u)  // blocks past the last are that one again, against zeros
       q.w[t][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(w + min(kb0 + u, last) * kW4TileBytes + lane * 16));
     const uint8_t* s = s_base[mat] + g * chunks * kW4ScaleTile + r * 16;
-    if (NBW == 5 || p.splits > 1) {  // blocks that begin anywhere
+    if constexpr (NBW == 3 || NBW == 5) {  // blocks that begin anywhere
 #pragma unroll
       for (int u = 0; u < NBW; ++u) {
         const int b = min(kb0 + u, last);
@@ -95,7 +116,9 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
       }
       return;
     }
-    s += (kb0 >> 2) * kW4ScaleTile + (kb0 & 3) * 4;
+    // (behind the last column's scales there is padding to be read, and a wave without blocks reads the last ones)
+    const int sb = min(kb0, last) & ~(NBW - 1);
+    s += (sb >> 2) * kW4ScaleTile + (sb & 3) * 4;
     if constexpr (NBW == 4) {
       const u32x4 v = *reinterpret_cast<const u32x4*>(s);
 #pragma unroll
@@ -108,6 +131,7 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
       q.s[t][0] = *reinterpret_cast<const uint32_t*>(s);
     }
   };
+  // (An expert's items are at least D, so the item that is multiplied next is of this row tile or the one before.)
   auto next_item = [&]() {
     if (--left <= 0) return;  // the last item is loaded again, and not used
     if (++lg < items_n) return;
@@ -139,16 +163,16 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
   };
 #pragma unroll
   for (int d = 0; d < D; ++d) {
+    if (d) next_item();
 #pragma unroll
     for (int t = 0; t < R; ++t) load(q[d], t);
-    next_item();
   }
   load_x();
 
   int parity = 0;
-  int64_t todo = end - first;
   auto item = [&](Codes& c) {
-    v4f* mine = red + (int64_t)parity * waves * R * 64;
+    next_item();
+    v4f* mine = red + parity * waves * R * 64;
 #pragma unroll
     for (int t = 0; t < R; ++t) {
       v4f acc = v4f{0.f, 0.f, 0.f, 0.f};
@@ -160,7 +184,6 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
       load(c, t);
       mine[(wave * R + t) * 64 + lane] = acc;
     }
-    next_item();
     // A plain barrier: loads stay in flight across it.
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     // The waves' sums, in wave order.  Other waves finish the next item's, and all go on meanwhile.
@@ -173,13 +196,13 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = silu_mul(v[i], u[i]);
       }
-      if (r < ck.m && cg * kTiles + t < groups) w4_store(p, ck.p0 + r, (cg * kTiles + t) * 16 + 4 * kq, v);
+      if (r < ck.m && cg * kTiles + t < groups) w4_store(p, (int64_t)ck.p0 + r, (cg * kTiles + t) * 16 + 4 * kq, v);
     }
     parity ^= 1;
     --todo;
     if (++cg == items_n && todo > 0) {
       cg = 0;
-      ck = find(ck.a + 1);
+      ck = lk;
       load_x();
     }
   };
@@ -200,18 +223,37 @@ __global__ __launch_bounds__(64 * few_waves(NBW), few_waves(NBW) / 4) void w4_fe
   }
 }
 
-template <int NBW, int R, int D, bool GATEUP>
-moe_status_t launch_few(const W4Args& a, int64_t rows, hipStream_t stream) {
-  const char* name = GATEUP ? "w4_few_gateup" : "w4_few";
+// K blocks of a workgroup: a part's, whole groups of four.
+int few_blocks(const W4Args& a) {
+  const int splits = std::max(1, a.splits), nb = a.K / kBlock;
+  return splits == 1 ? nb : 4 * (((nb + 3) / 4 + splits - 1) / splits);
+}
+
+template <int NBW, int D, FewMode MODE>
+moe_status_t launch_few(const W4Args& a, int rows, hipStream_t stream) {
+  constexpr int R = 2;
+  const char* name = MODE == kExpertsGateUp ? "w4_few_gateup" : "w4_few";
   const int splits = std::max(1, a.splits);
-  const int waves = ((a.K / kBlock + splits - 1) / splits + NBW - 1) / NBW;
-  const int tiles = GATEUP ? R / 2 : R;
+  const int waves = (few_blocks(a) + NBW - 1) / NBW;
+  const int tiles = MODE == kExpertsGateUp ? R / 2 : R;
   const int64_t items_n = (a.N / 16 + tiles - 1) / tiles;
-  // Row tiles of experts: each may leave its last one unfilled.
-  const int64_t m_tiles = a.offsets ? rows / 16 + (rows < a.E ? rows : (int64_t)a.E) : (rows + 15) / 16;
+  const int64_t m_tiles = MODE == kDense ? (rows + 15) / 16 : few_tiles(rows, a.E);
+  if (items_n * m_tiles > INT32_MAX) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "%s: too many rows and columns", name);
   const int64_t blocks = std::min<int64_t>(items_n * m_tiles, std::max(1, 256 * (few_waves(NBW) / waves) / splits));
-  MOE_LAUNCH(name, (w4_few_kernel<NBW, R, D, GATEUP>), dim3((unsigned)blocks, splits), dim3(64 * waves), 2 * waves * R * 1024, stream, a, rows);
+  const size_t lds = (size_t)2 * waves * R * 1024 + (MODE == kDense ? 0 : (m_tiles + 1) * sizeof(int2));
+  MOE_LAUNCH(name, (w4_few_kernel<NBW, R, D, MODE>), dim3((unsigned)blocks, splits), dim3(64 * waves), lds, stream, a, rows);
   return check_launch(name);
+}
+
+// NBW: a wave's K blocks.  Fewer waves of more blocks each, and more workgroups of them a CU, wait less for one another.
+template <FewMode MODE>
+moe_status_t few_by_length(const W4Args& a, int rows, hipStream_t stream) {
+  const int nb = few_blocks(a);
+  if (nb <= 8) return launch_few<1, 4, MODE>(a, rows, stream);
+  if (nb <= 24) return launch_few<2, 2, MODE>(a, rows, stream);
+  if (nb <= 36) return launch_few<3, 1, MODE>(a, rows, stream);
+  if (nb <= 48) return launch_few<4, 1, MODE>(a, rows, stream);
+  return launch_few<5, 1, MODE>(a, rows, stream);
 }
 
 }  // namespace
@@ -221,12 +263,11 @@ bool w4_few_fits(int32_t K) { return K / kBlock <= kFewMaxBlocks; }
 // Parts of K of one matrix whose rows are longer than a workgroup holds.
 int w4_few_splits(int32_t K) { return w4_few_fits(K) ? 1 : (K / kBlock + 31) / 32; }
 
+// Experts: at most kFewMaxRows rows.
 moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
-  const int splits = std::max(1, a.splits), nb = (a.K / kBlock + splits - 1) / splits;
-  if (nb <= 8) return gateup ? launch_few<1, 2, 4, true>(a, rows, stream) : launch_few<1, 2, 4, false>(a, rows, stream);
-  if (nb <= 32) return gateup ? launch_few<2, 2, 2, true>(a, rows, stream) : launch_few<2, 2, 2, false>(a, rows, stream);
-  if (nb <= 48) return gateup ? launch_few<4, 2, 1, true>(a, rows, stream) : launch_few<4, 2, 1, false>(a, rows, stream);
-  return gateup ? launch_few<5, 2, 1, true>(a, rows, stream) : launch_few<5, 2, 1, false>(a, rows, stream);
+  if (!a.offsets) return few_by_length<kDense>(a, (int)rows, stream);
+  if (rows > kFewMaxRows) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "w4_few: %lld rows", (long long)rows);
+  return gateup ? few_by_length<kExpertsGateUp>(a, (int)rows, stream) : few_by_length<kExperts>(a, (int)rows, stream);
 }
 
 }  // namespace moe

@@ -229,7 +229,7 @@ int64_t dense_tiles(int64_t rows, int32_t N) {
 int w4_gemm_splits(int64_t rows, int32_t K, int32_t N) {
   constexpr int kSplitSteps = 4;
   const int64_t tiles = dense_tiles(rows, N);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, K / kBlock / kSplitSteps));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, K / (kBlock * kSplitSteps)));
 }
 
 moe_status_t run_w4_gemm(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {

@@ -46,36 +46,25 @@ __device__ __forceinline__ TileCounts count_tiles(const int32_t* __restrict__ of
   return t;
 }
 
-// All experts' row tiles.
-__device__ __forceinline__ int all_tiles(const int32_t* __restrict__ offsets, int E, int tile, int rows) {
-  int n = 0;
-  for (int c0 = 0; c0 < E; c0 += 256) n += count_tiles(offsets, E, c0, tile, rows).all;
-  return n;
-}
-
-// The a-th tile of `tile` rows over all experts in order (an expert's last tile may
-// hold fewer rows).
-__device__ __forceinline__ ExpertRows find_row_tile(const int32_t* __restrict__ offsets, int E, int a, int tile, int rows) {
+// The row tiles of all experts in order, `tile` rows each but for an expert's last, as
+// {first row, expert | rows << 16}, those before `most`; returns how many there are.
+// tile <= 256, E <= 65536.  For the lanes of one wave.
+__device__ __forceinline__ int list_row_tiles(const int32_t* __restrict__ offsets, int E, int tile, int rows, int most, int2* list) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
   for (int c0 = 0; c0 < E; c0 += 256) {
     const TileCounts t = count_tiles(offsets, E, c0, tile, rows);
-    if (a < t.all) {
-      ExpertRows found{-1, 0, 0};
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const unsigned long long holds = __ballot(a < t.upto[c]);
-        if (found.e < 0 && holds) {
-          const int at = __ffsll((long long)holds) - 1;
-          const int n = __builtin_amdgcn_readlane(t.n[c], at);
-          const int back = __builtin_amdgcn_readlane(t.upto[c], at) - a;  // tiles from this one to the expert's last
-          const int skip = (((n + tile - 1) / tile) - back) * tile;
-          found = ExpertRows{c0 + 64 * c + at, __builtin_amdgcn_readlane(t.lo[c], at) + skip, min(tile, n - skip)};
-        }
+    for (int c = 0; c < 4; ++c) {
+      const int own = (t.n[c] + tile - 1) / tile;
+      for (int i = 0; i < own; ++i) {
+        const int at = before + t.upto[c] - own + i;
+        if (at < most) list[at] = make_int2(t.lo[c] + i * tile, (c0 + 64 * c + lane) | min(tile, t.n[c] - i * tile) << 16);
       }
-      return found;
     }
-    a -= t.all;
+    before += t.all;
   }
-  return ExpertRows{-1, 0, 0};
+  return min(before, most);
 }
 
 // Rows of each of `tiles` tiles that share n rows evenly, in parts of 16 (the last
@@ -85,7 +74,7 @@ __host__ __device__ __forceinline__ int64_t even_tile_rows(int64_t n, int64_t ti
 }
 
 // The a-th of the tiles that share their expert's rows evenly, the fewest of at most
-// `tile` rows (a multiple of 16): as many as find_row_tile's.
+// `tile` rows (a multiple of 16).
 __device__ __forceinline__ ExpertRows find_even_tile(const int32_t* __restrict__ offsets, int E, int a, int tile, int rows) {
   for (int c0 = 0; c0 < E; c0 += 256) {
     const TileCounts t = count_tiles(offsets, E, c0, tile, rows);
