@@ -56,6 +56,14 @@ struct W4Args {
   float* partial;
 };
 
+// A few slots' experts, sorted by the gate/up launch for the launches behind it (device memory).
+struct W4Slots {
+  const int32_t* ids;   // [slots], the router's
+  int32_t* dev_status;  // or NULL
+  int2* list;           // [kSortSlots + 1] row tiles, the last entry their number
+  int32_t* dest_row;    // [slots]
+};
+
 // This workgroup's part of K, in blocks (it begins with the scales of 512 columns); a
 // part of several writes its sums as they are.
 struct W4Range {

@@ -2,12 +2,17 @@
 #include <algorithm>
 
 #include "w4.h"
+#include "w4_rows.h"
 
 namespace moe {
 
 bool w4_few_fits(int32_t K);
 int w4_few_splits(int32_t K);
 moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
+moe_status_t run_w4_few_slots(const W4Args& a, int rows, const W4Slots& slots, hipStream_t stream);
+bool w4_down_combine_fits(int32_t K, int slots);
+moe_status_t run_w4_down_combine(const moe_dims_t& d, int tokens, const uint16_t* h, const W4Slots& s, const uint8_t* w,
+                                 const uint8_t* w_s, const float* topk_w, uint16_t* out, hipStream_t stream);
 int w4_gemm_splits(int64_t rows, int32_t K, int32_t N);
 moe_status_t run_w4_gemm(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
 
@@ -32,13 +37,13 @@ size_t partial_bytes(int32_t T, int32_t K, int32_t N) {
 
 // out = the parts' sums in their order (+ bias), four neighbouring outputs a lane.
 __global__ __launch_bounds__(256) void w4_join_kernel(W4Args p) {
-  const int64_t quads = p.x_rows * (p.N / 4);
+  const int n = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 4;
+  if (n >= p.N) return;
   const int64_t step = p.x_rows * p.N;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < quads; i += (int64_t)gridDim.x * blockDim.x) {
-    const int64_t row = i / (p.N / 4);
-    const int n = (int)(i - row * (p.N / 4)) * 4;
-    const float* from = p.partial + i * 4;
+  for (int64_t row = blockIdx.y; row < p.x_rows; row += gridDim.y) {
+    const float* from = p.partial + row * p.N + n;
     v4f v = *reinterpret_cast<const v4f*>(from);
+#pragma unroll 4
     for (int s = 1; s < p.splits; ++s) v += *reinterpret_cast<const v4f*>(from + s * step);
     w4_store(p, row, n, v);
   }
@@ -47,8 +52,8 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Args p) {
 moe_status_t run_linear(const W4Args& a, int32_t T, hipStream_t stream) {
   const moe_status_t st = T <= kFewRows ? run_w4_few(a, false, T, stream) : run_w4_gemm(a, false, T, stream);
   if (st != MOE_OK || a.splits <= 1) return st;
-  const int64_t blocks = ((int64_t)T * (a.N / 4) + 255) / 256;
-  MOE_LAUNCH("w4_join", w4_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream, a);
+  MOE_LAUNCH("w4_join", w4_join_kernel, dim3((unsigned)(((int64_t)a.N / 4 + 255) / 256), (unsigned)std::min(T, 1024)), dim3(256), 0,
+             stream, a);
   return check_launch("w4_join");
 }
 
@@ -78,14 +83,19 @@ moe_status_t check_workspace(const void* ws, size_t have, size_t need, const cha
   return MOE_OK;
 }
 
+W4Args gateup_args(const moe_dims_t& d, int32_t T, const uint16_t* x, const uint8_t* const (&w)[6], uint16_t* h) {
+  W4Args g{};
+  g.x = x; g.x_stride = d.hidden; g.x_rows = T; g.topk = d.topk; g.E = d.n_experts;
+  g.w0 = w[0]; g.s0 = w[1]; g.w1 = w[2]; g.s1 = w[3];
+  g.N = d.inter; g.K = d.hidden; g.out16 = h; g.out_stride = d.inter;
+  return g;
+}
+
 moe_status_t expert_ffn_w4(const moe_dims_t& d, int32_t T, const uint16_t* x, const int32_t* offsets, const int32_t* src,
                            const uint8_t* const (&w)[6], uint16_t* h, float* y, hipStream_t stream) {
   const int64_t rows = (int64_t)T * d.topk;
-  W4Args g{};
-  g.x = x; g.x_stride = d.hidden; g.x_rows = T; g.sorted_src = src; g.topk = d.topk;
-  g.offsets = offsets; g.E = d.n_experts;
-  g.w0 = w[0]; g.s0 = w[1]; g.w1 = w[2]; g.s1 = w[3];
-  g.N = d.inter; g.K = d.hidden; g.out16 = h; g.out_stride = d.inter;
+  W4Args g = gateup_args(d, T, x, w, h);
+  g.sorted_src = src; g.offsets = offsets;
   const moe_status_t st = run_experts(g, true, T, rows, stream);
   if (st != MOE_OK) return st;
   W4Args dn{};
@@ -97,7 +107,7 @@ moe_status_t expert_ffn_w4(const moe_dims_t& d, int32_t T, const uint16_t* x, co
 }
 
 struct W4LayerLayout {
-  size_t offsets, src, dest, y, perm, h, total;
+  size_t offsets, src, dest, list, y, perm, h, total;
 };
 
 W4LayerLayout w4_layer_layout(const moe_dims_t& d, int32_t T) {
@@ -112,6 +122,7 @@ W4LayerLayout w4_layer_layout(const moe_dims_t& d, int32_t T) {
   L.offsets = take((size_t)(d.n_experts + 1) * sizeof(int32_t));
   L.src = take(R * sizeof(int32_t));
   L.dest = take(R * sizeof(int32_t));
+  L.list = take((kSortSlots + 1) * sizeof(int2));
   L.y = take(R * d.hidden * sizeof(float));
   L.perm = take(moe_permute_workspace(T, d.topk, d.n_experts));
   L.h = take(moe_expert_ffn_w4_workspace(d, T));
@@ -210,9 +221,18 @@ extern "C" moe_status_t moe_ffn_layer_w4(moe_dims_t d, int32_t T, const uint16_t
   int32_t* src = reinterpret_cast<int32_t*>(b + L.src);
   int32_t* dest = reinterpret_cast<int32_t*>(b + L.dest);
   float* y = reinterpret_cast<float*>(b + L.y);
+  uint16_t* h = reinterpret_cast<uint16_t*>(b + L.h);
+  const int64_t slots = (int64_t)T * d.topk;
+  if (w4_few_fits(d.hidden) && slots <= kSortSlots && w4_down_combine_fits(d.inter, (int)slots)) {
+    // A few slots: two launches.  Gate/up sorts them itself, the down projection and the combine follow together.
+    const W4Slots s{topk_ids, dev_status, reinterpret_cast<int2*>(b + L.list), dest};
+    st = run_w4_few_slots(gateup_args(d, T, x, w, h), (int)slots, s, stream);
+    if (st != MOE_OK) return st;
+    return run_w4_down_combine(d, T, h, s, w_down, s_down, topk_w, out, stream);
+  }
   st = moe_permute(topk_ids, T, d.topk, d.n_experts, offsets, src, dest, dev_status, b + L.perm, L.h - L.perm, stream);
   if (st != MOE_OK) return st;
-  st = expert_ffn_w4(d, T, x, offsets, src, w, reinterpret_cast<uint16_t*>(b + L.h), y, stream);
+  st = expert_ffn_w4(d, T, x, offsets, src, w, h, y, stream);
   if (st != MOE_OK) return st;
   return moe_combine(y, dest, topk_w, T, d.topk, d.hidden, out, stream);
 }

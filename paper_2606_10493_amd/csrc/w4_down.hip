@@ -1,0 +1,138 @@
+// The down projection and the combine of a few slots with 4-bit weights in one
+// launch: a workgroup computes 16 output columns for every slot and combines them
+// per token in LDS, so that the fp32 expert rows are not written.
+//
+// Wave w takes the row tiles w, w + 8, ... (a few slots have about as many active
+// experts) and streams their 16 weight rows over all of K with two halves of kBlocks K
+// blocks in flight; the slots' rows of h lie in LDS.  The sums of a row tile are
+// the same as w4_few's but for their order in K; the combine is the definition's order
+// (see moe_combine).
+#include "w4.h"
+#include "w4_rows.h"
+
+namespace moe {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kDownWaves = 8;
+constexpr int kDownBlocks = 8;            // K blocks that are loaded together
+constexpr int kDownBytes = 64 * 1024;     // of LDS
+
+struct W4DownArgs {
+  const uint16_t* h;    // bf16 [slots, K], sorted
+  const int2* list;     // row tiles, their number in entry kSortSlots
+  const uint8_t *w, *s;  // packed [E, N, K]
+  int slots, tokens, topk, N, K;
+  const int32_t* dest_row;
+  const float* topk_w;
+  uint16_t* out;        // bf16 [tokens, N]
+};
+
+constexpr int down_stride(int K) { return 2 * K + 16; }  // bytes of a row of h in LDS: rows begin on other banks
+constexpr int64_t down_bytes(int K, int slots) { return (int64_t)slots * (64 + down_stride(K)); }
+
+__global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4DownArgs p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  float* y = reinterpret_cast<float*>(lds);  // [slots][16]
+  uint8_t* h = lds + p.slots * 64;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, kq = lane >> 4;
+  const int nb = p.K / kBlock, groups = p.N / 16, chunks = (nb + 3) / 4;
+  const int stride = down_stride(p.K);
+  const int n = __builtin_amdgcn_readfirstlane(p.list[kSortSlots].x);
+
+  struct Blocks {
+    u32x4 w[kDownBlocks];
+    u32x4 s[kDownBlocks / 4];
+  };
+  int e = 0, p0 = 0, m = 0;
+  const uint8_t *wt = p.w, *st = p.s;
+  auto point = [&](int a) {
+    const int x = __builtin_amdgcn_readfirstlane(p.list[a].x), em = __builtin_amdgcn_readfirstlane(p.list[a].y);
+    p0 = x;
+    e = em & 0xffff;
+    m = em >> 16;
+    const int64_t g = (int64_t)e * groups + blockIdx.x;
+    wt = p.w + g * nb * kW4TileBytes + lane * 16;
+    st = p.s + g * chunks * kW4ScaleTile + r * 16;
+  };
+  auto load = [&](int b, Blocks& q) {  // blocks past the last are that one again, against zeros
+#pragma unroll
+    for (int u = 0; u < kDownBlocks; ++u)
+      q.w[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wt + (int64_t)min(b + u, nb - 1) * kW4TileBytes));
+#pragma unroll
+    for (int u = 0; u < kDownBlocks / 4; ++u)
+      q.s[u] = *reinterpret_cast<const u32x4*>(st + min((b >> 2) + u, chunks - 1) * kW4ScaleTile);
+  };
+  Blocks q0, q1;
+  if (wave < n) {
+    point(wave);
+    load(0, q0);
+    load(kDownBlocks, q1);
+  }
+  // The slots' rows, 16 bytes a lane.
+  const int pieces = p.K / 8;
+  for (int i = threadIdx.x; i < p.slots * pieces; i += 64 * kDownWaves) {
+    const int row = i / pieces, c = i - row * pieces;
+    *reinterpret_cast<uint4*>(h + row * stride + c * 16) = *reinterpret_cast<const uint4*>(p.h + (int64_t)row * p.K + c * 8);
+  }
+  __syncthreads();
+
+  for (int a = wave; a < n; a += kDownWaves) {
+    if (a != wave) {
+      point(a);
+      load(0, q0);
+      load(kDownBlocks, q1);
+    }
+    const uint8_t* x = h + (p0 + min(r, m - 1)) * stride + 16 * kq;
+    v4f acc = v4f{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](int b, const Blocks& q) {
+#pragma unroll
+      for (int u = 0; u < kDownBlocks; ++u) {
+        if (b + u >= nb) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              w4_expand(q.w[u][j], w4_scale(q.s[u / 4][u % 4], j)),
+              __builtin_bit_cast(w4_bf16x8, *reinterpret_cast<const uint4*>(x + (b + u) * (2 * kBlock) + 64 * j)), acc, 0, 0, 0);
+      }
+    };
+    for (int b = 0; b < nb; b += 2 * kDownBlocks) {
+      multiply(b, q0);
+      if (b + 2 * kDownBlocks < nb) load(b + 2 * kDownBlocks, q0);
+      if (b + kDownBlocks >= nb) break;
+      multiply(b + kDownBlocks, q1);
+      if (b + 3 * kDownBlocks < nb) load(b + 3 * kDownBlocks, q1);
+    }
+    if (r < m) *reinterpret_cast<v4f*>(y + (p0 + r) * 16 + 4 * kq) = acc;
+  }
+  __syncthreads();
+  // Tokens' sums in slot order, products and sums rounded separately.
+  for (int i = threadIdx.x; i < p.tokens * 16; i += 64 * kDownWaves) {
+#pragma clang fp contract(off)
+    const int t = i / 16, c = i % 16;
+    float sum = 0.0f;
+    for (int j = 0; j < p.topk; ++j) sum = sum + p.topk_w[t * p.topk + j] * y[p.dest_row[t * p.topk + j] * 16 + c];
+    p.out[(int64_t)t * p.N + blockIdx.x * 16 + c] = f32_to_bf16_rne(sum);
+  }
+}
+
+}  // namespace
+
+bool w4_down_combine_fits(int32_t K, int slots) {
+  return slots <= kSortSlots && down_bytes(K, slots) <= kDownBytes;
+}
+
+moe_status_t run_w4_down_combine(const moe_dims_t& d, int tokens, const uint16_t* h, const W4Slots& s, const uint8_t* w,
+                                 const uint8_t* w_s, const float* topk_w, uint16_t* out, hipStream_t stream) {
+  const int slots = tokens * d.topk;
+  const W4DownArgs a{h, s.list, w, w_s, slots, tokens, d.topk, d.hidden, d.inter, s.dest_row, topk_w, out};
+  MOE_LAUNCH("w4_down_combine", w4_down_combine_kernel, dim3((unsigned)(d.hidden / 16)), dim3(64 * kDownWaves),
+             (size_t)down_bytes(d.inter, slots), stream, a);
+  return check_launch("w4_down_combine");
+}
+
+}  // namespace moe

@@ -34,11 +34,11 @@ constexpr int kFewMaxBlocks = 60;  // K blocks: 12 waves of 5
 constexpr int kFewMaxRows = MOE_DECODE_MAX_TOKENS * 32;
 constexpr int few_tiles(int rows, int E) { return (rows < E ? rows : E) + rows / 16; }
 
-enum FewMode { kDense, kExperts, kExpertsGateUp };
+enum FewMode { kDense, kExperts, kExpertsGateUp, kSlotsGateUp };
 
 template <int NBW, int R, int D, FewMode MODE>
-__global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_kernel(W4Args p, int rows) {
-  constexpr bool GATEUP = MODE == kExpertsGateUp;
+__global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_kernel(W4Args p, int rows, W4Slots slots) {
+  constexpr bool GATEUP = MODE == kExpertsGateUp || MODE == kSlotsGateUp;
   constexpr int kTiles = GATEUP ? R / 2 : R;  // tiles of outputs
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63;
@@ -56,7 +56,24 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
   // The row tiles, and this workgroup's items: neighbouring ones, of neighbouring weights.
   int m_tiles = (rows + 15) / 16;
   int2* list = reinterpret_cast<int2*>(lds + (size_t)2 * waves * R * 1024);
-  if constexpr (MODE != kDense) {
+  int* slot_src = reinterpret_cast<int*>(list + kSortSlots);  // kSlotsGateUp
+  if constexpr (MODE == kSlotsGateUp) {
+    int* count = slot_src + kSortSlots;
+    if (wave == 0) {
+      int place;
+      const int n = sort_slots(slots.ids, rows, p.E, list, slot_src, place);
+      if (lane == 0) *count = n;
+      if (blockIdx.x == 0 && lane < rows) slots.dest_row[lane] = place;
+    }
+    __syncthreads();
+    m_tiles = __builtin_amdgcn_readfirstlane(*count);
+    if (blockIdx.x == 0 && wave == waves - 1) {
+      const int bad = slot_errors(slots.ids, rows, p.topk, p.E);
+      if (slots.dev_status && bad && lane == 0) atomicOr(slots.dev_status, bad);
+      if (lane < m_tiles) slots.list[lane] = list[lane];
+      if (lane == 0) slots.list[kSortSlots] = make_int2(m_tiles, 0);
+    }
+  } else if constexpr (MODE != kDense) {
     const int most = few_tiles(rows, p.E);
     if (wave == 0) {
       const int n = list_row_tiles(p.offsets, p.E, 16, rows, most, list);
@@ -148,7 +165,9 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
     // Rows past the tile's last read that one again: what a lane has for an activation row reaches that row's sums
     // alone, which are not stored.
     int64_t row = ck.p0 + min(r, ck.m - 1);
-    if (p.sorted_src) {
+    if constexpr (MODE == kSlotsGateUp) {
+      row = slot_src[row] / p.topk;
+    } else if (p.sorted_src) {
       row = p.sorted_src[row] / p.topk;
       if (row < 0 || row >= p.x_rows) row = 0;
     }
@@ -230,30 +249,33 @@ int few_blocks(const W4Args& a) {
 }
 
 template <int NBW, int D, FewMode MODE>
-moe_status_t launch_few(const W4Args& a, int rows, hipStream_t stream) {
+moe_status_t launch_few(const W4Args& a, int rows, const W4Slots& slots, hipStream_t stream) {
   constexpr int R = 2;
-  const char* name = MODE == kExpertsGateUp ? "w4_few_gateup" : "w4_few";
+  constexpr bool kGateUp = MODE == kExpertsGateUp || MODE == kSlotsGateUp;
+  const char* name = kGateUp ? "w4_few_gateup" : "w4_few";
   const int splits = std::max(1, a.splits);
   const int waves = (few_blocks(a) + NBW - 1) / NBW;
-  const int tiles = MODE == kExpertsGateUp ? R / 2 : R;
+  const int tiles = kGateUp ? R / 2 : R;
   const int64_t items_n = (a.N / 16 + tiles - 1) / tiles;
   const int64_t m_tiles = MODE == kDense ? (rows + 15) / 16 : few_tiles(rows, a.E);
   if (items_n * m_tiles > INT32_MAX) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "%s: too many rows and columns", name);
   const int64_t blocks = std::min<int64_t>(items_n * m_tiles, std::max(1, 256 * (few_waves(NBW) / waves) / splits));
-  const size_t lds = (size_t)2 * waves * R * 1024 + (MODE == kDense ? 0 : (m_tiles + 1) * sizeof(int2));
-  MOE_LAUNCH(name, (w4_few_kernel<NBW, R, D, MODE>), dim3((unsigned)blocks, splits), dim3(64 * waves), lds, stream, a, rows);
+  const size_t lds = (size_t)2 * waves * R * 1024 + (MODE == kDense         ? 0
+                                                     : MODE == kSlotsGateUp ? kSortSlots * sizeof(int2) + (kSortSlots + 1) * sizeof(int)
+                                                                            : (m_tiles + 1) * sizeof(int2));
+  MOE_LAUNCH(name, (w4_few_kernel<NBW, R, D, MODE>), dim3((unsigned)blocks, splits), dim3(64 * waves), lds, stream, a, rows, slots);
   return check_launch(name);
 }
 
 // NBW: a wave's K blocks.  Fewer waves of more blocks each, and more workgroups of them a CU, wait less for one another.
 template <FewMode MODE>
-moe_status_t few_by_length(const W4Args& a, int rows, hipStream_t stream) {
+moe_status_t few_by_length(const W4Args& a, int rows, const W4Slots& slots, hipStream_t stream) {
   const int nb = few_blocks(a);
-  if (nb <= 8) return launch_few<1, 4, MODE>(a, rows, stream);
-  if (nb <= 24) return launch_few<2, 2, MODE>(a, rows, stream);
-  if (nb <= 36) return launch_few<3, 1, MODE>(a, rows, stream);
-  if (nb <= 48) return launch_few<4, 1, MODE>(a, rows, stream);
-  return launch_few<5, 1, MODE>(a, rows, stream);
+  if (nb <= 8) return launch_few<1, 4, MODE>(a, rows, slots, stream);
+  if (nb <= 24) return launch_few<2, 2, MODE>(a, rows, slots, stream);
+  if (nb <= 36) return launch_few<3, 1, MODE>(a, rows, slots, stream);
+  if (nb <= 48) return launch_few<4, 1, MODE>(a, rows, slots, stream);
+  return launch_few<5, 1, MODE>(a, rows, slots, stream);
 }
 
 }  // namespace
@@ -265,9 +287,15 @@ int w4_few_splits(int32_t K) { return w4_few_fits(K) ? 1 : (K / kBlock + 31) / 3
 
 // Experts: at most kFewMaxRows rows.
 moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
-  if (!a.offsets) return few_by_length<kDense>(a, (int)rows, stream);
+  if (!a.offsets) return few_by_length<kDense>(a, (int)rows, W4Slots{}, stream);
   if (rows > kFewMaxRows) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "w4_few: %lld rows", (long long)rows);
-  return gateup ? few_by_length<kExpertsGateUp>(a, (int)rows, stream) : few_by_length<kExperts>(a, (int)rows, stream);
+  return gateup ? few_by_length<kExpertsGateUp>(a, (int)rows, W4Slots{}, stream)
+                : few_by_length<kExperts>(a, (int)rows, W4Slots{}, stream);
+}
+
+// Gate and up of at most kSortSlots slots that nothing has sorted yet.
+moe_status_t run_w4_few_slots(const W4Args& a, int rows, const W4Slots& slots, hipStream_t stream) {
+  return few_by_length<kSlotsGateUp>(a, rows, slots, stream);
 }
 
 }  // namespace moe

@@ -67,6 +67,56 @@ __device__ __forceinline__ int list_row_tiles(const int32_t* __restrict__ offset
   return min(before, most);
 }
 
+constexpr int kSortSlots = 64;  // slots that a wave sorts by itself
+
+// The sort of moe_permute for up to 64 slots, one a lane, by one wave: src[p] = slot at
+// sorted position p, `place` the lane's position, and the row tiles of 16 as
+// list_row_tiles lists them (returned: how many).  Slots whose id lies outside [0, E)
+// come last and belong to no tile.  Every lane compares with every slot.
+__device__ __forceinline__ int sort_slots(const int32_t* __restrict__ ids, int slots, int E, int2* list, int* src, int& place) {
+  const int lane = threadIdx.x & 63;
+  const int id = lane < slots ? ids[lane] : -1;
+  const bool ok = id >= 0 && id < E;
+  const int key = ok ? id : INT32_MAX;
+  int less = 0, before = 0, same = 0;
+  for (int i0 = 0; i0 < slots; i0 += 8) {  // (lanes behind the last slot count as bad ids behind it)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int other = __builtin_amdgcn_readlane(key, i0 + u);
+      less += other < key ? 1 : 0;
+      same += other == key ? 1 : 0;
+      before += other == key && i0 + u < lane ? 1 : 0;
+    }
+  }
+  place = less + before;
+  const bool begins = ok && before % 16 == 0;
+  const unsigned long long all = __ballot(begins);
+  int rank = 0;
+  const int begin_at = begins ? place : INT32_MAX;
+  for (int i0 = 0; i0 < slots; i0 += 8) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) rank += __builtin_amdgcn_readlane(begin_at, i0 + u) < place ? 1 : 0;
+  }
+  if (lane < slots) src[place] = lane;
+  if (begins) list[rank] = make_int2(place, id | min(16, same - before) << 16);
+  return __popcll(all);
+}
+
+// MOE_DEV_* bits of the slots' ids, known to every lane.
+__device__ __forceinline__ int slot_errors(const int32_t* __restrict__ ids, int slots, int topk, int E) {
+  const int lane = threadIdx.x & 63;
+  const int id = lane < slots ? ids[lane] : -1;
+  const int token = lane / topk * topk;  // the token's first slot
+  bool twice = false;
+  for (int i0 = 0; i0 < slots; i0 += 8) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      twice |= i0 + u >= token && i0 + u < lane && lane < slots && __builtin_amdgcn_readlane(id, i0 + u) == id;
+  }
+  const bool bad = lane < slots && (id < 0 || id >= E);
+  return (__any(bad) ? MOE_DEV_BAD_EXPERT_ID : 0) | (__any(twice && !bad) ? MOE_DEV_DUP_EXPERT_ID : 0);
+}
+
 // Rows of each of `tiles` tiles that share n rows evenly, in parts of 16 (the last
 // tile may hold fewer, or none).
 __host__ __device__ __forceinline__ int64_t even_tile_rows(int64_t n, int64_t tiles) {
