@@ -42,7 +42,9 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
   const int r = lane & 15, kq = lane >> 4;
   const int nb = p.K / kBlock, groups = p.N / 16, chunks = (nb + 3) / 4;
   const int stride = down_stride(p.K);
-  const int n = __builtin_amdgcn_readfirstlane(p.list[kSortSlots].x);
+  // (both loads go out together)
+  const int2 count = p.list[kSortSlots], own = p.list[wave];
+  const int n = __builtin_amdgcn_readfirstlane(count.x);
 
   struct Blocks {
     u32x4 w[kDownBlocks];
@@ -50,9 +52,9 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
   };
   int e = 0, p0 = 0, m = 0;
   const uint8_t *wt = p.w, *st = p.s;
-  auto point = [&](int a) {
-    const int x = __builtin_amdgcn_readfirstlane(p.list[a].x), em = __builtin_amdgcn_readfirstlane(p.list[a].y);
-    p0 = x;
+  auto point = [&](int2 tile) {
+    const int em = __builtin_amdgcn_readfirstlane(tile.y);
+    p0 = __builtin_amdgcn_readfirstlane(tile.x);
     e = em & 0xffff;
     m = em >> 16;
     const int64_t g = (int64_t)e * groups + blockIdx.x;
@@ -69,7 +71,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
   };
   Blocks q0, q1;
   if (wave < n) {
-    point(wave);
+    point(own);
     load(0, q0);
     load(kDownBlocks, q1);
   }
@@ -83,7 +85,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
 
   for (int a = wave; a < n; a += kDownWaves) {
     if (a != wave) {
-      point(a);
+      point(p.list[a]);
       load(0, q0);
       load(kDownBlocks, q1);
     }

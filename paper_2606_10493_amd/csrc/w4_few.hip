@@ -57,7 +57,18 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
   int m_tiles = (rows + 15) / 16;
   int2* list = reinterpret_cast<int2*>(lds + (size_t)2 * waves * R * 1024);
   int* slot_src = reinterpret_cast<int*>(list + kSortSlots);  // kSlotsGateUp
-  if constexpr (MODE == kSlotsGateUp) {
+  // What the launch behind this one, and the caller, need to know of the slots.
+  auto report_slots = [&]() {
+    const int bad = slot_errors(slots.ids, rows, p.topk, p.E);
+    if (slots.dev_status && bad && lane == 0) atomicOr(slots.dev_status, bad);
+    if (lane == 0) slots.list[kSortSlots] = make_int2(m_tiles, 0);
+  };
+  // One token's slots need no sort: slot j is row tile j (one with a bad id is computed with expert 0, which
+  // nothing but this token's output sees).
+  const bool one = MODE == kSlotsGateUp && rows == p.topk;
+  if (one) {
+    m_tiles = rows;
+  } else if constexpr (MODE == kSlotsGateUp) {
     int* count = slot_src + kSortSlots;
     if (wave == 0) {
       int place;
@@ -67,11 +78,9 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
     }
     __syncthreads();
     m_tiles = __builtin_amdgcn_readfirstlane(*count);
-    if (blockIdx.x == 0 && wave == waves - 1) {
-      const int bad = slot_errors(slots.ids, rows, p.topk, p.E);
-      if (slots.dev_status && bad && lane == 0) atomicOr(slots.dev_status, bad);
+    if (blockIdx.x == 0 && wave == waves - 1) {  // also where no slot has an expert
+      report_slots();
       if (lane < m_tiles) slots.list[lane] = list[lane];
-      if (lane == 0) slots.list[kSortSlots] = make_int2(m_tiles, 0);
     }
   } else if constexpr (MODE != kDense) {
     const int most = few_tiles(rows, p.E);
@@ -94,6 +103,10 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
   };
   auto find = [&](int a) {
     if constexpr (MODE == kDense) return Tile{a, 0, a * 16, min(16, rows - a * 16)};
+    if (one) {
+      const int e = slots.ids[a];
+      return Tile{a, (uint32_t)e < (uint32_t)p.E ? e : 0, a, 1};
+    }
     const int p0 = __builtin_amdgcn_readfirstlane(list[a].x), em = __builtin_amdgcn_readfirstlane(list[a].y);
     return Tile{a, em & 0xffff, p0, em >> 16};
   };
@@ -166,7 +179,7 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
     // alone, which are not stored.
     int64_t row = ck.p0 + min(r, ck.m - 1);
     if constexpr (MODE == kSlotsGateUp) {
-      row = slot_src[row] / p.topk;
+      row = one ? 0 : slot_src[row] / p.topk;
     } else if (p.sorted_src) {
       row = p.sorted_src[row] / p.topk;
       if (row < 0 || row >= p.x_rows) row = 0;
@@ -176,9 +189,15 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
     for (int u = 0; u < NBW; ++u)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint4 v = *reinterpret_cast<const uint4*>(xr + min(kb0 + u, last) * kBlock + 32 * j);
-        x[u][j] = __builtin_bit_cast(w4_bf16x8, kb0 + u <= last ? v : make_uint4(0, 0, 0, 0));
+        x[u][j] = __builtin_bit_cast(w4_bf16x8, *reinterpret_cast<const uint4*>(xr + min(kb0 + u, last) * kBlock + 32 * j));
       }
+    if (kb0 + NBW - 1 > last) {  // the last wave
+#pragma unroll
+      for (int u = 0; u < NBW; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[u][j] = kb0 + u <= last ? x[u][j] : __builtin_bit_cast(w4_bf16x8, make_uint4(0, 0, 0, 0));
+    }
   };
 #pragma unroll
   for (int d = 0; d < D; ++d) {
@@ -187,6 +206,14 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
     for (int t = 0; t < R; ++t) load(q[d], t);
   }
   load_x();
+  if (one && blockIdx.x == 0 && wave == waves - 1) {
+    report_slots();
+    if (lane < rows) {
+      const int e = slots.ids[lane];
+      slots.list[lane] = make_int2(lane, ((uint32_t)e < (uint32_t)p.E ? e : 0) | 1 << 16);
+      slots.dest_row[lane] = lane;
+    }
+  }
 
   int parity = 0;
   auto item = [&](Codes& c) {

@@ -138,6 +138,25 @@ def test_bad_ids_are_reported_and_leave_the_other_tokens(moe, tokens):
         assert torch.equal(out[rest.cuda()], good[rest.cuda()])
 
 
+@pytest.mark.parametrize("tokens", [1, 2, 70])
+def test_no_id_is_an_experts(moe, tokens):
+    """Every slot is bad: it is reported, and nothing outside the output is written."""
+    rng = np.random.default_rng(3)
+    h, i, e, k = 256, 128, 8, 2
+    stack = Stack(moe, rng, h, i, e)
+    dims = moe.MoeDims(h, i, e, k)
+    x = torch.ones((tokens, h), dtype=torch.bfloat16, device="cuda")
+    ids = torch.full((tokens, k), 2 ** 30, dtype=torch.int32, device="cuda")
+    canvas = torch.full((tokens + 2, h), 7.0, dtype=torch.bfloat16, device="cuda")
+    need = moe.moe_ffn_layer_w4_workspace(dims, tokens)
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    moe.moe_ffn_layer_w4(dims, tokens, x, ids, torch.ones((tokens, k), device="cuda"), *stack.packed, canvas[1:-1], status,
+                         ws[:need])
+    assert int(status.item()) == moe.MOE_DEV_BAD_EXPERT_ID
+    assert (canvas[0] == 7).all() and (canvas[-1] == 7).all() and (ws[need:] == 255).all()
+
+
 def test_rows_outside_the_offsets_stay(moe):
     """A step call with rows of some experts only: the others' rows of y are left as they were."""
     rng = np.random.default_rng(6)
