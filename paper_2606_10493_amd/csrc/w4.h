@@ -64,22 +64,29 @@ struct W4Slots {
   int32_t* dest_row;    // [slots]
 };
 
-// This workgroup's part of K, in blocks (it begins with the scales of 512 columns); a
-// part of several writes its sums as they are.
+// This workgroup's part of K, in blocks (a whole number of `unit`); a part of several
+// writes its sums as they are.
 struct W4Range {
   int b0, n;
 };
-__device__ __forceinline__ W4Range w4_part(W4Args& p, int part) {
+__device__ __forceinline__ W4Range w4_part(W4Args& p, int part, int unit) {
   const int nb = p.K / kBlock;
   if (p.splits <= 1) return W4Range{0, nb};
-  const uint32_t chunks = (nb + 3) / 4, each = chunks / p.splits, more = chunks - each * p.splits;
-  const int b0 = 4 * (part * each + min((uint32_t)part, more));
-  const int b1 = min(nb, b0 + 4 * (int)(each + ((uint32_t)part < more ? 1u : 0u)));
+  const uint32_t units = (nb + unit - 1) / unit, each = units / p.splits, more = units - each * p.splits;
+  const int b0 = unit * (part * each + min((uint32_t)part, more));
+  const int b1 = min(nb, b0 + unit * (int)(each + ((uint32_t)part < more ? 1u : 0u)));
   p.out32 = p.partial + (int64_t)part * p.x_rows * p.N;
   p.out_stride = p.N;
   p.bias = nullptr;
   return W4Range{b0, b1 - b0};
 }
+
+// How the product of one matrix is cut (see w4_gemm_cut).  Parts of K are at most 16 and
+// have at most 1024 rows of sums together, or one part.
+struct W4Cut {
+  int tile, parts;
+};
+inline int w4_most_parts(int64_t rows) { return rows > 512 ? 1 : (int)(rows <= 64 ? 16 : 1024 / rows); }
 
 // Four neighbouring outputs of a row.
 __device__ __forceinline__ void w4_store(const W4Args& p, int64_t row, int n, v4f v) {

@@ -7,13 +7,13 @@
 namespace moe {
 
 bool w4_few_fits(int32_t K);
-int w4_few_splits(int32_t K);
+int w4_few_parts(int32_t K);
 moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
 moe_status_t run_w4_few_slots(const W4Args& a, int rows, const W4Slots& slots, hipStream_t stream);
 bool w4_down_combine_fits(int32_t K, int slots);
 moe_status_t run_w4_down_combine(const moe_dims_t& d, int tokens, const uint16_t* h, const W4Slots& s, const uint8_t* w,
                                  const uint8_t* w_s, const float* topk_w, uint16_t* out, hipStream_t stream);
-int w4_gemm_splits(int64_t rows, int32_t K, int32_t N);
+W4Cut w4_gemm_cut(int64_t rows, int32_t K, int32_t N);
 moe_status_t run_w4_gemm(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream);
 
 namespace {
@@ -28,12 +28,8 @@ moe_status_t run_experts(const W4Args& a, bool gateup, int32_t T, int64_t rows, 
   return run_w4_gemm(a, gateup, rows, stream);
 }
 
-int linear_splits(int32_t T, int32_t K, int32_t N) { return T <= kFewRows ? w4_few_splits(K) : w4_gemm_splits(T, K, N); }
-
-size_t partial_bytes(int32_t T, int32_t K, int32_t N) {
-  const int splits = linear_splits(T, K, N);
-  return splits > 1 ? (size_t)splits * (size_t)T * (size_t)N * sizeof(float) : 0;
-}
+// One matrix: whether w4_few takes it.
+bool few_linear(int32_t T, int32_t K) { return T <= kFewRows && w4_few_parts(K) <= w4_most_parts(kFewRows); }
 
 // out = the parts' sums in their order (+ bias), four neighbouring outputs a lane.
 __global__ __launch_bounds__(256) void w4_join_kernel(W4Args p) {
@@ -50,7 +46,7 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Args p) {
 }
 
 moe_status_t run_linear(const W4Args& a, int32_t T, hipStream_t stream) {
-  const moe_status_t st = T <= kFewRows ? run_w4_few(a, false, T, stream) : run_w4_gemm(a, false, T, stream);
+  const moe_status_t st = few_linear(T, a.K) ? run_w4_few(a, false, T, stream) : run_w4_gemm(a, false, T, stream);
   if (st != MOE_OK || a.splits <= 1) return st;
   MOE_LAUNCH("w4_join", w4_join_kernel, dim3((unsigned)(((int64_t)a.N / 4 + 255) / 256), (unsigned)std::min(T, 1024)), dim3(256), 0,
              stream, a);
@@ -138,13 +134,12 @@ using namespace moe;
 
 extern "C" size_t moe_linear_w4_workspace(int32_t T, int32_t K, int32_t N) {
   if (T <= 0 || K <= 0 || N <= 0 || K % kBlock || N % 16) return 0;
-  // No smaller T needs more: the most rows of every number of parts count.
-  size_t need = partial_bytes(T, K, N);
-  const int32_t ends[] = {kFewRows, 32, 64};
-  for (const int32_t t : ends)
-    if (t < T) need = std::max(need, partial_bytes(t, K, N));
-  for (int32_t t = 128; t < T && t <= 128 * 256; t += 128) need = std::max(need, partial_bytes(t, K, N));
-  return align256(need);
+  // Sums of the parts of K.  No smaller T needs more.
+  if (few_linear(T, K)) {
+    const int parts = w4_few_parts(K);
+    return parts > 1 ? align256((size_t)parts * T * N * sizeof(float)) : 0;
+  }
+  return align256((size_t)std::min<int64_t>(16 * (int64_t)T, 1024) * N * sizeof(float));
 }
 
 extern "C" moe_status_t moe_linear_w4(const uint16_t* x, int64_t x_stride, int32_t T, int32_t K, const uint8_t* w,
@@ -169,7 +164,7 @@ extern "C" moe_status_t moe_linear_w4(const uint16_t* x, int64_t x_stride, int32
   a.out32 = out_type == MOE_F32 ? static_cast<float*>(out) : nullptr;
   a.out16 = out_type == MOE_F32 ? nullptr : static_cast<uint16_t*>(out);
   a.out_stride = out_stride;
-  a.splits = linear_splits(T, K, N);
+  a.splits = few_linear(T, K) ? w4_few_parts(K) : w4_gemm_cut(T, K, N).parts;
   a.partial = static_cast<float*>(ws);
   return run_linear(a, T, stream);
 }

@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
   const int nb = p.K / kBlock;
   const int groups = p.N / 16;
   const int items_n = (groups + kTiles - 1) / kTiles;
-  const W4Range range = w4_part(p, blockIdx.y);
+  const W4Range range = w4_part(p, blockIdx.y, 4);  // whole pieces of the scales' layout
   const int kb0 = range.b0 + wave * NBW, last = range.b0 + range.n - 1;
   const int64_t chunks = (nb + 3) / 4;
 
@@ -310,7 +310,7 @@ moe_status_t few_by_length(const W4Args& a, int rows, const W4Slots& slots, hipS
 bool w4_few_fits(int32_t K) { return K / kBlock <= kFewMaxBlocks; }
 
 // Parts of K of one matrix whose rows are longer than a workgroup holds.
-int w4_few_splits(int32_t K) { return w4_few_fits(K) ? 1 : (K / kBlock + 31) / 32; }
+int w4_few_parts(int32_t K) { return w4_few_fits(K) ? 1 : (K / kBlock + 31) / 32; }
 
 // Experts: at most kFewMaxRows rows.
 moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
