@@ -22,10 +22,16 @@ constexpr int kFewRows = 16;  // rows of one matrix that w4_few takes
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Experts.  Up to MOE_DECODE_MAX_TOKENS tokens most experts have a few rows, and all are bound by their weights.
-moe_status_t run_experts(const W4Args& a, bool gateup, int32_t T, int64_t rows, hipStream_t stream) {
-  if (T <= MOE_DECODE_MAX_TOKENS && w4_few_fits(a.K)) return run_w4_few(a, gateup, rows, stream);
-  return run_w4_gemm(a, gateup, rows, stream);
+// Experts with a few rows each, whose weights are many: w4_few streams them faster than the GEMM's smallest tiles (7168 x
+// 2048, 256 experts: 376 against 418 us a layer at 16 tokens, 777 against 842 at 64, 1002 against 1051 at 256), and slower
+// where an expert's run is short (2048 x 768, 128 experts: 76 against 64 us at 33 tokens; 4096 x 1536, 16 experts: 45
+// against 38 at 16).
+bool few_experts(const W4Args& a, int64_t rows) {
+  return (int64_t)a.N * a.K >= (1 << 23) && rows <= kFewMaxRows && rows <= 8 * (int64_t)a.E && w4_few_fits(a.K);
+}
+
+moe_status_t run_experts(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
+  return few_experts(a, rows) ? run_w4_few(a, gateup, rows, stream) : run_w4_gemm(a, gateup, rows, stream);
 }
 
 // One matrix: whether w4_few takes it.
@@ -92,14 +98,14 @@ moe_status_t expert_ffn_w4(const moe_dims_t& d, int32_t T, const uint16_t* x, co
   const int64_t rows = (int64_t)T * d.topk;
   W4Args g = gateup_args(d, T, x, w, h);
   g.sorted_src = src; g.offsets = offsets;
-  const moe_status_t st = run_experts(g, true, T, rows, stream);
+  const moe_status_t st = run_experts(g, true, rows, stream);
   if (st != MOE_OK) return st;
   W4Args dn{};
   dn.x = h; dn.x_stride = d.inter; dn.x_rows = rows;
   dn.offsets = offsets; dn.E = d.n_experts;
   dn.w0 = w[4]; dn.s0 = w[5];
   dn.N = d.hidden; dn.K = d.inter; dn.out32 = y; dn.out_stride = d.hidden;
-  return run_experts(dn, false, T, rows, stream);
+  return run_experts(dn, false, rows, stream);
 }
 
 struct W4LayerLayout {

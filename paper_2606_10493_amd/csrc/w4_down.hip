@@ -18,7 +18,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kDownWaves = 8;
 constexpr int kDownBlocks = 8;            // K blocks that are loaded together
-constexpr int kDownBytes = 64 * 1024;     // of LDS
+constexpr int kDownBytes = 80 * 1024;     // of LDS
 
 struct W4DownArgs {
   const uint16_t* h;    // bf16 [slots, K], sorted

@@ -31,7 +31,6 @@ constexpr int few_waves(int nbw) { return nbw <= 2 ? 16 : 12; }
 constexpr int kFewMaxWaves = 12;
 constexpr int kFewMaxBlocks = 60;  // K blocks: 12 waves of 5
 // Row tiles of experts: at most one an expert, and one for 16 rows.
-constexpr int kFewMaxRows = MOE_DECODE_MAX_TOKENS * 32;
 constexpr int few_tiles(int rows, int E) { return (rows < E ? rows : E) + rows / 16; }
 
 enum FewMode { kDense, kExperts, kExpertsGateUp, kSlotsGateUp };
@@ -315,7 +314,6 @@ int w4_few_parts(int32_t K) { return w4_few_fits(K) ? 1 : (K / kBlock + 31) / 32
 // Experts: at most kFewMaxRows rows.
 moe_status_t run_w4_few(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
   if (!a.offsets) return few_by_length<kDense>(a, (int)rows, W4Slots{}, stream);
-  if (rows > kFewMaxRows) return fail(MOE_ERR_UNSUPPORTED_SHAPE, "w4_few: %lld rows", (long long)rows);
   return gateup ? few_by_length<kExpertsGateUp>(a, (int)rows, W4Slots{}, stream)
                 : few_by_length<kExperts>(a, (int)rows, W4Slots{}, stream);
 }

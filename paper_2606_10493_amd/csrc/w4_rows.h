@@ -67,6 +67,8 @@ __device__ __forceinline__ int list_row_tiles(const int32_t* __restrict__ offset
   return min(before, most);
 }
 
+constexpr int kFewMaxRows = 2048;  // rows of all experts whose tiles w4_few lists in LDS
+
 constexpr int kSortSlots = 64;  // slots that a wave sorts by itself
 
 // The sort of moe_permute for up to 64 slots, one a lane, by one wave: src[p] = slot at
