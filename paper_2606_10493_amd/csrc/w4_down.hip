@@ -17,7 +17,8 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kDownWaves = 8;
-constexpr int kDownBlocks = 8;            // K blocks that are loaded together
+constexpr int kDownBlocks = 4;            // K blocks that are loaded together
+constexpr int kDownFirst = 2 * (kDownBlocks + kDownBlocks / 4);  // loads of a wave's first weights
 constexpr int kDownBytes = 80 * 1024;     // of LDS
 
 struct W4DownArgs {
@@ -30,18 +31,28 @@ struct W4DownArgs {
   uint16_t* out;        // bf16 [tokens, N]
 };
 
-constexpr int down_stride(int K) { return 2 * K + 16; }  // bytes of a row of h in LDS: rows begin on other banks
-constexpr int64_t down_bytes(int K, int slots) { return (int64_t)slots * (64 + down_stride(K)); }
+// LDS: the rows of h (whole loads of 1 KB; the 16-byte piece c of row i lies at c ^ i % 16, so that rows begin on other
+// banks), then y.
+constexpr int64_t down_h_bytes(int K, int slots) { return ((int64_t)slots * K * 2 + 1023) / 1024 * 1024; }
+constexpr int64_t down_bytes(int K, int slots) { return down_h_bytes(K, slots) + slots * 64; }
 
 __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4DownArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  float* y = reinterpret_cast<float*>(lds);  // [slots][16]
-  uint8_t* h = lds + p.slots * 64;
+  float* y = reinterpret_cast<float*>(lds + down_h_bytes(p.K, p.slots));  // [slots][16]
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, kq = lane >> 4;
   const int nb = p.K / kBlock, groups = p.N / 16, chunks = (nb + 3) / 4;
-  const int stride = down_stride(p.K);
+  // The rows of h go out first, so that they are there when the first weights are.
+  const int pieces = p.K / 8;
+  {
+    const int all = p.slots * pieces;
+    const uint32_t to = lds_address(lds);
+    for (int i = wave * 64; i < all; i += kDownWaves * 64) {
+      const int at = min(i + lane, all - 1), row = at / pieces;
+      async_load_1k(p.h + (int64_t)row * p.K + ((at - row * pieces) ^ (row & 15)) * 8, to + i * 16);
+    }
+  }
   // (both loads go out together)
   const int2 count = p.list[kSortSlots], own = p.list[wave];
   const int n = __builtin_amdgcn_readfirstlane(count.x);
@@ -61,13 +72,13 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
     wt = p.w + g * nb * kW4TileBytes + lane * 16;
     st = p.s + g * chunks * kW4ScaleTile + r * 16;
   };
-  auto load = [&](int b, Blocks& q) {  // blocks past the last are that one again, against zeros
-#pragma unroll
-    for (int u = 0; u < kDownBlocks; ++u)
-      q.w[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wt + (int64_t)min(b + u, nb - 1) * kW4TileBytes));
+  auto load = [&](int b, Blocks& q) {  // blocks past the last are that one again
 #pragma unroll
     for (int u = 0; u < kDownBlocks / 4; ++u)
       q.s[u] = *reinterpret_cast<const u32x4*>(st + min((b >> 2) + u, chunks - 1) * kW4ScaleTile);
+#pragma unroll
+    for (int u = 0; u < kDownBlocks; ++u)
+      q.w[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wt + (int64_t)min(b + u, nb - 1) * kW4TileBytes));
   };
   Blocks q0, q1;
   if (wave < n) {
@@ -75,13 +86,9 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
     load(0, q0);
     load(kDownBlocks, q1);
   }
-  // The slots' rows, 16 bytes a lane.
-  const int pieces = p.K / 8;
-  for (int i = threadIdx.x; i < p.slots * pieces; i += 64 * kDownWaves) {
-    const int row = i / pieces, c = i - row * pieces;
-    *reinterpret_cast<uint4*>(h + row * stride + c * 16) = *reinterpret_cast<const uint4*>(p.h + (int64_t)row * p.K + c * 8);
-  }
-  __syncthreads();
+  // A wave's loads of h are its oldest.
+  if (wave < n) wait_async_and_barrier<kDownFirst>();
+  else wait_async_and_barrier<0>();
 
   for (int a = wave; a < n; a += kDownWaves) {
     if (a != wave) {
@@ -89,17 +96,28 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
       load(0, q0);
       load(kDownBlocks, q1);
     }
-    const uint8_t* x = h + (p0 + min(r, m - 1)) * stride + 16 * kq;
-    v4f acc = v4f{0.f, 0.f, 0.f, 0.f};
+    const int row = p0 + min(r, m - 1);
+    const uint8_t* x = lds + row * (2 * p.K);
+    const int turn = row & 15;
+    v4f acc[2] = {v4f{0.f, 0.f, 0.f, 0.f}, v4f{0.f, 0.f, 0.f, 0.f}};  // of even and odd blocks
+    auto block = [&](int b, int u, const Blocks& q) {
+      w4_bf16x8 xu[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        xu[j] = __builtin_bit_cast(w4_bf16x8, *reinterpret_cast<const uint4*>(x + ((4 * j + kq) ^ turn) * 16 + (b + u) * (2 * kBlock)));
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        acc[u & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w4_expand(q.w[u][j], w4_scale(q.s[u / 4][u % 4], j)), xu[j], acc[u & 1],
+                                                             0, 0, 0);
+    };
     auto multiply = [&](int b, const Blocks& q) {
+      if (b + kDownBlocks <= nb) {  // (one basic block, whose reads of h run ahead of the products)
 #pragma unroll
-      for (int u = 0; u < kDownBlocks; ++u) {
-        if (b + u >= nb) break;
+        for (int u = 0; u < kDownBlocks; ++u) block(b, u, q);
+      } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              w4_expand(q.w[u][j], w4_scale(q.s[u / 4][u % 4], j)),
-              __builtin_bit_cast(w4_bf16x8, *reinterpret_cast<const uint4*>(x + (b + u) * (2 * kBlock) + 64 * j)), acc, 0, 0, 0);
+        for (int u = 0; u < kDownBlocks; ++u)
+          if (b + u < nb) block(b, u, q);
       }
     };
     for (int b = 0; b < nb; b += 2 * kDownBlocks) {
@@ -109,7 +127,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
       multiply(b + kDownBlocks, q1);
       if (b + 3 * kDownBlocks < nb) load(b + 3 * kDownBlocks, q1);
     }
-    if (r < m) *reinterpret_cast<v4f*>(y + (p0 + r) * 16 + 4 * kq) = acc;
+    if (r < m) *reinterpret_cast<v4f*>(y + (p0 + r) * 16 + 4 * kq) = acc[0] + acc[1];
   }
   __syncthreads();
   // Tokens' sums in slot order, products and sums rounded separately.
