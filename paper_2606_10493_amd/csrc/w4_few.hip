@@ -25,11 +25,10 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// Waves of a CU, so that NBW blocks of activations fit their registers; a workgroup
-// has up to 12, whose sums fit 64 KB of LDS beside the list of row tiles.
-constexpr int few_waves(int nbw) { return nbw <= 2 ? 16 : 12; }
-constexpr int kFewMaxWaves = 12;
-constexpr int kFewMaxBlocks = 60;  // K blocks: 12 waves of 5
+// Waves of a CU, so that NBW blocks of activations fit their registers.
+constexpr int few_waves(int nbw) { return nbw <= 2 ? 16 : nbw <= 4 ? 12 : 8; }
+constexpr int kFewMaxWaves = 8;    // of a workgroup
+constexpr int kFewMaxBlocks = 64;  // K blocks: 8 waves of 8
 // Row tiles of experts: at most one an expert, and one for 16 rows.
 constexpr int few_tiles(int rows, int E) { return (rows < E ? rows : E) + rows / 16; }
 
@@ -137,21 +136,16 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
     for (int u = 0; u < NBW; ++u)  // blocks past the last are that one again, against zeros
       q.w[t][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(w + min(kb0 + u, last) * kW4TileBytes + lane * 16));
     const uint8_t* s = s_base[mat] + g * chunks * kW4ScaleTile + r * 16;
-    if constexpr (NBW == 3 || NBW == 5) {  // blocks that begin anywhere
-#pragma unroll
-      for (int u = 0; u < NBW; ++u) {
-        const int b = min(kb0 + u, last);
-        q.s[t][u] = *reinterpret_cast<const uint32_t*>(s + (b >> 2) * kW4ScaleTile + (b & 3) * 4);
-      }
-      return;
-    }
     // (behind the last column's scales there is padding to be read, and a wave without blocks reads the last ones)
     const int sb = min(kb0, last) & ~(NBW - 1);
     s += (sb >> 2) * kW4ScaleTile + (sb & 3) * 4;
-    if constexpr (NBW == 4) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(s);
+    if constexpr (NBW >= 4) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) q.s[t][u] = v[u];
+      for (int c = 0; c < NBW / 4; ++c) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(s + (c ? min(c, (last >> 2) - (sb >> 2)) : 0) * kW4ScaleTile);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) q.s[t][4 * c + u] = v[u];
+      }
     } else if constexpr (NBW == 2) {
       const u32x2 v = *reinterpret_cast<const u32x2*>(s);
       q.s[t][0] = v[0];
@@ -174,8 +168,7 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
   int cg = lg;
   w4_bf16x8 x[NBW][4];
   auto load_x = [&]() {
-    // Rows past the tile's last read that one again: what a lane has for an activation row reaches that row's sums
-    // alone, which are not stored.
+    // Lanes without an activation row load nothing: the address path takes as long for a row that sixteen lanes share.
     int64_t row = ck.p0 + min(r, ck.m - 1);
     if constexpr (MODE == kSlotsGateUp) {
       row = one ? 0 : slot_src[row] / p.topk;
@@ -187,9 +180,14 @@ __global__ __launch_bounds__(64 * kFewMaxWaves, few_waves(NBW) / 4) void w4_few_
 #pragma unroll
     for (int u = 0; u < NBW; ++u)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[u][j] = __builtin_bit_cast(w4_bf16x8, *reinterpret_cast<const uint4*>(xr + min(kb0 + u, last) * kBlock + 32 * j));
-      }
+      for (int j = 0; j < 4; ++j) x[u][j] = __builtin_bit_cast(w4_bf16x8, make_uint4(0, 0, 0, 0));
+    if (r < ck.m) {
+#pragma unroll
+      for (int u = 0; u < NBW; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[u][j] = __builtin_bit_cast(w4_bf16x8, *reinterpret_cast<const uint4*>(xr + min(kb0 + u, last) * kBlock + 32 * j));
+    }
     if (kb0 + NBW - 1 > last) {  // the last wave
 #pragma unroll
       for (int u = 0; u < NBW; ++u)
@@ -293,15 +291,14 @@ moe_status_t launch_few(const W4Args& a, int rows, const W4Slots& slots, hipStre
   return check_launch(name);
 }
 
-// NBW: a wave's K blocks.  Fewer waves of more blocks each, and more workgroups of them a CU, wait less for one another.
+// NBW: a wave's K blocks.
 template <FewMode MODE>
 moe_status_t few_by_length(const W4Args& a, int rows, const W4Slots& slots, hipStream_t stream) {
   const int nb = few_blocks(a);
-  if (nb <= 8) return launch_few<1, 4, MODE>(a, rows, slots, stream);
-  if (nb <= 24) return launch_few<2, 2, MODE>(a, rows, slots, stream);
-  if (nb <= 36) return launch_few<3, 1, MODE>(a, rows, slots, stream);
-  if (nb <= 48) return launch_few<4, 1, MODE>(a, rows, slots, stream);
-  return launch_few<5, 1, MODE>(a, rows, slots, stream);
+  if (nb <= 4) return launch_few<1, 4, MODE>(a, rows, slots, stream);
+  if (nb <= 8) return launch_few<2, 2, MODE>(a, rows, slots, stream);
+  if (nb <= 32) return launch_few<4, 1, MODE>(a, rows, slots, stream);
+  return launch_few<8, 1, MODE>(a, rows, slots, stream);
 }
 
 }  // namespace
