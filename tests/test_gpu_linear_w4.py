@@ -101,7 +101,8 @@ def test_every_code_and_scale_expands_exactly(moe, tokens):
 
 
 TOKENS = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 257, 1000]
-SIZES = [(128, 16), (256, 48), (384, 256), (640, 272), (1024, 1536), (1152, 240), (7168, 512), (2048, 4112)]
+SIZES = [(128, 16), (256, 48), (384, 256), (640, 272), (1024, 1536), (1152, 240), (7168, 512), (2048, 4112), (4480, 96), (8320, 48),
+         (16384, 32), (5120, 1040)]
 
 
 @pytest.mark.parametrize("k,n", SIZES)
@@ -140,7 +141,7 @@ def test_ordinary_values(moe, tokens):
 
 def test_long_and_wide(moe):
     """K past 2^15 with few columns, and many columns with little K."""
-    for k, n, t in ((40960, 32, 3), (40960, 32, 70), (128, 70000, 2), (128, 70000, 66)):
+    for k, n, t in ((40960, 32, 3), (40960, 32, 70), (75776, 16, 2), (75776, 16, 16), (128, 70000, 2), (128, 70000, 66)):
         rng = np.random.default_rng(k)
         q, s = whole(rng, n, k)
         w, ws = packed(moe, q, s)
