@@ -129,7 +129,7 @@ __device__ __forceinline__ void w4_gemm_wave(const uint8_t* smem, int nb, int x_
 // Rows of one expert, or of the one matrix, are cut into the fewest tiles of at most
 // 32 S rows, equal ones but for the rounding to parts of 16.
 template <int S, int H, bool GATEUP>
-__global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int64_t rows, int n_tiles) {
+__global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int64_t rows, int n_tiles, int dealt) {
   constexpr int kXStage = 32 * S * 2 * kBlock;
   constexpr int kStage = gemm_stage(S), kStages = gemm_stages(S);
   constexpr int kXLoads = S;                      // a wave's a step: 8 S KB in all
@@ -141,20 +141,24 @@ __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int6
   const int half = H == 2 ? wave >> 2 : 0, share = H == 2 ? wave & 3 : wave;  // of the activation rows, of the weight rows
   const int r = lane & 15, kq = lane >> 4;
   const int nb = p.K / kBlock, groups = p.N / 16;
-  const int nt = (int)(blockIdx.x % n_tiles);
+  // Workgroups are dealt to the XCDs in turn.  Row tiles too, where there are enough of them: an XCD takes all of a row
+  // tile's items one after the other, and its L2 holds the activations.
+  const uint32_t x = dealt ? blockIdx.x / kXcd : blockIdx.x;
+  const int turn = (int)(x / (uint32_t)n_tiles), nt = (int)(x - (uint32_t)turn * n_tiles);
+  const int mt = dealt ? turn * kXcd + (int)(blockIdx.x % kXcd) : turn;
   const W4Range range = w4_part(p, blockIdx.y, 1);
 
   int e = 0, mc;
   int64_t p0;
   if (p.offsets) {
-    const ExpertRows ref = find_even_tile(p.offsets, p.E, (int)(blockIdx.x / n_tiles), 32 * S, (int)rows);
+    const ExpertRows ref = find_even_tile(p.offsets, p.E, mt, 32 * S, (int)rows);
     if (ref.e < 0) return;  // the whole workgroup
     e = ref.e;
     p0 = ref.p0;
     mc = ref.m;
   } else {
     const int64_t tiles = (rows + 32 * S - 1) / (32 * S), part = even_tile_rows(rows, tiles);
-    p0 = (int64_t)(blockIdx.x / n_tiles) * part;
+    p0 = (int64_t)mt * part;
     if (p0 >= rows) return;
     mc = (int)min(part, rows - p0);
   }
@@ -235,10 +239,12 @@ moe_status_t launch_gemm(const W4Args& a, int64_t rows, hipStream_t stream) {
   const int cols = GATEUP ? kGemmRows / 2 : kGemmRows;
   const int n_tiles = (a.N + cols - 1) / cols;
   const int64_t m_tiles = a.offsets ? rows / (32 * S) + (rows < a.E ? rows : (int64_t)a.E) : (rows + 32 * S - 1) / (32 * S);
-  if (m_tiles * n_tiles * std::max(1, a.splits) > w4_max_blocks(64 * kGemmWaves))
+  const bool dealt = m_tiles >= 4 * kXcd;
+  const int64_t blocks = (dealt ? (m_tiles + kXcd - 1) / kXcd * kXcd : m_tiles) * n_tiles;
+  if (blocks * std::max(1, a.splits) > w4_max_blocks(64 * kGemmWaves))
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "%s: too many rows and columns", name);
-  MOE_LAUNCH(name, (w4_gemm_kernel<S, H, GATEUP>), dim3((unsigned)(m_tiles * n_tiles), std::max(1, a.splits)),
-             dim3(64 * kGemmWaves), 0, stream, a, rows, n_tiles);
+  MOE_LAUNCH(name, (w4_gemm_kernel<S, H, GATEUP>), dim3((unsigned)blocks, std::max(1, a.splits)), dim3(64 * kGemmWaves), 0,
+             stream, a, rows, n_tiles, (int)dealt);
   return check_launch(name);
 }
 
