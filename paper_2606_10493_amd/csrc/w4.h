@@ -84,7 +84,7 @@ __device__ __forceinline__ W4Range w4_part(W4Args& p, int part, int unit) {
 // How the product of one matrix is cut (see w4_gemm_cut).  Parts of K are at most 16 and
 // have at most 1024 rows of sums together, or one part.
 struct W4Cut {
-  int tile, parts;
+  int S, tiles, parts;  // tiles of 32 S activation rows by 128 tiles weight rows, parts of K
 };
 inline int w4_most_parts(int64_t rows) { return rows > 512 ? 1 : (int)(rows <= 64 ? 16 : 1024 / rows); }
 

@@ -1,22 +1,21 @@
 // Products of many rows with 4-bit weights: an LDS-tiled bf16 GEMM that expands
 // the weights in registers on their way from LDS to the matrix instruction.
 //
-// A workgroup takes a tile of up to 32 S activation rows against 256 weight rows
-// (GATEUP: 128 of W_gate and the same 128 of W_up).  Its eight waves, two to a SIMD,
-// share them: with H = 2 they are two halves of the activation rows by four quarters of
-// the weight rows, a wave expanding 64 weight rows for up to 16 S activation rows; with
-// H = 1, for small tiles, where the expansion is what counts, each has 32 weight rows
-// and all activation rows, and nothing is expanded twice.  How many 16-row parts of
-// activations a wave has is known when the tile is, and each number has its own loop,
-// so that an expert's rows are cut into equal tiles whose size follows them.
+// A workgroup takes a tile of up to 32 S activation rows against 128 TILES weight rows
+// (GATEUP: 64 TILES of W_gate and the same rows of W_up).  Each of its eight waves, two to a
+// SIMD, has 16 TILES weight rows and all activation rows, so that nothing is expanded
+// twice and the expansion of one wave of a SIMD runs beside the products of the
+// other.  How many 16-row parts the activation tile has is known when it is found, and
+// each number has its own loop, so that an expert's rows are cut into equal tiles whose
+// size follows them.
 //
 // Steps of 128 K.  Activations (256 bytes a row), codes (1 KB a tile of 16 rows) and
 // scales (one dword a row) go straight from global memory into LDS stages, one or
 // two steps ahead, with one barrier a step; activation rows are gathered on the
 // way.  The 16-byte piece c of an activation row lies at position c ^ row % 16, so
 // that a quarter wave's reads fill all banks.  A step's barrier stands before the last
-// quarter of the step in front of it, whose operands are in registers by then: the next
-// codes are read and expanded beside those products.
+// products of the step in front of it, whose operands are in registers by then: the next
+// codes are read and expanded beside them.
 #include <algorithm>
 #include <type_traits>
 
@@ -28,11 +27,18 @@ namespace moe {
 namespace {
 
 constexpr int kGemmWaves = 8;
-constexpr int kGemmRows = 256;                         // weight rows of a workgroup
-constexpr int kGemmCodes = kGemmRows / 16 * kW4TileBytes;  // of a stage
-constexpr int kGemmScales = kGemmWaves * 256;          // 64 rows' for each wave
-constexpr int gemm_stage(int s) { return 32 * s * 2 * kBlock + kGemmCodes + kGemmScales; }
-constexpr int gemm_stages(int s) { return 3 * gemm_stage(s) <= 160 * 1024 ? 3 : 2; }
+constexpr int kGemmScales = kGemmWaves * 256;  // of a stage: up to 64 rows' for each wave
+constexpr int gemm_rows(int tiles) { return kGemmWaves * tiles * 16; }  // weight rows of a workgroup
+constexpr int gemm_stage(int s, int tiles) { return 32 * s * 2 * kBlock + kGemmWaves * tiles * kW4TileBytes + kGemmScales; }
+constexpr int gemm_stages(int s, int tiles) { return 3 * gemm_stage(s, tiles) <= 160 * 1024 ? 3 : 2; }
+
+// async_load_1k of base + offset (base uniform, offset the lane's).
+__device__ __forceinline__ void async_load_1k_at(const void* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(base)
+               : "memory");
+}
 
 // async_load_1k's counterpart for 4 bytes a lane.
 __device__ __forceinline__ void async_load_256(const void* src, uint32_t lds) {
@@ -47,7 +53,7 @@ __device__ __forceinline__ void async_load_256(const void* src, uint32_t lds) {
 // x_at, w_at and s_at are the wave's first activation part, its codes and its scales
 // in stage 0.
 template <int CNT, int TILES, int STAGES, int STAGE_BYTES, int LOADS, typename Load, typename Store>
-__device__ __forceinline__ void w4_gemm_wave(const uint8_t* smem, int nb, int x_at, int w_at, int s_at, Load load, Store store) {
+__device__ __forceinline__ void w4_gemm_wave(const uint8_t* smem, int nb, int w_at, int s_at, Load load, Store store) {
   const int lane = threadIdx.x & 63;
   const int r = lane & 15, kq = lane >> 4;
   v4f acc[TILES][CNT];
@@ -73,7 +79,7 @@ __device__ __forceinline__ void w4_gemm_wave(const uint8_t* smem, int nb, int x_
   };
   auto read_x = [&](const uint8_t* at, int j, int c) {
     return __builtin_bit_cast(
-        w4_bf16x8, *reinterpret_cast<const uint4*>(at + x_at + (c * 16 + r) * (2 * kBlock) + (((4 * j + kq) ^ r) * 16)));
+        w4_bf16x8, *reinterpret_cast<const uint4*>(at + (c * 16 + r) * (2 * kBlock) + (((4 * j + kq) ^ r) * 16)));
   };
 #pragma unroll
   for (int s = 0; s < STAGES; ++s) load(s, s);
@@ -85,32 +91,34 @@ __device__ __forceinline__ void w4_gemm_wave(const uint8_t* smem, int nb, int x_
   for (int b = 0; b < nb; ++b) {
     const uint8_t* at = smem + stage * STAGE_BYTES;
     const int next = stage + 1 == STAGES ? 0 : stage + 1;
-    w4_bf16x8 x3[CNT];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (j < 3) {
+      constexpr int kLate = CNT * TILES <= 24 ? CNT : CNT <= 8 ? 3 : 2;  // parts whose last operands are read in front of the barrier
+      const int now = j == 3 ? CNT - kLate : CNT;
 #pragma unroll
-        for (int c = 0; c < CNT; ++c) {
-          const w4_bf16x8 x = read_x(at, j, c);
+      for (int c = 0; c < CNT; ++c) {
+        if (c >= now) break;
+        const w4_bf16x8 x = read_x(at, j, c);
 #pragma unroll
-          for (int t = 0; t < TILES; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j & 1][t], x, acc[t][c], 0, 0, 0);
-        }
-        expand(j + 1, w[(j + 1) & 1]);
-        if (j == 2) {
-#pragma unroll
-          for (int c = 0; c < CNT; ++c) x3[c] = read_x(at, 3, c);
-        }
-      } else {
-        // Step b + 1 has landed for every wave, and every wave has read all of step b, whose stage is loaded next.
-        wait_async_and_barrier<(STAGES - 2) * LOADS>();
-        read_codes(smem + next * STAGE_BYTES);
-        load(b + STAGES, stage);
-#pragma unroll
-        for (int c = 0; c < CNT; ++c)
-#pragma unroll
-          for (int t = 0; t < TILES; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[1][t], x3[c], acc[t][c], 0, 0, 0);
-        expand(0, w[0]);
+        for (int t = 0; t < TILES; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j & 1][t], x, acc[t][c], 0, 0, 0);
       }
+      if (j < 3) {
+        expand(j + 1, w[(j + 1) & 1]);
+        continue;
+      }
+      w4_bf16x8 late[kLate];
+#pragma unroll
+      for (int c = 0; c < kLate; ++c) late[c] = read_x(at, 3, now + c);
+      // Step b + 1 has landed for every wave, and every wave has read all of step b, whose stage is loaded next.
+      wait_async_and_barrier<(STAGES - 2) * LOADS>();
+      read_codes(smem + next * STAGE_BYTES);
+      load(b + STAGES, stage);
+#pragma unroll
+      for (int c = 0; c < kLate; ++c)
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+          acc[t][now + c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[1][t], late[c], acc[t][now + c], 0, 0, 0);
+      expand(0, w[0]);
     }
     stage = next;
   }
@@ -128,17 +136,15 @@ __device__ __forceinline__ void w4_gemm_wave(const uint8_t* smem, int nb, int x_
 
 // Rows of one expert, or of the one matrix, are cut into the fewest tiles of at most
 // 32 S rows, equal ones but for the rounding to parts of 16.
-template <int S, int H, bool GATEUP>
+template <int S, int TILES, bool GATEUP>
 __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int64_t rows, int n_tiles, int dealt) {
   constexpr int kXStage = 32 * S * 2 * kBlock;
-  constexpr int kStage = gemm_stage(S), kStages = gemm_stages(S);
+  constexpr int kStage = gemm_stage(S, TILES), kStages = gemm_stages(S, TILES);
+  constexpr int kRows = gemm_rows(TILES);
   constexpr int kXLoads = S;                      // a wave's a step: 8 S KB in all
-  constexpr int kWLoads = kGemmCodes / 1024 / kGemmWaves;
-  constexpr int kTiles = 2 * H;                   // 16-row weight tiles of a wave
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * kStage];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int half = H == 2 ? wave >> 2 : 0, share = H == 2 ? wave & 3 : wave;  // of the activation rows, of the weight rows
   const int r = lane & 15, kq = lane >> 4;
   const int nb = p.K / kBlock, groups = p.N / 16;
   // Workgroups are dealt to the XCDs in turn.  Row tiles too, where there are enough of them: an XCD takes all of a row
@@ -163,8 +169,6 @@ __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int6
     mc = (int)min(part, rows - p0);
   }
   const int parts = (mc + 15) / 16;
-  const int first = half ? (parts + 1) / 2 : 0, count = H == 1 ? parts : half ? parts / 2 : (parts + 1) / 2;
-
   // Sources.  Load i of the activations takes rows 32 i + 4 wave + lane / 16.
   const uint16_t* xs[kXLoads];
 #pragma unroll
@@ -177,23 +181,20 @@ __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int6
     }
     xs[i] = p.x + row * p.x_stride + (((lane & 15) ^ (m & 15)) * 8);
   }
-  // Tile t of a share: 16-row group group(t) of its matrix (groups past the last are that one again).
+  // Tile t of the wave: 16-row group group(t) of its matrix (groups past the last are that one again).
   auto group = [&](int t) {
-    if (GATEUP) return nt * (kGemmRows / 32) + share * H + t % H;
-    return nt * (kGemmRows / 16) + share * kTiles + t;
+    if (GATEUP) return nt * (kRows / 32) + wave * (TILES / 2) + t % (TILES / 2);
+    return nt * (kRows / 16) + wave * TILES + t;
   };
-  auto up = [&](int t) { return GATEUP && t >= H; };
+  auto up = [&](int t) { return GATEUP && t >= TILES / 2; };
   auto held = [&](int t) { return (int64_t)e * groups + min(group(t), groups - 1); };
-  const uint8_t* ws[kWLoads];  // this wave's part of its share's tiles
+  const uint8_t* ws[TILES];
 #pragma unroll
-  for (int i = 0; i < kWLoads; ++i) {
-    const int t = half * kWLoads + i;
-    ws[i] = (up(t) ? p.w1 : p.w0) + held(t) * nb * kW4TileBytes + lane * 16;
-  }
-  const int st = (lane >> 4) % kTiles;  // lane 16 t + r: row r of tile t
+  for (int t = 0; t < TILES; ++t) ws[t] = (up(t) ? p.w1 : p.w0) + held(t) * nb * kW4TileBytes;
+  const int st = (lane >> 4) % TILES;  // lane 16 t + r: row r of tile t
   const uint8_t* ss = (up(st) ? p.s1 : p.s0) + held(st) * ((nb + 3) / 4) * kW4ScaleTile + r * 16;
-  const int w_at = kXStage + share * kTiles * kW4TileBytes;
-  const int s_at = kXStage + kGemmCodes + wave * 256;
+  const int w_at = kXStage + wave * TILES * kW4TileBytes;
+  const int s_at = kXStage + kGemmWaves * TILES * kW4TileBytes + wave * 256;
   const uint32_t lds0 = lds_address(smem);
   // Steps past the end load the last one again, so that every step issues the same loads.
   auto load = [&](int step, int stage) {
@@ -202,88 +203,100 @@ __global__ __launch_bounds__(64 * kGemmWaves) void w4_gemm_kernel(W4Args p, int6
 #pragma unroll
     for (int i = 0; i < kXLoads; ++i) async_load_1k(xs[i] + (int64_t)b * kBlock, to + (i * kGemmWaves + wave) * 1024);
 #pragma unroll
-    for (int i = 0; i < kWLoads; ++i)
-      async_load_1k(ws[i] + (int64_t)b * kW4TileBytes, to + w_at + (half * kWLoads + i) * kW4TileBytes);
+    for (int t = 0; t < TILES; ++t) async_load_1k_at(ws[t] + (int64_t)b * kW4TileBytes, lane * 16, to + w_at + t * kW4TileBytes);
     async_load_256(ss + (b >> 2) * kW4ScaleTile + (b & 3) * 4, to + s_at);
   };
-  auto store = [&](int c, v4f (&v)[kTiles]) {
-    const int m = (first + c) * 16 + r;
+  auto store = [&](int c, v4f (&v)[TILES]) {
+    const int m = c * 16 + r;
     if (m >= mc) return;
 #pragma unroll
-    for (int t = 0; t < (GATEUP ? H : kTiles); ++t) {
+    for (int t = 0; t < (GATEUP ? TILES / 2 : TILES); ++t) {
       if (GATEUP) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[t][i] = silu_mul_fast(v[t][i], v[t + H][i]);
+        for (int i = 0; i < 4; ++i) v[t][i] = silu_mul_fast(v[t][i], v[t + TILES / 2][i]);
       }
       if (group(t) < groups) w4_store(p, p0 + m, group(t) * 16 + 4 * kq, v[t]);
     }
   };
-  // A half without rows goes along with one part, of which it stores nothing.
-  const int x_at = first * 16 * 2 * kBlock;
-  constexpr int kMost = 2 * S / H;
+  // The loop for this number of parts.
   auto with = [&](auto parts_of) {
-    constexpr int kCnt = decltype(parts_of)::value;
-    w4_gemm_wave<kCnt, kTiles, kStages, kStage, kXLoads + kWLoads + 1>(smem, range.n, x_at, w_at, s_at, load, store);
+    w4_gemm_wave<decltype(parts_of)::value, TILES, kStages, kStage, kXLoads + TILES + 1>(smem, range.n, w_at, s_at, load, store);
   };
-  if (kMost >= 5 && count == 5) with(std::integral_constant<int, kMost >= 5 ? 5 : 1>{});
-  else if (kMost >= 4 && count == 4) with(std::integral_constant<int, kMost >= 4 ? 4 : 1>{});
-  else if (kMost >= 3 && count == 3) with(std::integral_constant<int, kMost >= 3 ? 3 : 1>{});
-  else if (kMost >= 2 && count == 2) with(std::integral_constant<int, kMost >= 2 ? 2 : 1>{});
-  else with(std::integral_constant<int, 1>{});
+  auto choose = [&](auto self, auto n) {
+    constexpr int kN = decltype(n)::value;
+    if constexpr (kN == 1) {
+      with(n);
+    } else {
+      if (parts == kN) with(n);
+      else self(self, std::integral_constant<int, kN - 1>{});
+    }
+  };
+  choose(choose, std::integral_constant<int, 2 * S>{});
 }
 
-template <int S, bool GATEUP>
+template <int S, int TILES, bool GATEUP>
 moe_status_t launch_gemm(const W4Args& a, int64_t rows, hipStream_t stream) {
-  constexpr int H = S <= 2 ? 1 : 2;
   const char* name = GATEUP ? "w4_gemm_gateup" : "w4_gemm";
-  const int cols = GATEUP ? kGemmRows / 2 : kGemmRows;
+  const int cols = gemm_rows(TILES) / (GATEUP ? 2 : 1);
   const int n_tiles = (a.N + cols - 1) / cols;
   const int64_t m_tiles = a.offsets ? rows / (32 * S) + (rows < a.E ? rows : (int64_t)a.E) : (rows + 32 * S - 1) / (32 * S);
   const bool dealt = m_tiles >= 4 * kXcd;
   const int64_t blocks = (dealt ? (m_tiles + kXcd - 1) / kXcd * kXcd : m_tiles) * n_tiles;
   if (blocks * std::max(1, a.splits) > w4_max_blocks(64 * kGemmWaves))
     return fail(MOE_ERR_UNSUPPORTED_SHAPE, "%s: too many rows and columns", name);
-  MOE_LAUNCH(name, (w4_gemm_kernel<S, H, GATEUP>), dim3((unsigned)blocks, std::max(1, a.splits)), dim3(64 * kGemmWaves), 0,
+  MOE_LAUNCH(name, (w4_gemm_kernel<S, TILES, GATEUP>), dim3((unsigned)blocks, std::max(1, a.splits)), dim3(64 * kGemmWaves), 0,
              stream, a, rows, n_tiles, (int)dealt);
   return check_launch(name);
 }
 
 template <bool GATEUP>
 moe_status_t gemm_by_rows(const W4Args& a, int64_t rows, hipStream_t stream) {
-  // By the rows that an expert has on average: most experts in one tile, few of its parts empty.  (7168 x 2048, 256
-  // experts, us a layer with S = 1 .. 5: 16 rows 1134 1162 1322 1377 1827, 48 rows 1860 1645 1702 1737 1998, 64 rows
-  // 2210 2051 1893 1922 2153, 94 rows 2870 2779 2593 2369 2500, 128 rows 3700 3562 3508 3246 3008.)
+  // S by the rows that an expert has on average: most experts in one tile, few of its parts empty.  Wide tiles read the
+  // activations half as often, where the weights fill them and there are enough of them.  (7168 x 2048, 256 experts, us
+  // a layer with S = 1 .. 5, TILES = 2: 32 rows 1473 1344 1362 1418 1846, 64 rows 2307 2087 1873 1902 2111, 128 rows 4203
+  // 3582 3619 3305 3053; TILES = 4: 32 rows 1456 1226 1346 1347 1387, 64 rows 2302 1898 1706 1719 1719, 128 rows 4151
+  // 3211 3251 2929 2786, 256 rows 7775 5996 5552 5366 5300.)
   const int64_t mean = rows / a.E;
-  if (mean <= 24) return launch_gemm<1, GATEUP>(a, rows, stream);
-  if (mean <= 52) return launch_gemm<2, GATEUP>(a, rows, stream);
-  if (mean <= 76) return launch_gemm<3, GATEUP>(a, rows, stream);
-  if (mean <= 112) return launch_gemm<4, GATEUP>(a, rows, stream);
-  return launch_gemm<5, GATEUP>(a, rows, stream);
+  const int cols = gemm_rows(4) / (GATEUP ? 2 : 1), n_tiles = (a.N + cols - 1) / cols;
+  const bool wide = (int64_t)n_tiles * cols * 7 <= (int64_t)a.N * 8 && std::min<int64_t>(rows, a.E) * n_tiles >= 256;
+  if (wide && mean > 12) {
+    if (mean <= 52) return launch_gemm<2, 4, GATEUP>(a, rows, stream);
+    if (mean <= 72) return launch_gemm<3, 4, GATEUP>(a, rows, stream);
+    if (mean <= 104) return launch_gemm<4, 4, GATEUP>(a, rows, stream);
+    return launch_gemm<5, 4, GATEUP>(a, rows, stream);
+  }
+  if (mean <= 24) return launch_gemm<1, 2, GATEUP>(a, rows, stream);
+  if (mean <= 52) return launch_gemm<2, 2, GATEUP>(a, rows, stream);
+  if (mean <= 76) return launch_gemm<3, 2, GATEUP>(a, rows, stream);
+  if (mean <= 112) return launch_gemm<4, 2, GATEUP>(a, rows, stream);
+  return launch_gemm<5, 2, GATEUP>(a, rows, stream);
 }
 
 }  // namespace
 
-// How one matrix is cut: S of the tiles, and parts of K that a join adds up.  Taken by
-// the time that each cut is expected to need, in us: rounds of 256 workgroups, each
-// 4 and its steps (a step of 0.15 + 0.16 for every 16 rows, not less than 0.47:
-// 20.6 us for 168 workgroups of 32 steps and 32 rows, 80 for 256 of 14 steps ... of 128
-// rows), and for several parts a launch and their sums' way through memory.  Measured over 17 to 2048
-// rows of 4096 x 6144, 7168 x 4096 and 2048 x 7168 it takes the fastest cut or one within 8 % of it.
+// How one matrix is cut, by the time that each cut is expected to need, in us: rounds of
+// 256 workgroups, each 4 and its steps, a step 0.15 and 0.0115 an activation row with
+// narrow tiles, 0.3 and 0.019 with wide ones; and for several parts of K a launch and their sums' way through
+// memory.  (20.3 us for 168 workgroups of 32 steps of 29 rows, 53.5 for 192 of 32 of 128; wide, 92.5 for
+// 192 of 32 of 128 rows and 338 for 512 of 56.)
 W4Cut w4_gemm_cut(int64_t rows, int32_t K, int32_t N) {
-  const int64_t n_tiles = ((int64_t)N + kGemmRows - 1) / kGemmRows;
   const int nb = K / kBlock;
-  W4Cut best{4, 1};
+  constexpr struct {
+    int S, tiles;
+    double step, row;
+  } kKinds[] = {{1, 2, 0.15, 0.0115}, {2, 2, 0.15, 0.0115}, {4, 2, 0.15, 0.0115}, {3, 4, 0.3, 0.019}, {4, 4, 0.3, 0.019}, {5, 4, 0.3, 0.019}};
+  W4Cut best{4, 2, 1};
   double best_us = 1e30;
-  for (const int S : {1, 2, 4}) {
-    const int64_t m_tiles = (rows + 32 * S - 1) / (32 * S);
-    const double step = std::max(0.47, 0.15 + 0.01 * (double)even_tile_rows(rows, m_tiles));
+  for (const auto& k : kKinds) {
+    const int64_t m_tiles = (rows + 32 * k.S - 1) / (32 * k.S), n_tiles = ((int64_t)N + gemm_rows(k.tiles) - 1) / gemm_rows(k.tiles);
+    const double step = k.step + k.row * (double)even_tile_rows(rows, m_tiles);
     for (int parts = 1; parts <= w4_most_parts(rows) && parts * 3 <= std::max(nb, 3); ++parts) {
       const double rounds = (double)((m_tiles * n_tiles * parts + 255) / 256);
       const double us = rounds * (4.0 + (nb + parts - 1) / parts * step) +
                         (parts > 1 ? 4.0 + 8e-6 / 4.5 * (double)(parts * rows * N) : 0.0);
       if (us < best_us) {
         best_us = us;
-        best = W4Cut{S, parts};
+        best = W4Cut{k.S, k.tiles, parts};
       }
     }
   }
@@ -292,10 +305,14 @@ W4Cut w4_gemm_cut(int64_t rows, int32_t K, int32_t N) {
 
 moe_status_t run_w4_gemm(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
   if (a.offsets) return gateup ? gemm_by_rows<true>(a, rows, stream) : gemm_by_rows<false>(a, rows, stream);
-  switch (w4_gemm_cut(rows, a.K, a.N).tile) {
-    case 1: return launch_gemm<1, false>(a, rows, stream);
-    case 2: return launch_gemm<2, false>(a, rows, stream);
-    default: return launch_gemm<4, false>(a, rows, stream);
+  const W4Cut cut = w4_gemm_cut(rows, a.K, a.N);
+  switch (10 * cut.tiles + cut.S) {
+    case 21: return launch_gemm<1, 2, false>(a, rows, stream);
+    case 22: return launch_gemm<2, 2, false>(a, rows, stream);
+    case 24: return launch_gemm<4, 2, false>(a, rows, stream);
+    case 43: return launch_gemm<3, 4, false>(a, rows, stream);
+    case 44: return launch_gemm<4, 4, false>(a, rows, stream);
+    default: return launch_gemm<5, 4, false>(a, rows, stream);
   }
 }
 

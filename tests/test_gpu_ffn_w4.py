@@ -72,7 +72,8 @@ CASES = [  # hidden, inter, experts, k, tokens, skew
     (128, 128, 1, 1, 1, 0.0), (256, 128, 8, 2, 16, 0.0), (384, 256, 5, 3, 1, 0.0), (256, 128, 8, 8, 7, 0.0),
     (512, 384, 16, 2, 33, 0.5), (256, 256, 300, 4, 17, 0.0), (640, 128, 4, 1, 64, 2.0), (256, 128, 3, 2, 63, 0.0),
     (256, 2048, 8, 8, 2, 0.0), (2048, 4096, 5, 2, 20, 0.3), (7168, 1280, 3, 1, 18, 0.5), (4096, 2176, 2, 2, 7, 0.0),
-    (256, 128, 8, 2, 65, 0.0), (512, 256, 16, 4, 100, 0.6), (384, 384, 4, 2, 130, 3.0), (256, 128, 1024, 8, 200, 0.0),
+    (512, 256, 256, 8, 640, 0.0), (512, 256, 256, 8, 1920, 0.002), (512, 256, 256, 8, 2880, 0.0), (512, 256, 256, 8, 4480, 0.001),
+    (512, 384, 8, 2, 250, 0.0), (512, 384, 8, 2, 400, 0.0), (256, 128, 8, 2, 65, 0.0), (512, 256, 16, 4, 100, 0.6), (384, 384, 4, 2, 130, 3.0), (256, 128, 1024, 8, 200, 0.0),
     (256, 128, 2, 1, 513, 1.5), (1280, 640, 6, 2, 257, 0.0), (256, 128, 1, 1, 1000, 0.0)]
 
 

@@ -139,6 +139,16 @@ def test_ordinary_values(moe, tokens):
     assert ((out - ref).abs() <= k * 2.0 ** -23 * (size + bias.double().abs()) + 2.0 ** -8 * ref.abs()).all()
 
 
+@pytest.mark.parametrize("tokens,k,n", [(1500, 384, 2064), (2100, 256, 4112), (8200, 256, 1040), (4097, 640, 2560),
+                                        (8191, 384, 4096), (6200, 128, 8208), (12290, 256, 2048)])
+def test_many_tokens_bit_for_bit(moe, tokens, k, n):
+    rng = np.random.default_rng(tokens)
+    q, s = whole(rng, n, k)
+    w, ws = packed(moe, q, s)
+    x = torch.from_numpy(rng.integers(-4, 5, (tokens, k)).astype(np.float32)).bfloat16().cuda()
+    assert torch.equal(times(moe, x, w, ws, n, x_stride=k + 16).double(), x.double() @ values(q, s).t())
+
+
 def test_long_and_wide(moe):
     """K past 2^15 with few columns, and many columns with little K."""
     for k, n, t in ((40960, 32, 3), (40960, 32, 70), (75776, 16, 2), (75776, 16, 16), (128, 70000, 2), (128, 70000, 66)):
