@@ -1,10 +1,11 @@
 """One decoder layer, attention and routed experts, over a prompt and then token by token.
 
-    python examples/decoder_layer.py [--tokens 300] [--steps 8]
+    python examples/decoder_layer.py [--tokens 300] [--steps 8] [--weights4]
 
 A batch of prompts that begin with the same system prompt: the shared prefix is computed and cached once (its pages
 belong to all), each prompt's own part attends to prefix and itself, and every step's new tokens attend to the cache.
-Weights are random; the projections and norms are torch's, everything else runs in the library's kernels.
+Weights are random.  Everything runs in the library's kernels but the projections, which are torch's; with --weights4
+projections and experts have 4-bit weights, and those run there too.
 """
 import argparse
 import math
@@ -23,44 +24,75 @@ PAGE, POSITIONS = 64, 4096
 SCALE = 1.0 / math.sqrt(DIMS.head_dim)
 
 
+def packed8(w):
+    """fp32 matrices [n, rows, cols] -> e4m3 codes and scales, packed."""
+    q = torch.empty(w.shape, dtype=torch.uint8, device="cuda")
+    s = torch.empty((w.shape[0], w.shape[1] // 128, w.shape[2] // 128), device="cuda")
+    moe.moe_quant_weight(w, q, s)
+    packed = torch.empty_like(q)
+    moe.moe_pack_weight(q, packed)
+    return packed, s
+
+
+def packed4(w):
+    """fp32 matrices [.., rows, cols] -> 4-bit codes and scales, packed."""
+    q = torch.empty((*w.shape[:-1], w.shape[-1] // 2), dtype=torch.uint8, device="cuda")
+    s = torch.empty((*w.shape[:-1], w.shape[-1] // moe.MOE_W4_GROUP), dtype=torch.uint8, device="cuda")
+    moe.moe_quant_weight_w4(w, q, s)
+    packed = torch.empty_like(q)
+    mats = w.shape[0] if w.dim() == 3 else 1
+    packed_s = torch.empty(moe.moe_w4_scale_bytes(mats, *w.shape[-2:]), dtype=torch.uint8, device="cuda")
+    moe.moe_pack_weight_w4(q, s, packed, packed_s)
+    return packed, packed_s
+
+
 class Layer:
-    def __init__(self, seed=0):
+    def __init__(self, seed=0, weights4=False):
         g = torch.Generator(device="cuda").manual_seed(seed)
         heads = DIMS.q_heads + 2 * DIMS.kv_heads
 
         def draw(*shape):
             return torch.randn(shape, generator=g, device="cuda") / math.sqrt(shape[-1])
-        self.w_in = draw(heads * DIMS.head_dim, HIDDEN).bfloat16()
-        self.w_out = draw(HIDDEN, DIMS.q_heads * DIMS.head_dim).bfloat16()
+        self.weights4 = weights4
+        kept = packed4 if weights4 else torch.Tensor.bfloat16
+        self.w_in = kept(draw(heads * DIMS.head_dim, HIDDEN))
+        self.w_out = kept(draw(HIDDEN, DIMS.q_heads * DIMS.head_dim))
         self.w_router = draw(EXPERTS, HIDDEN).bfloat16()
+        self.norms = [(1 + draw(HIDDEN)).bfloat16() for _ in range(2)]
         self.experts = []
         for shape in ((EXPERTS, INTER, HIDDEN), (EXPERTS, INTER, HIDDEN), (EXPERTS, HIDDEN, INTER)):
-            w = draw(*shape)
-            q = torch.empty(shape, dtype=torch.uint8, device="cuda")
-            s = torch.empty((shape[0], shape[1] // 128, shape[2] // 128), device="cuda")
-            moe.moe_quant_weight(w, q, s)
-            packed = torch.empty_like(q)
-            moe.moe_pack_weight(q, packed)
-            self.experts += [packed, s]
+            self.experts += packed4(draw(*shape)) if weights4 else packed8(draw(*shape))
         self.table = torch.empty((POSITIONS, DIMS.head_dim), device="cuda")
         moe.moe_rope_table(self.table, base=500000.0, scaling=moe.MOE_ROPE_BY_PARTS, factor=4.0, original_len=1024.0)
 
+    def linear(self, x, w, outputs):
+        if not self.weights4:
+            return x @ w.t()
+        t, k = x.shape
+        out = torch.empty((t, outputs), dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(max(256, moe.moe_linear_w4_workspace(t, k, outputs)), dtype=torch.uint8, device="cuda")
+        moe.moe_linear_w4(x, *w, out, ws=ws)
+        return out
+
     def project(self, x):
         """Queries, keys and values as views of one projection."""
-        row = (torch.nn.functional.rms_norm(x.float(), (HIDDEN,)).bfloat16() @ self.w_in.t()).unflatten(1, (-1, DIMS.head_dim))
+        normed = torch.empty_like(x)
+        moe.moe_add_norm(x, self.norms[0], normed)
+        row = self.linear(normed, self.w_in, (DIMS.q_heads + 2 * DIMS.kv_heads) * DIMS.head_dim).unflatten(1, (-1, DIMS.head_dim))
         return row.split((DIMS.q_heads, DIMS.kv_heads, DIMS.kv_heads), dim=1)
 
     def finish(self, x, attended):
-        """The rest of the layer: output projection, router, routed experts."""
-        x = x + attended.flatten(1) @ self.w_out.t()
+        """The rest of the layer: output projection, residual and norm, router, routed experts."""
+        out = self.linear(attended.flatten(1), self.w_out, HIDDEN)
+        h, total = torch.empty_like(x), torch.empty_like(x)
+        moe.moe_add_norm(out, self.norms[1], h, residual=x, sum_out=total)
         t = x.shape[0]
-        h = torch.nn.functional.rms_norm(x.float(), (HIDDEN,)).bfloat16()
         ids = torch.empty((t, TOPK), dtype=torch.int32, device="cuda")
         weights = torch.empty((t, TOPK), device="cuda")
         ws = torch.empty(max(256, moe.moe_router_workspace(t, HIDDEN, EXPERTS)), dtype=torch.uint8, device="cuda")
         moe.moe_router(h, self.w_router, None, ids, weights, ws=ws)
-        buf = moe.MoELayerBuffers(HIDDEN, INTER, EXPERTS, TOPK, t, fused=True)
-        return x + moe.run_layer(buf, h, ids, weights, self.experts).view(torch.bfloat16)
+        buf = moe.MoELayerBuffers(HIDDEN, INTER, EXPERTS, TOPK, t, fused=True, w4=self.weights4)
+        return total + moe.run_layer(buf, h, ids, weights, self.experts).view(torch.bfloat16)
 
 
 def ints(values):
@@ -128,12 +160,13 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--tokens", type=int, default=300, help="tokens of the longest prompt")
     ap.add_argument("--steps", type=int, default=8)
+    ap.add_argument("--weights4", action="store_true", help="projections and experts with 4-bit weights")
     a = ap.parse_args()
     g = torch.Generator(device="cuda").manual_seed(1)
 
     def tokens(n):
         return torch.randn((n, HIDDEN), generator=g, device="cuda").bfloat16()
-    layer = Layer()
+    layer = Layer(weights4=a.weights4)
     prefix = tokens(200)
     prompts = [tokens(max(1, a.tokens // k)) for k in (1, 2, 5)]
     outputs = run(layer, prefix, prompts, [tokens(3) for _ in range(a.steps)])

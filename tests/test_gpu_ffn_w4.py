@@ -5,6 +5,9 @@ Bounds: G and U are off by H roundings of 2^-23 of their terms' sizes each, whic
 1.1; h = silu(G) U is rounded once to bf16 (2^-8) after a few roundings in fp32 (2^-20 covers them); y adds I roundings of
 2^-23 of its own terms' sizes.
 """
+import importlib.util
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -14,6 +17,7 @@ from oracle import w4_oracle as wo
 from w4_cases import ordinary, packed, values
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -308,3 +312,23 @@ def test_a_layer_from_norm_to_norm(moe, tokens):
         bound.index_add_(0, t, (off + 2.0 ** -21 * rows_y.abs()) * p_h[t, j][:, None])
     near(y, ref, bound + 2.0 ** -8 * (ref.abs() + bound))
     assert int(layer.dev_status.item()) == 0 and int(buf.dev_status.item()) == 0
+
+
+def test_the_examples_layer_with_such_weights(moe):
+    """A token by a step against the same token as its prompt's last: what differs is the cache's e4m3 rows, as with other
+    weights, so the hidden states are a few percent off at most."""
+    spec = importlib.util.spec_from_file_location("decoder_layer", os.path.join(ROOT, "examples", "decoder_layer.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    g = torch.Generator(device="cuda").manual_seed(3)
+
+    def tokens(n):
+        return torch.randn((n, ex.HIDDEN), generator=g, device="cuda").bfloat16()
+    layer, prefix, prompts = ex.Layer(weights4=True), tokens(100), [tokens(70), tokens(33)]
+    new = tokens(2)
+    by_step = ex.run(layer, prefix, prompts, [new])[1]
+    whole = ex.run(layer, prefix, [torch.cat([p, new[i:i + 1]]) for i, p in enumerate(prompts)], [])[0]
+    by_prompt = whole[[70, 70 + 34]]
+    off = ((by_step - by_prompt).float().norm() / by_prompt.float().norm()).item()
+    log(f"step against prompt: {off:.4f}")
+    assert off < 0.1
