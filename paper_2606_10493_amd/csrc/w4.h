@@ -16,8 +16,8 @@ constexpr int kW4ScaleTile = 16 * kW4ScaleCols / kW4Group;  // bytes of 16 rows'
 constexpr int kW4MaxScale = 252;
 
 // Eight e2m1 codes (a dword, the first column lowest) times 2^(byte - 127) -> eight
-// bf16.  Exact: one bit of mantissa.  `scale` is the byte in an fp32's exponent field,
-// where the instruction takes it from.
+// bf16.  Exact: one bit of mantissa.  The instruction takes the exponent field of
+// `scale` and nothing else of it (every byte, with 16384 signs and mantissas each: the same bits).
 __device__ __forceinline__ w4_bf16x8 w4_expand(uint32_t codes, float scale) {
   const w4_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
   const w4_bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
@@ -26,9 +26,9 @@ __device__ __forceinline__ w4_bf16x8 w4_expand(uint32_t codes, float scale) {
   return w4_bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Byte j of a row's four scales of a 128-column block, as w4_expand takes it.
+// Byte j of a row's four scales of a 128-column block in the exponent field, as w4_expand takes it; other bytes around it.
 __device__ __forceinline__ float w4_scale(uint32_t four, int j) {
-  return __uint_as_float((j == 3 ? four >> 1 : four << (23 - 8 * j)) & 0x7f800000u);
+  return __uint_as_float(j == 3 ? four >> 1 : four << (23 - 8 * j));
 }
 
 inline int64_t w4_scale_chunks(int32_t cols) { return ((int64_t)cols + kW4ScaleCols - 1) / kW4ScaleCols; }
