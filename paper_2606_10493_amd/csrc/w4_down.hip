@@ -43,6 +43,8 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, kq = lane >> 4;
   const int nb = p.K / kBlock, groups = p.N / 16, chunks = (nb + 3) / 4;
+  // (Loaded in front of the asm below, the list comes as scalars and waits for no other load.)
+  const int2 count = p.list[kSortSlots], own = p.list[wave];
   // The rows of h go out first, so that they are there when the first weights are.
   const int pieces = p.K / 8;
   {
@@ -53,8 +55,6 @@ __global__ __launch_bounds__(64 * kDownWaves, 4) void w4_down_combine_kernel(W4D
       async_load_1k(p.h + (int64_t)row * p.K + ((at - row * pieces) ^ (row & 15)) * 8, to + i * 16);
     }
   }
-  // (both loads go out together)
-  const int2 count = p.list[kSortSlots], own = p.list[wave];
   const int n = __builtin_amdgcn_readfirstlane(count.x);
 
   struct Blocks {
