@@ -22,12 +22,12 @@ constexpr int kFewRows = 16;  // rows of one matrix that w4_few takes
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Experts with a few rows each, whose weights are many: w4_few streams them faster than the GEMM's smallest tiles (7168 x
-// 2048, 256 experts: 376 against 418 us a layer at 16 tokens, 777 against 842 at 64, 1002 against 1051 at 256), and slower
-// where an expert's run is short (2048 x 768, 128 experts: 76 against 64 us at 33 tokens; 4096 x 1536, 16 experts: 45
-// against 38 at 16).
+// Experts with a few rows each: w4_few streams their weights faster than the GEMM's smallest tiles (a layer of 7168 x 2048,
+// 256 experts of 8 a token: 380 against 428 us at 16 tokens, 832 against 893 at 64, 1010 against 1026 at 256; 2048 x 768,
+// 128 experts of 8: 53 against 61 at 16, 78 against 75 at 128; 4096 x 1536, 16 experts of 2: 46 against 49 at 33, 48
+// against 49 at 64), and slower where they have more than 8 (the same layers, 12 rows: 89 against 78 and 54 against 49).
 bool few_experts(const W4Args& a, int64_t rows) {
-  return (int64_t)a.N * a.K >= (1 << 23) && rows <= kFewMaxRows && rows <= 8 * (int64_t)a.E && w4_few_fits(a.K);
+  return rows <= kFewMaxRows && rows <= 8 * (int64_t)a.E && w4_few_fits(a.K);
 }
 
 moe_status_t run_experts(const W4Args& a, bool gateup, int64_t rows, hipStream_t stream) {
