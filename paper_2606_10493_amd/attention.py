@@ -21,14 +21,14 @@ from ._lib import MoeAttnDims, MoeKvCache, MoeRopeCfg, MOE_ROPE_HALF, MOE_ROPE_P
 
 
 class _NoBinding:
-    """Stands for a binding that is not there: the rest of the package works, every attention call says why it does not."""
+    """Stands for a binding that is not there: the rest of the package works, every call that needs it says why it does not."""
 
     def __init__(self, why: str):
         self.why = why
 
     def __getattr__(self, name):
-        raise ImportError(f"_binding.so, which the attention calls need, cannot be loaded ({self.why}); build it with "
-                          "`python paper_2606_10493_amd/build.py`")
+        raise ImportError(f"_binding.so, which the attention calls, the norm and the calls with 4-bit weights need, cannot be "
+                          f"loaded ({self.why}); build it with `python paper_2606_10493_amd/build.py`")
 
 
 try:

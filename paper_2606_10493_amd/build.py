@@ -1,5 +1,6 @@
 """Build libmoe.so (the HIP kernels and the C ABI) in-tree for gfx950, and
-_binding.so, the attention calls' native Python binding.
+_binding.so, the native Python binding of the attention calls, the norm and the
+calls with 4-bit weights.
 
     python paper_2606_10493_amd/build.py
 
@@ -9,7 +10,7 @@ Every .hip file under csrc/ is compiled with hipcc in parallel and linked
 into paper_2606_10493_amd/libmoe.so.  It compiles on a machine without a
 GPU (hipcc cross-compiles for gfx950).  csrc/binding.cpp is compiled with g++
 against the Python and torch headers and linked with libmoe.so; where one of
-these is missing the library is built all the same, and the attention calls
+these is missing the library is built all the same, and these calls
 are left without their Python binding.
 """
 from __future__ import annotations
@@ -70,7 +71,8 @@ def build_binding() -> bool:
     except ImportError:
         missing = "torch"
     if missing:
-        print(f"_binding.so is not built, the attention calls have no Python binding: {missing} is missing", file=sys.stderr)
+        print("_binding.so is not built, the attention calls, the norm and the calls with 4-bit weights have no Python "
+              f"binding: {missing} is missing", file=sys.stderr)
         return False
     lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
     include = os.path.join(os.path.dirname(torch.__file__), "include")

@@ -1,5 +1,6 @@
 // The Python binding of the attention calls, the norm and the calls with 4-bit
-// weights: checks of the tensors and the call of the C ABI in one native function each.  A decode step makes these calls for every
+// weights: checks of the tensors and the call of the C ABI in one native function
+// each.  A decode step makes these calls for every
 // layer and is bound by the host: moe_rope_cache takes 3 us of it here, most of
 // them the launch, and 9 with the same checks in Python and ctypes.
 //
@@ -486,7 +487,8 @@ PyMethodDef kMethods[] = {method<rope, 10>("rope"),
                           method<ffn_layer_w4, 15>("ffn_layer_w4"),
                           {nullptr, nullptr, 0, nullptr}};
 
-PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", "The attention calls, the norm and the calls with 4-bit weights of libmoe.so on torch tensors.", -1, kMethods};
+PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding",
+                       "The attention calls, the norm and the calls with 4-bit weights of libmoe.so on torch tensors.", -1, kMethods};
 
 }  // namespace
 

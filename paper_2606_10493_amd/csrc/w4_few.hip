@@ -1,5 +1,8 @@
 // Products of up to 16 rows a matrix with 4-bit weights: every weight is read once
-// and the kernel is bound by that stream.
+// and the kernel is bound by that stream.  (64 tokens of Zipf routing, gate/up of 256
+// experts of 7168 x 2048: 2.2 GB in 358 us, 6.1 TB/s, where a plain read reaches 7.0; down:
+// 1.1 GB in 210 us.  One token, gate/up: 125 MB in 24.9 us, 8 of them for the launch, the
+// sort and the first weights' way, then 7.4 TB/s.  One row by 16384 x 7168: 62 MB in 13.0 us.)
 //
 // An item is R tiles of 16 weight rows (with GATEUP half of them W_gate's and half
 // the same rows of W_up) against a tile of up to 16 activation rows.  A workgroup
@@ -8,7 +11,11 @@
 // NBW w + NBW - 1 in registers from one item to the next and streams those blocks
 // of the weights; the waves' sums are added through LDS in wave order.  So the loop
 // over items loads weights and scales alone.  D items are in flight: a register is
-// loaded again, for the item D further on, as soon as it has been used.
+// loaded again, for the item D further on, as soon as it has been used.  (With a workgroup
+// an item, which loads its activations, that one token's layer took 72.6 us, so 53.0.)
+// NBW is 1, 2, 4 or 8: a line of 128 bytes of scales that one wave asks for while another's load
+// has it on its way stalls both, and with these no line is two waves' (3 and 5 blocks a wave, which
+// would leave no wave without work, took 42.2 us for the layer against 40.4).
 //
 // The matrix instruction is 16x16x32 bf16 with the weights as its first operand:
 // 32 columns are one scale group, expanded to bf16 with the scale in it, and a

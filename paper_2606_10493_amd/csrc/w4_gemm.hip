@@ -9,6 +9,15 @@
 // each number has its own loop, so that an expert's rows are cut into equal tiles whose
 // size follows them.
 //
+// Small tiles are bound by the expansion (an operand of 32 K takes four conversions of 6.5 cycles; a
+// step of 32 activation rows 0.5 us), or by the weights' stream where one row tile has them all
+// (24 rows by 7168 x 65536 to fp32: 48.6 us, 5.3 TB/s); large ones by the matrix cores and the
+// power that they draw (8192 rows by 7168 x 4096: 336 us, 1.43 PFLOP/s, where the library's product
+// of bf16 weights takes 365; 4095 tokens of 8 of 256 experts of 7168 x 2048: gate and up 1.60 ms,
+// 1.20 PFLOP/s, down 0.97 ms with 0.94 GB of sums).  With four waves, one to
+// a SIMD, and tiles of 128 rows that layer took 4359 us, with eight and equal tiles 3077; up to six stages instead of three 50.4
+// against 48.8 us (24 rows); the scales of four steps in one load as long as a step's.
+//
 // Steps of 128 K.  Activations (256 bytes a row), codes (1 KB a tile of 16 rows) and
 // scales (one dword a row) go straight from global memory into LDS stages, one or
 // two steps ahead, with one barrier a step; activation rows are gathered on the

@@ -108,6 +108,13 @@ def test_layer(moe, h, i, e, k, tokens, skew):
     assert (off <= bound + (k + 1) * 2.0 ** -24 * size + 2.0 ** -8 * (ref.abs() + bound)).all()
 
 
+@pytest.mark.parametrize("h,i", [(128, 256), (512, 1024), (1024, 512), (640, 2176), (2048, 384), (4352, 128), (8192, 256)])
+@pytest.mark.parametrize("tokens", [24, 25])
+def test_layers_of_eight_rows_an_expert(moe, h, i, tokens):
+    """At eight rows an expert and behind it the kernel changes; some experts have two tiles of rows, some none."""
+    test_layer(moe, h, i, 12, 4, tokens, 1.5)
+
+
 @pytest.mark.parametrize("tokens", [1, 5, 64, 65, 300])
 def test_no_run_differs_from_another(moe, tokens):
     rng = np.random.default_rng(tokens)
