@@ -1,7 +1,7 @@
 // Products of many rows with 4-bit weights: an LDS-tiled bf16 GEMM that expands
 // the weights in registers on their way from LDS to the matrix instruction.
 //
-// A workgroup takes a tile of up to 32 S activation rows against 128 TILES weight rows
+// A workgroup takes a tile of up to 32 S activation rows against 128 TILES weight rows (1, 2 or 4)
 // (GATEUP: 64 TILES of W_gate and the same rows of W_up).  Each of its eight waves, two to a
 // SIMD, has 16 TILES weight rows and all activation rows, so that nothing is expanded
 // twice and the expansion of one wave of a SIMD runs beside the products of the
@@ -285,15 +285,18 @@ moe_status_t gemm_by_rows(const W4Args& a, int64_t rows, hipStream_t stream) {
 
 // How one matrix is cut, by the time that each cut is expected to need, in us: rounds of
 // 256 workgroups, each 4 and its steps, a step 0.15 and 0.0115 an activation row with
-// narrow tiles, 0.3 and 0.019 with wide ones; and for several parts of K a launch and their sums' way through
-// memory.  (20.3 us for 168 workgroups of 32 steps of 29 rows, 53.5 for 192 of 32 of 128; wide, 92.5 for
-// 192 of 32 of 128 rows and 338 for 512 of 56.)
+// narrow tiles, 0.3 and 0.019 with wide ones, 0.31 with the smallest; and for several parts of K a launch and
+// their sums' way through memory.  (20.3 us for 168 workgroups of 32 steps of 29 rows, 53.5 for 192 of 32 of 128; wide, 92.5 for
+// 192 of 32 of 128 rows and 338 for 512 of 56.  The smallest, 128 weight rows by 32, beside 256 by 32 in parts of K: 6.0
+// against 7.8 us for 100 rows by 1024 x 1536, 9.1 against 11.7 for 2048 x 7168, 14.0 against 16.7 for 4096 x
+// 6144; 128 by 64 instead: 35.5 against 33.0 for 512 rows by 7168 x 4096.)
 W4Cut w4_gemm_cut(int64_t rows, int32_t K, int32_t N) {
   const int nb = K / kBlock;
   constexpr struct {
     int S, tiles;
     double step, row;
-  } kKinds[] = {{1, 2, 0.15, 0.0115}, {2, 2, 0.15, 0.0115}, {4, 2, 0.15, 0.0115}, {3, 4, 0.3, 0.019}, {4, 4, 0.3, 0.019}, {5, 4, 0.3, 0.019}};
+  } kKinds[] = {{1, 1, 0.31, 0.0},   {1, 2, 0.15, 0.0115}, {2, 2, 0.15, 0.0115}, {4, 2, 0.15, 0.0115},
+                {3, 4, 0.3, 0.019}, {4, 4, 0.3, 0.019},   {5, 4, 0.3, 0.019}};
   W4Cut best{4, 2, 1};
   double best_us = 1e30;
   for (const auto& k : kKinds) {
@@ -316,6 +319,7 @@ moe_status_t run_w4_gemm(const W4Args& a, bool gateup, int64_t rows, hipStream_t
   if (a.offsets) return gateup ? gemm_by_rows<true>(a, rows, stream) : gemm_by_rows<false>(a, rows, stream);
   const W4Cut cut = w4_gemm_cut(rows, a.K, a.N);
   switch (10 * cut.tiles + cut.S) {
+    case 11: return launch_gemm<1, 1, false>(a, rows, stream);
     case 21: return launch_gemm<1, 2, false>(a, rows, stream);
     case 22: return launch_gemm<2, 2, false>(a, rows, stream);
     case 24: return launch_gemm<4, 2, false>(a, rows, stream);
