@@ -4,7 +4,7 @@
 // 1.1 GB in 210 us.  One token, gate/up: 125 MB in 24.9 us, 8 of them for the launch, the
 // sort and the first weights' way, then 7.4 TB/s.  One row by 16384 x 7168: 62 MB in 13.0 us.)
 //
-// An item is R tiles of 16 weight rows (with GATEUP half of them W_gate's and half
+// An item is R tiles of 16 weight rows, 2 or 1 (with GATEUP half of them W_gate's and half
 // the same rows of W_up) against a tile of up to 16 activation rows.  A workgroup
 // takes a run of neighbouring items, so neighbouring weights and mostly the same
 // activations: wave w keeps the activations' K blocks of 128 from NBW w to
@@ -279,9 +279,8 @@ int few_blocks(const W4Args& a) {
   return splits == 1 ? nb : 4 * (((nb + 3) / 4 + splits - 1) / splits);
 }
 
-template <int NBW, int D, FewMode MODE>
+template <int NBW, int D, FewMode MODE, int R = 2>
 moe_status_t launch_few(const W4Args& a, int rows, const W4Slots& slots, hipStream_t stream) {
-  constexpr int R = 2;
   constexpr bool kGateUp = MODE == kExpertsGateUp || MODE == kSlotsGateUp;
   const char* name = kGateUp ? "w4_few_gateup" : "w4_few";
   const int splits = std::max(1, a.splits);
@@ -302,6 +301,14 @@ moe_status_t launch_few(const W4Args& a, int rows, const W4Slots& slots, hipStre
 template <FewMode MODE>
 moe_status_t few_by_length(const W4Args& a, int rows, const W4Slots& slots, hipStream_t stream) {
   const int nb = few_blocks(a);
+  if constexpr (MODE == kDense) {
+    // Items of one tile where items of two leave half of the CUs without work (1, 16 rows by 7168 x 4096: 8.0, 11.6 against 8.9,
+    // 13.2 us; 4096 x 2048: 5.1, 7.1 against 5.6, 8.2; 192 items of two, 2048 x 6144: 5.1, 7.2 against 4.4, 5.6).
+    if (nb > 8 && (int64_t)a.N / 32 * std::max(1, a.splits) <= 128) {
+      if (nb <= 32) return launch_few<4, 1, MODE, 1>(a, rows, slots, stream);
+      return launch_few<8, 1, MODE, 1>(a, rows, slots, stream);
+    }
+  }
   if (nb <= 4) return launch_few<1, 4, MODE>(a, rows, slots, stream);
   if (nb <= 8) return launch_few<2, 2, MODE>(a, rows, slots, stream);
   if (nb <= 32) return launch_few<4, 1, MODE>(a, rows, slots, stream);

@@ -122,6 +122,12 @@ def test_whole_numbers_bit_for_bit(moe, k, n):
         assert torch.equal(out, (ref + bias.double()).float().bfloat16()), t
 
 
+@pytest.mark.parametrize("k,n", [(1152, 4176), (2048, 4096), (2048, 4128), (7168, 4144), (8192, 4112), (16384, 1024), (16384, 1072)])
+def test_whole_numbers_where_items_change(moe, k, n):
+    """Few rows: matrices on both sides of the size where a workgroup's item has one tile of rows or two, odd ones among them."""
+    test_whole_numbers_bit_for_bit(moe, k, n)
+
+
 @pytest.mark.parametrize("tokens", [1, 30, 64, 100, 300])
 def test_ordinary_values(moe, tokens):
     k, n = 2048, 528
