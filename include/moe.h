@@ -676,7 +676,9 @@ typedef struct {
  * H a multiple of 8, and of 128 with q, 8..32768; else
  * MOE_ERR_UNSUPPORTED_SHAPE.  Strides are multiples of 8 and at least heads * H;
  * pointers are 16-byte aligned (q 8, s 4).  z has to fit fp32; its squares need
- * not.  weight: device bf16 [H].
+ * not.  weight: device bf16 [H].  Values that are not finite show: a NaN in z makes its
+ * row NaN, an infinity itself NaN and the rest of its row 0, and blocks of 128
+ * with a NaN have NaN for their scale; other rows are not touched by it.
  */
 moe_status_t moe_add_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
                           const uint16_t* weight_bf16, int32_t T, int32_t H, moe_norm_cfg_t cfg, void* sum,

@@ -12,7 +12,8 @@
 // values (16 bytes of bf16): piece v of the row is lane v % LANES's, so that 16
 // neighbouring lanes hold a scale block.  Squares add up in fp32 (a lane's in
 // order, then across lanes); where the sum leaves fp32's range the row is
-// scaled by a power of two first, which changes no bit of the quotient.
+// scaled by a power of two first, which changes no bit of the quotient (but of
+// values that the row's largest exceeds 2^126 times: these lose bits, or are 0).
 #include <algorithm>
 
 #include "common.h"
@@ -42,17 +43,31 @@ struct NormArgs {
   float* s;
 };
 
+typedef float v8f __attribute__((ext_vector_type(8)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+
+// The conversion instruction, which keeps NaN: f32_to_bf16_rne rounds one of the largest payloads to a zero.  (Of all
+// 2^32 fp32 patterns the others come out as by f32_to_bf16_rne.)
 __device__ __forceinline__ uint4 to_bf16x8(const float (&v)[8]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w[i] = (uint32_t)f32_to_bf16_rne(v[2 * i]) | ((uint32_t)f32_to_bf16_rne(v[2 * i + 1]) << 16);
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  return __builtin_bit_cast(uint4, __builtin_convertvector((v8f{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}), v8bf));
 }
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) { *reinterpret_cast<uint4*>(p) = to_bf16x8(v); }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
   *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// quant_group8 with a maximum that NaN pass through: a block that holds one has NaN for its scale, and with the finite
+// codes of such values reads as NaN.  (By a maximum that passes over them it would read as zeros.)
+__device__ __forceinline__ float quant_group8_nan(const float (&v)[8], uint2& codes) {
+  float amax = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) amax = __builtin_elementwise_maximum(amax, fabsf(v[i]));
+#pragma unroll
+  for (int m = 8; m >= 1; m >>= 1) amax = __builtin_elementwise_maximum(amax, __shfl_xor(amax, m, 16));
+  const float sc = amax / kE4M3Max;
+  codes = make_uint2(quantize4_e4m3(v[0], v[1], v[2], v[3], sc), quantize4_e4m3(v[4], v[5], v[6], v[7], sc));
+  return sc;
 }
 
 // The sum (or the maximum) over a row's lanes, known to all of them.  `red`
@@ -179,7 +194,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void add_norm_kernel(Nor
       for (int i = 0; i < NV; ++i) {
         if (in[i]) {  // a scale block's 16 lanes together: H is a multiple of 128
           uint2 codes;
-          const float sc = quant_group8(z[i], codes);
+          const float sc = quant_group8_nan(z[i], codes);
           *reinterpret_cast<uint2*>(p.q + row * p.H + at[i]) = codes;
           if (at[i] % kBlock == 0) p.s[row * (p.H / kBlock) + at[i] / kBlock] = sc;
         }
