@@ -741,7 +741,8 @@ moe_status_t moe_pack_weight_w4(const uint8_t* q, const uint8_t* s, int32_t n_ma
  * device bf16 or fp32, rows out_stride elements apart (a multiple of 8, at least
  * N); rows and columns outside [T, N] are not written.  All pointers 16-byte
  * aligned (bias 8); out overlaps nothing.  ws: moe_linear_w4_workspace(T, K, N) bytes,
- * 256-byte aligned; no smaller T needs more.
+ * 256-byte aligned: sums of parts of K, 0 where it is multiplied whole; no smaller T
+ * needs more.
  */
 size_t moe_linear_w4_workspace(int32_t T, int32_t K, int32_t N);
 moe_status_t moe_linear_w4(const uint16_t* x_bf16, int64_t x_stride, int32_t T, int32_t K, const uint8_t* w,

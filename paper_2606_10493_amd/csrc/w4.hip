@@ -37,6 +37,14 @@ moe_status_t run_experts(const W4Args& a, bool gateup, int64_t rows, hipStream_t
 // One matrix: whether w4_few takes it.
 bool few_linear(int32_t T, int32_t K) { return T <= kFewRows && w4_few_parts(K) <= w4_most_parts(kFewRows); }
 
+// Parts of K that one matrix is multiplied in.
+int linear_parts(int32_t T, int32_t K, int32_t N) {
+  return few_linear(T, K) ? w4_few_parts(K) : w4_gemm_cut(T, K, N).parts;
+}
+
+// Bytes of the sums of `rows` = parts * T rows.
+size_t sums_bytes(int64_t rows, int32_t N) { return align256((size_t)rows * N * sizeof(float)); }
+
 // out = the parts' sums in their order (+ bias), four neighbouring outputs a lane.
 __global__ __launch_bounds__(256) void w4_join_kernel(W4Args p) {
   const int n = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 4;
@@ -140,12 +148,19 @@ using namespace moe;
 
 extern "C" size_t moe_linear_w4_workspace(int32_t T, int32_t K, int32_t N) {
   if (T <= 0 || K <= 0 || N <= 0 || K % kBlock || N % 16) return 0;
-  // Sums of the parts of K.  No smaller T needs more.
-  if (few_linear(T, K)) {
-    const int parts = w4_few_parts(K);
-    return parts > 1 ? align256((size_t)parts * T * N * sizeof(float)) : 0;
+  // Sums of the parts of K, of this T and every smaller one.  Of 16 j + 1 to 16 j + 16 rows the first has the most parts:
+  // within them a cut's estimate grows by its sums alone, and by more the more parts it has.
+  int64_t most = 0;
+  int32_t first = 1;
+  if (few_linear(1, K)) {
+    if (w4_few_parts(K) > 1) most = (int64_t)w4_few_parts(K) * std::min(T, kFewRows);
+    first = kFewRows + 1;
   }
-  return align256((size_t)std::min<int64_t>(16 * (int64_t)T, 1024) * N * sizeof(float));
+  for (; first <= T && w4_most_parts(first) > 1; first += 16) {
+    const int parts = w4_gemm_cut(first, K, N).parts;
+    if (parts > 1) most = std::max(most, (int64_t)parts * std::min(T, first + 15));
+  }
+  return sums_bytes(most, N);
 }
 
 extern "C" moe_status_t moe_linear_w4(const uint16_t* x, int64_t x_stride, int32_t T, int32_t K, const uint8_t* w,
@@ -162,7 +177,8 @@ extern "C" moe_status_t moe_linear_w4(const uint16_t* x, int64_t x_stride, int32
   if (x_stride < K || x_stride % 8 || out_stride < N || out_stride % 8)
     return fail(MOE_ERR_INVALID_ARG, "moe_linear_w4: strides %lld of x, %lld of out must be multiples of 8, at least %d and %d",
                 (long long)x_stride, (long long)out_stride, K, N);
-  const moe_status_t st = check_workspace(ws, ws_bytes, moe_linear_w4_workspace(T, K, N), "moe_linear_w4");
+  const int parts = linear_parts(T, K, N);
+  const moe_status_t st = check_workspace(ws, ws_bytes, parts > 1 ? sums_bytes((int64_t)parts * T, N) : 0, "moe_linear_w4");
   if (st != MOE_OK) return st;
   W4Args a{};
   a.x = x; a.x_stride = x_stride; a.x_rows = T;
@@ -170,7 +186,7 @@ extern "C" moe_status_t moe_linear_w4(const uint16_t* x, int64_t x_stride, int32
   a.out32 = out_type == MOE_F32 ? static_cast<float*>(out) : nullptr;
   a.out16 = out_type == MOE_F32 ? nullptr : static_cast<uint16_t*>(out);
   a.out_stride = out_stride;
-  a.splits = few_linear(T, K) ? w4_few_parts(K) : w4_gemm_cut(T, K, N).parts;
+  a.splits = parts;
   a.partial = static_cast<float*>(ws);
   return run_linear(a, T, stream);
 }
