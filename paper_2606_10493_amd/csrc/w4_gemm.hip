@@ -247,7 +247,7 @@ template <int S, int TILES, bool GATEUP>
 moe_status_t launch_gemm(const W4Args& a, int64_t rows, hipStream_t stream) {
   const char* name = GATEUP ? "w4_gemm_gateup" : "w4_gemm";
   const int cols = gemm_rows(TILES) / (GATEUP ? 2 : 1);
-  const int n_tiles = (a.N + cols - 1) / cols;
+  const int n_tiles = (int)(((int64_t)a.N + cols - 1) / cols);
   const int64_t m_tiles = a.offsets ? rows / (32 * S) + (rows < a.E ? rows : (int64_t)a.E) : (rows + 32 * S - 1) / (32 * S);
   const bool dealt = m_tiles >= 4 * kXcd;
   const int64_t blocks = (dealt ? (m_tiles + kXcd - 1) / kXcd * kXcd : m_tiles) * n_tiles;
@@ -266,8 +266,9 @@ moe_status_t gemm_by_rows(const W4Args& a, int64_t rows, hipStream_t stream) {
   // 3582 3619 3305 3053; TILES = 4: 32 rows 1456 1226 1346 1347 1387, 64 rows 2302 1898 1706 1719 1719, 128 rows 4151
   // 3211 3251 2929 2786, 256 rows 7775 5996 5552 5366 5300.)
   const int64_t mean = rows / a.E;
-  const int cols = gemm_rows(4) / (GATEUP ? 2 : 1), n_tiles = (a.N + cols - 1) / cols;
-  const bool wide = (int64_t)n_tiles * cols * 7 <= (int64_t)a.N * 8 && std::min<int64_t>(rows, a.E) * n_tiles >= 256;
+  const int cols = gemm_rows(4) / (GATEUP ? 2 : 1);
+  const int64_t n_tiles = ((int64_t)a.N + cols - 1) / cols;
+  const bool wide = n_tiles * cols * 7 <= (int64_t)a.N * 8 && std::min<int64_t>(rows, a.E) * n_tiles >= 256;
   if (wide && mean > 12) {
     if (mean <= 52) return launch_gemm<2, 4, GATEUP>(a, rows, stream);
     if (mean <= 72) return launch_gemm<3, 4, GATEUP>(a, rows, stream);
