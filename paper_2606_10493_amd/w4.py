@@ -30,7 +30,9 @@ def _matrices(t, name):
 
 def _on_stream(stream, **tensors):
     import torch
-    device = torch.cuda.current_device() if stream is None else stream.device_index
+    device = getattr(stream, "device_index", None)  # an object that has a handle alone is of the current device
+    if device is None:
+        device = torch.cuda.current_device()
     for name, t in tensors.items():
         if t is not None and t.device.index != device:
             raise ValueError(f"{name} is on another device than the call's stream")
