@@ -14,6 +14,7 @@ constexpr int kW4TileBytes = 16 * kBlock / 2;          // 16 rows x 128 columns 
 constexpr int kW4ScaleCols = 512;                      // columns whose scales lie together
 constexpr int kW4ScaleTile = 16 * kW4ScaleCols / kW4Group;  // bytes of 16 rows' scales of them
 constexpr int kW4MaxScale = 252;
+constexpr int kW4NoScale = 255;
 
 // Eight e2m1 codes (a dword, the first column lowest) times 2^(byte - 127) -> eight
 // bf16.  Exact: one bit of mantissa.  The instruction takes the exponent field of

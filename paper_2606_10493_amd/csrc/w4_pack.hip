@@ -10,7 +10,8 @@ namespace {
 // One lane a group of 32 columns.  2^e is the smallest power of two with
 // max|w| <= 7 * 2^e: with 2^x <= max < 2^(x + 1) that is e = x - 2, or x - 1 where
 // the mantissa is above 1.75.  The division by 2^e is exact but for results far
-// below the smallest code.
+// below the smallest code.  The codes have no NaN and no infinity: a group with one
+// gets the scale byte kW4NoScale, which pack_scale_w4_kernel reports.
 __global__ __launch_bounds__(256) void quant_weight_w4_kernel(const float* __restrict__ w, int64_t groups,
                                                               uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
   for (int64_t g = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; g < groups; g += (int64_t)gridDim.x * blockDim.x) {
@@ -20,7 +21,7 @@ __global__ __launch_bounds__(256) void quant_weight_w4_kernel(const float* __res
     for (int i = 0; i < 4; ++i) {
       load8_f32(w + g * kW4Group + 8 * i, v[i]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[i][j]));
+      for (int j = 0; j < 8; ++j) top = __builtin_elementwise_maximum(top, fabsf(v[i][j]));  // NaN passes through
     }
     const uint32_t bits = __float_as_uint(top);
     int e = (int)(bits >> 23) - 127 - 2 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
@@ -40,7 +41,7 @@ __global__ __launch_bounds__(256) void quant_weight_w4_kernel(const float* __res
       }
     }
     *reinterpret_cast<uint4*>(q + g * (kW4Group / 2)) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
-    s[g] = (uint8_t)(e + 127);
+    s[g] = (uint8_t)(top < __builtin_huge_valf() ? e + 127 : kW4NoScale);
   }
 }
 
