@@ -704,11 +704,11 @@ moe_status_t moe_add_norm(const void* x, int64_t x_stride, const void* residual,
  * Weight quantization, w: device fp32 [n_mats, rows, cols] -> q: device
  * [n_mats, rows, cols / 2], s: device [n_mats, rows, cols / 32].  Per group: the
  * smallest scale 2^e, -120 <= e <= 120, that leaves no magnitude above 7 * 2^e
- * (so that none is off by more than half a step of the codes there), code = nearest e2m1 of w / 2^e,
- * ties to the even code, above 6 the 6; a value that rounds to zero keeps its
- * sign.  A group with a NaN or an infinity gets the scale byte 255, which
- * moe_pack_weight_w4 reports.  rows >= 1, cols a multiple of 32; w and q 16-byte aligned.  Offline, like
- * moe_quant_weight.
+ * (so that none is off by more than half a step of the codes there), code =
+ * nearest e2m1 of w / 2^e, ties to the even code, above 6 the 6; a value that
+ * rounds to zero keeps its sign.  A group with a NaN or an infinity gets the
+ * scale byte 255, which moe_pack_weight_w4 reports.  rows >= 1, cols a multiple
+ * of 32; w and q 16-byte aligned.  Offline, like moe_quant_weight.
  */
 moe_status_t moe_quant_weight_w4(const float* w, int32_t n_mats, int32_t rows, int32_t cols, uint8_t* q, uint8_t* s,
                                  hipStream_t stream);

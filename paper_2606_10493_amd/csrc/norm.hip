@@ -5,8 +5,8 @@
 // once and stays in registers between the sum of squares and the outputs, so
 // the kernel is bound by memory: 2 or 4 bytes a value each for x, residual and
 // sum, 2 for out, 1 + 1/32 for the codes.  (8192 rows of 7168, bf16 x, fp32 residual and
-// sum, out and codes: 151 us, 5.1 TB/s, a little more than a plain copy reaches; 509 tokens of
-// 40 rows of 128: 4.1 us; one row of 7168: 4.4 us, a launch and the two round trips to memory.)
+// sum, out and codes: 150 us, 5.1 TB/s, a little more than a plain copy reaches; 509 tokens of
+// 40 rows of 128: 4.1 us; one row of 7168: 4.2 us, a launch and the two round trips to memory.)
 //
 // LANES lanes of a 256-thread workgroup share a row, each holding NV pieces of 8
 // values (16 bytes of bf16): piece v of the row is lane v % LANES's, so that 16

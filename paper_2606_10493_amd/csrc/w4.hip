@@ -93,6 +93,8 @@ moe_status_t check_workspace(const void* ws, size_t have, size_t need, const cha
   return MOE_OK;
 }
 
+// h is bf16: the matrix instruction of the down projection takes 16 bits, and h in two such parts would double its
+// products.  (2.3e-3 of the output's norm against 1.7e-3 for the output's own rounding.)  All sums are fp32.
 W4Args gateup_args(const moe_dims_t& d, int32_t T, const uint16_t* x, const uint8_t* const (&w)[6], uint16_t* h) {
   W4Args g{};
   g.x = x; g.x_stride = d.hidden; g.x_rows = T; g.topk = d.topk; g.E = d.n_experts;

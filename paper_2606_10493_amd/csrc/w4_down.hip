@@ -8,7 +8,7 @@
 // 62 MB in 14 us, 7 of them for the launch and the dependent loads (the list, the weights) before the
 // stream and the combine behind it; with a combine of its own the layer took 7 us more.  The sums of a row tile are
 // the same as w4_few's but for their order in K; the combine is the definition's order
-// (see moe_combine).
+// (see moe_combine).  Three values are kept in scratch memory, outside of the product loops.
 #include "w4.h"
 #include "w4_rows.h"
 

@@ -9,14 +9,16 @@
 // each number has its own loop, so that an expert's rows are cut into equal tiles whose
 // size follows them.
 //
-// Small tiles are bound by the expansion (an operand of 32 K takes four conversions of 6.5 cycles; a
-// step of 32 activation rows 0.5 us), or by the weights' stream where one row tile has them all
-// (24 rows by 7168 x 65536 to fp32: 48.6 us, 5.3 TB/s); large ones by the matrix cores and the
-// power that they draw (8192 rows by 7168 x 4096: 336 us, 1.43 PFLOP/s, where the library's product
+// Small tiles pay the expansion for few rows (an operand of 32 K takes four conversions of 6.5 cycles,
+// 0.17 us of a step; with 32 activation rows a step takes 0.5 us), or are bound by the weights' stream where one row
+// tile has them all (24 rows by 7168 x 65536 to fp32: 48 us, 5.3 TB/s); large ones by the matrix cores and the
+// power that they draw (8192 rows by 7168 x 4096: 326 to 336 us, 1.43 to 1.48 PFLOP/s, where the library's product
 // of bf16 weights takes 365; 4095 tokens of 8 of 256 experts of 7168 x 2048: gate and up 1.60 ms,
 // 1.20 PFLOP/s, down 0.97 ms with 0.94 GB of sums).  With four waves, one to
 // a SIMD, and tiles of 128 rows that layer took 4359 us, with eight and equal tiles 3077; up to six stages instead of three 50.4
-// against 48.8 us (24 rows); the scales of four steps in one load as long as a step's.
+// against 48.8 us (24 rows); the scales of four steps in one load as long as a step's.  The widest tiles
+// (S = 5, TILES = 4) leave no register over: 28 bytes are kept in scratch memory, of which the loop of ten parts reads three
+// or four values back a step.
 //
 // Steps of 128 K.  Activations (256 bytes a row), codes (1 KB a tile of 16 rows) and
 // scales (one dword a row) go straight from global memory into LDS stages, one or
